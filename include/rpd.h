@@ -46,8 +46,9 @@ extern "C" {
 
 #define RPD_ABI_VERSION 3
 
-/* element type of `hidden` and `w_u` (both must have the same type) */
-enum { RPD_DTYPE_BF16 = 0, RPD_DTYPE_F32 = 1 };
+/* element types: `hidden` and `w_u` of the commit step are RPD_DTYPE_BF16 or
+ * RPD_DTYPE_F32 (both the same); RPD_DTYPE_F16 exists in the operators that name it */
+enum { RPD_DTYPE_BF16 = 0, RPD_DTYPE_F32 = 1, RPD_DTYPE_F16 = 2 };
 
 typedef enum rpd_status {
   RPD_OK = 0,
@@ -358,6 +359,191 @@ int32_t rpd_projection_variant(const rpd_problem* p);
 rpd_status rpd_apply_commit(int32_t B, int32_t L, uint8_t* mask, int32_t* canvas, const uint8_t* commit,
                             const int32_t* token, int32_t* progress, int32_t progress_len, int32_t* step,
                             void* stream);
+
+/* ------------------------------------------------------------------------
+ * Operators around the commit step: an output head with 4-bit weights, the
+ * verification of drafted tokens, and the distillation of a drafter. The
+ * conventions above hold for them too. Random numbers are inputs. Element
+ * types are RPD_DTYPE_BF16, RPD_DTYPE_F16 and RPD_DTYPE_F32 as each entry
+ * says; strides are in elements, the last dimension is contiguous, and rows
+ * need no alignment beyond their element's. NaN and infinities follow IEEE
+ * arithmetic and stay in the row (sequence) that holds them.
+ */
+
+/*
+ * An output head with 4-bit weights and group scales:
+ *   W[v][k] = scales[v][k / group] * (code[v][k] - zeros[v][k / group])
+ *   V, d        1 <= V < 2^28, 8 <= d <= 2^20, d % 8 == 0, V * d <= 2^36
+ *   group       32, 64 or 128 columns that share a scale; the last group of a
+ *               row may be shorter
+ *   dtype       RPD_DTYPE_BF16 or RPD_DTYPE_F16: type of the scales and of
+ *               the rows that are projected
+ *   has_zeros   0: every zero point is 8; 1: zero points 0..15 are given
+ * The codes are laid out once, by rpd_quant_pack, for the matrix cores.
+ */
+typedef struct rpd_quant_head {
+  int32_t V, d, group, dtype, has_zeros;
+} rpd_quant_head;
+
+/* Bytes of the packed head (about V * d / 2 plus 2 or 3 per group); 0 if `h`
+ * is out of range. */
+size_t rpd_quant_packed_size(const rpd_quant_head* h);
+
+/*
+ * Lays a head out into `packed` (device, rpd_quant_packed_size bytes, 256-byte
+ * aligned), which rpd_quant_project then reads in place of the inputs.
+ *   codes   device [V][d/2] uint8; byte j of a row holds column 2j in its low
+ *           and column 2j+1 in its high nibble
+ *   scales  device [V][ceil(d / group)] of type dtype
+ *   zeros   device [V][ceil(d / group)] uint8 (low nibble), NULL without has_zeros
+ */
+rpd_status rpd_quant_pack(const rpd_quant_head* h, const uint8_t* codes, const void* scales, const uint8_t* zeros,
+                          void* packed, size_t packed_bytes, void* stream);
+
+/* Workspace bytes that rpd_quant_project needs for M rows (0 without the
+ * statistics; 0 too if h or M is out of range). */
+size_t rpd_quant_workspace_size(const rpd_quant_head* h, int32_t M, int32_t statistics);
+
+/*
+ * M rows through the head: logits y = W x, or the softmax statistics of
+ * logit_scale * y as rpd_gate_commit takes them (the logits then never reach
+ * memory). Exactly one of `logits` and the three statistics is given. Codes
+ * are exact operands and sums are float32; x is exact up to 2^-28 of the
+ * row's largest finite magnitude. Equal rows of the head give equal logits;
+ * of equal logits the lowest index is the argmax.
+ *   M          0 <= M <= 2^20 (0: nothing is done)
+ *   x          device [M][d] of type dtype, rows x_stride >= d apart
+ *   logits     device [M][V], rows logits_stride >= V apart, of type
+ *              logits_dtype: dtype or RPD_DTYPE_F32; or NULL
+ *   argmax, confidence, entropy   device [M] int32 / float / float (top
+ *              probability, nats); all given or all NULL
+ *   logit_scale  finite and > 0, or 0 for 1; the statistics only
+ *   workspace  rpd_quant_workspace_size bytes, 256-byte aligned (may be NULL
+ *              for logits); its prior contents do not matter
+ * The codes are streamed once for up to 32 rows (16 above d = 4096); the
+ * workgroups of further rows read them at the same time, through the caches.
+ */
+rpd_status rpd_quant_project(const rpd_quant_head* h, const void* packed, int32_t M, const void* x, int64_t x_stride,
+                             void* logits, int64_t logits_stride, int32_t logits_dtype, int32_t* argmax,
+                             float* confidence, float* entropy, float logit_scale, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+#define RPD_VERIFY_GREEDY 1u /* accept a drafted token iff it is the target's argmax */
+
+/*
+ * Verification of drafted tokens (speculative decoding; a draft may come from
+ * parallel commitments). With p_t = softmax(target_scale * target[b][t]) and
+ * q_t = softmax(draft_scale * draft[b][t]), token x_t = token[b][t] of the
+ * len[b] drafted ones is accepted with probability
+ *   accept[b][t] = min(1, p_t(x_t) / q_t(x_t)),
+ * that is while u[b][t] < accept[b][t]; the first that is not ends it. After n
+ * accepted tokens one more is drawn: from max(0, p_n - q_n) where x_n was
+ * turned down (from p_n if that is empty), from p_n where the draft ended:
+ * the lowest v whose running sum exceeds r[b] times the whole. Without draft
+ * logits (a draft that names one token with certainty) q_t is 1 at x_t.
+ *   B, T, V    B >= 1, T >= 0 drafted tokens at most, 1 <= V <= 2^28,
+ *              B * (T + 1) <= 2^20; together with V bounded by what one launch
+ *              holds (logits of 100 GB are far below that)
+ *   dtype      of the logits: RPD_DTYPE_BF16, _F16 or _F32
+ *   target     device [B][T+1][V]; row t is the target's after the first t
+ *              drafted tokens. Rows behind the draft (t > len) are not read
+ *   draft      device [B][T][V] or NULL; rows t >= len are not read
+ *   token      device [B][T]; one outside 0..V-1 is never accepted
+ *   len        device [B], read as within 0..T, or NULL: T everywhere
+ *   u, r       device [B][T] and [B] float32 in [0, 1)
+ *   target_scale, draft_scale   inverse temperatures, finite and > 0, or 0 for 1
+ *   flags      RPD_VERIFY_GREEDY: x_t is accepted iff it is the target's
+ *              argmax (lowest index of equals, NaN never), and the further
+ *              token is an argmax; draft, u, r and the scales are not used
+ *   out_token  device [B][T+1] int32: the accepted tokens, the further one, -1
+ *              behind it. The further token is -1 too where p_n has no
+ *              distribution (NaN, +inf or nothing but -inf in the row)
+ *   n_accept   device [B] int32
+ *   accept     device [B][T] float32 (greedy: 1 or 0); 0 for t >= len; NaN
+ *              where p_t or q_t has no distribution or both are 0 at x_t
+ * Acceptance probabilities carry float32 sums; the drawn token's sums are
+ * float64.
+ */
+typedef struct rpd_verify {
+  int32_t B, T, V, dtype;
+  const void* target;
+  int64_t target_batch_stride, target_row_stride;
+  const void* draft;
+  int64_t draft_batch_stride, draft_row_stride;
+  const int32_t* token;
+  const int32_t* len;
+  const float* u;
+  const float* r;
+  float target_scale, draft_scale;
+  uint32_t flags;
+  int32_t* out_token;
+  int32_t* n_accept;
+  float* accept;
+} rpd_verify;
+
+/* Workspace bytes of rpd_verify_draft (pointers only tested for NULL); 0 if
+ * the shape is out of range. */
+size_t rpd_verify_workspace_size(const rpd_verify* p);
+rpd_status rpd_verify_draft(const rpd_verify* p, void* workspace, size_t workspace_bytes, void* stream);
+
+#define RPD_DISTILL_MAX_K 256 /* longest list of a teacher's tokens */
+#define RPD_DISTILL_STATE 8   /* floats kept per row between the loss and the gradient */
+
+/*
+ * Distillation from a teacher's top logits. For row n of the student's
+ * logits, q = softmax(logit_scale * logits[n]); the teacher's list gives
+ * p_j for its tokens: the softmax of logit_scale * teacher[n] over the list,
+ * or, with teacher_lse, e^(logit_scale * teacher[n][j] - teacher_lse[n]), the
+ * rest p_T = max(0, 1 - sum p_j) then being one entry for all tokens outside
+ * the list (student's mass q_T).
+ *   loss[n] = weight[n] * (sum_j p_j ln(p_j / q_j) + p_T ln(p_T / q_T))
+ *   grad[n] = weight[n] * grad_loss[n] * d loss_n / d logits[n]
+ * Rows are independent (the masked positions of a canvas, say).
+ *   N, V, k    0 <= N <= 2^24 (0: nothing is done), 1 <= V <= 2^20,
+ *              1 <= k <= RPD_DISTILL_MAX_K; together bounded by what one launch
+ *              holds (logits of 100 GB are far below that)
+ *   dtype      of logits and grad: RPD_DTYPE_BF16, _F16 or _F32
+ *   logits     device [N][V], rows logits_stride >= V apart
+ *   id         device [N][k]; an entry outside 0..V-1 is no part of the list
+ *              (shorter lists are padded with -1); a token listed twice has
+ *              the sum of its entries
+ *   teacher    device [N][k] of type teacher_dtype (any of the three); -inf is
+ *              probability 0
+ *   teacher_lse  device [N] float32 or NULL: log-sum-exp of logit_scale times
+ *              all of the teacher's logits
+ *   weight     device [N] float32 or NULL (1): a row of weight 0 is not read,
+ *              its loss and gradient are 0 (unmasked positions)
+ *   grad_loss  device [N] float32 or NULL (1): the upstream gradient
+ *   loss       device [N] float32
+ *   state      device [N][RPD_DISTILL_STATE] float32: what the gradient needs
+ *              of the loss
+ *   grad       device [N][V], rows grad_stride >= V apart
+ * A list without entries (or of probability 0 without teacher_lse) has loss
+ * and gradient 0. A list token of student probability 0 makes the loss inf.
+ */
+typedef struct rpd_distill {
+  int32_t N, V, k, dtype, teacher_dtype;
+  const void* logits;
+  int64_t logits_stride;
+  const int32_t* id;
+  const void* teacher;
+  const float* teacher_lse;
+  const float* weight;
+  const float* grad_loss;
+  float logit_scale;
+  float* loss;
+  float* state;
+  void* grad;
+  int64_t grad_stride;
+} rpd_distill;
+
+/* Workspace bytes of the entries below; 0 if N, V or k is out of range or N is 0. */
+size_t rpd_distill_workspace_size(const rpd_distill* p);
+/* loss and state; and, where `grad` is given, the gradient in the same pass */
+rpd_status rpd_distill_loss(const rpd_distill* p, void* workspace, size_t workspace_bytes, void* stream);
+/* the gradient, from the state that rpd_distill_loss left for the same inputs
+ * (`loss` is not used; needs no workspace) */
+rpd_status rpd_distill_grad(const rpd_distill* p, void* stream);
 
 /* Static text for a status code. */
 const char* rpd_status_string(rpd_status s);

@@ -17,6 +17,7 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "librpd.so"
 
 DTYPE_BF16 = 0
 DTYPE_F32 = 1
+DTYPE_F16 = 2   # the operators beside the commit step only
 
 FLAG_CANDIDATE = 1
 FLAG_HIGH_CONF = 2
@@ -46,6 +47,30 @@ class RpdParams(ctypes.Structure):
                 ("w", ctypes.c_float), ("k_max", ctypes.c_int32), ("beta", ctypes.c_float),
                 ("window", ctypes.c_int32), ("flags", ctypes.c_uint32), ("block", ctypes.c_int32),
                 ("logit_scale", ctypes.c_float)]
+
+
+class RpdQuantHead(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("V", "d", "group", "dtype", "has_zeros")]
+
+
+class RpdVerify(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("target", ctypes.c_void_p), ("target_batch_stride", ctypes.c_int64),
+                ("target_row_stride", ctypes.c_int64),
+                ("draft", ctypes.c_void_p), ("draft_batch_stride", ctypes.c_int64),
+                ("draft_row_stride", ctypes.c_int64),
+                ("token", ctypes.c_void_p), ("len", ctypes.c_void_p), ("u", ctypes.c_void_p), ("r", ctypes.c_void_p),
+                ("target_scale", ctypes.c_float), ("draft_scale", ctypes.c_float), ("flags", ctypes.c_uint32),
+                ("out_token", ctypes.c_void_p), ("n_accept", ctypes.c_void_p), ("accept", ctypes.c_void_p)]
+
+
+class RpdDistill(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("V", ctypes.c_int32), ("k", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("teacher_dtype", ctypes.c_int32),
+                ("logits", ctypes.c_void_p), ("logits_stride", ctypes.c_int64), ("id", ctypes.c_void_p),
+                ("teacher", ctypes.c_void_p), ("teacher_lse", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("grad_loss", ctypes.c_void_p), ("logit_scale", ctypes.c_float), ("loss", ctypes.c_void_p),
+                ("state", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("grad_stride", ctypes.c_int64)]
 
 
 _OUT_FIELDS = ["commit", "token", "entropy", "confidence", "persistence", "drop", "stability", "flags",
@@ -128,6 +153,21 @@ def lib() -> ctypes.CDLL:
         L.rpd_apply_commit.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p,
                                        ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
                                        ctypes.c_void_p, ctypes.c_void_p]
+        v, i32, i64, size = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+        head, ver, dis = ctypes.POINTER(RpdQuantHead), ctypes.POINTER(RpdVerify), ctypes.POINTER(RpdDistill)
+        for name, res, args in (
+                ("rpd_quant_packed_size", size, [head]),
+                ("rpd_quant_pack", ctypes.c_int, [head, v, v, v, v, size, v]),
+                ("rpd_quant_workspace_size", size, [head, i32, i32]),
+                ("rpd_quant_project", ctypes.c_int,
+                 [head, v, i32, v, i64, v, i64, i32, v, v, v, ctypes.c_float, v, size, v]),
+                ("rpd_verify_workspace_size", size, [ver]),
+                ("rpd_verify_draft", ctypes.c_int, [ver, v, size, v]),
+                ("rpd_distill_workspace_size", size, [dis]),
+                ("rpd_distill_loss", ctypes.c_int, [dis, v, size, v]),
+                ("rpd_distill_grad", ctypes.c_int, [dis, v])):
+            f = getattr(L, name)
+            f.restype, f.argtypes = res, args
         L.rpd_status_string.restype = ctypes.c_char_p
         L.rpd_status_string.argtypes = [ctypes.c_int]
         L.rpd_last_error.restype = ctypes.c_char_p
@@ -485,3 +525,282 @@ class Decoder:
             torch.cuda.synchronize()
             out["proj_ms"] = [a.elapsed_time(b) for a, b in ev]
         return out
+
+
+# ------------------------------------------------ operators beside the commit step --
+
+_FLOAT_CODES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32, torch.float16: DTYPE_F16}
+VERIFY_GREEDY = 1
+DISTILL_MAX_K = 256
+DISTILL_STATE = 8
+
+
+def _float_code(name: str, t: torch.Tensor) -> int:
+    if t.dtype not in _FLOAT_CODES:
+        raise TypeError(f"{name} has dtype {t.dtype} (bfloat16, float16 or float32)")
+    return _FLOAT_CODES[t.dtype]
+
+
+def _one_device(first: str, t: torch.Tensor, **others) -> torch.device:
+    """The device that t and every other tensor given are on."""
+    if not t.is_cuda:
+        raise ValueError(f"{first} must be a device tensor")
+    for name, o in others.items():
+        if o is not None and o.device != t.device:
+            raise ValueError(f"{name} is on {o.device}, {first} on {t.device}")
+    return t.device
+
+
+def _rows(name: str, t: torch.Tensor) -> torch.Tensor:
+    """t [..., n] as 2-d rows: the last dimension contiguous, the leading ones of one stride (a view, never a copy)."""
+    if t.dim() < 1 or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+    try:
+        r = t.view(-1, t.shape[-1]) if t.dim() != 2 else t
+    except RuntimeError as e:
+        raise ValueError(f"{name}'s leading dimensions must be rows of one stride (call .contiguous())") from e
+    if r.shape[0] > 1 and r.stride(0) < r.shape[1]:
+        raise ValueError(f"{name}'s rows overlap")
+    return r
+
+
+def _row_stride(r: torch.Tensor) -> int:
+    return r.stride(0) if r.shape[0] > 1 else max(r.shape[1], 1)
+
+
+def _enqueue(device: torch.device, stream, call) -> None:
+    """call(stream handle) with ``device`` current, on ``stream`` or that device's current stream."""
+    if device.index == torch.cuda.current_device():
+        _check(call((torch.cuda.current_stream() if stream is None else stream).cuda_stream or None))
+        return
+    with torch.cuda.device(device):
+        _check(call((torch.cuda.current_stream() if stream is None else stream).cuda_stream or None))
+
+
+class QuantHead:
+    """An output head with 4-bit weights and group scales (``rpd_quant_pack``, ``rpd_quant_project``):
+    W[v][k] = scales[v][k // group] * (code[v][k] - zeros[v][k // group]).
+
+    codes uint8 [V][d/2] (column 2j in the low nibble of byte j, 2j+1 in the high one), scales [V][ceil(d/group)]
+    bfloat16 or float16, optional zeros uint8 of the same shape (values 0..15; 8 everywhere without). Packs them once
+    into ``packed`` on the current stream; the inputs are not kept. Calls on another stream than that one wait for it
+    as for any tensor of the caller's (``stream.wait_stream``)."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor | None = None,
+                 group: int = 128):
+        self.device = _one_device("codes", codes, scales=scales, zeros=zeros)
+        if codes.dim() != 2:
+            raise ValueError("codes must be [V][d/2]")
+        if scales.dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError(f"scales has dtype {scales.dtype} (bfloat16 or float16)")
+        V, d = codes.shape[0], 2 * codes.shape[1]
+        groups = -(-d // group) if group > 0 else 0
+        _check_dev("codes", codes, (V, d // 2), (torch.uint8,))
+        _check_dev("scales", scales, (V, groups), (scales.dtype,))
+        if zeros is not None:
+            _check_dev("zeros", zeros, (V, groups), (torch.uint8,))
+        self.V, self.d, self.group, self.dtype = V, d, int(group), scales.dtype
+        self.head = RpdQuantHead(V, d, self.group, _FLOAT_CODES[scales.dtype], int(zeros is not None))
+        # an invalid head has size 0, and the call below says what is wrong with it
+        self.packed = torch.empty(max(int(lib().rpd_quant_packed_size(ctypes.byref(self.head))), 1),
+                                  dtype=torch.uint8, device=self.device)
+        _enqueue(self.device, None, lambda s: lib().rpd_quant_pack(
+            ctypes.byref(self.head), codes.data_ptr(), scales.data_ptr(), _ptr(zeros), self.packed.data_ptr(),
+            self.packed.numel(), s))
+
+    def _x(self, x: torch.Tensor) -> torch.Tensor:
+        _one_device("x", x, packed=self.packed)
+        if x.dtype != self.dtype:
+            raise TypeError(f"x has dtype {x.dtype}, the head {self.dtype}")
+        if x.shape[-1] != self.d:
+            raise ValueError(f"x has {x.shape[-1]} columns, the head {self.d}")
+        return _rows("x", x)
+
+    def logits(self, x: torch.Tensor, out_dtype: torch.dtype | None = None, out: torch.Tensor | None = None,
+               stream=None) -> torch.Tensor:
+        """x [..., d] through the head: [..., V] of type ``out_dtype`` (x's, or float32), into ``out`` if given."""
+        r = self._x(x)
+        if out is None:
+            out = torch.empty((*x.shape[:-1], self.V), dtype=out_dtype or x.dtype, device=x.device)
+        elif tuple(out.shape) != (*x.shape[:-1], self.V) or (out_dtype and out.dtype != out_dtype):
+            raise ValueError(f"out has shape {tuple(out.shape)} and dtype {out.dtype}")
+        _one_device("out", out, x=x)
+        o = _rows("out", out)
+        code = _float_code("out", out)
+        _enqueue(x.device, stream, lambda s: lib().rpd_quant_project(
+            ctypes.byref(self.head), self.packed.data_ptr(), r.shape[0], r.data_ptr(), _row_stride(r), o.data_ptr(),
+            _row_stride(o), code, None, None, None, 1.0, None, 0, s))
+        return out
+
+    def stats(self, x: torch.Tensor, logit_scale: float = 1.0, stream=None) -> dict:
+        """The softmax statistics of logit_scale * (x through the head), as ``gate_commit`` takes them for
+        x [K][B][L][d]: argmax int32, confidence and entropy float32, of x's leading shape."""
+        r = self._x(x)
+        e = dict(device=x.device)
+        o = {"argmax": torch.empty(x.shape[:-1], dtype=torch.int32, **e),
+             "confidence": torch.empty(x.shape[:-1], dtype=torch.float32, **e),
+             "entropy": torch.empty(x.shape[:-1], dtype=torch.float32, **e)}
+        ws = torch.empty(int(lib().rpd_quant_workspace_size(ctypes.byref(self.head), r.shape[0], 1)),
+                         dtype=torch.uint8, **e)
+        if stream is not None:
+            ws.record_stream(stream)
+        _enqueue(x.device, stream, lambda s: lib().rpd_quant_project(
+            ctypes.byref(self.head), self.packed.data_ptr(), r.shape[0], r.data_ptr(), _row_stride(r), None, 0, 0,
+            o["argmax"].data_ptr(), o["confidence"].data_ptr(), o["entropy"].data_ptr(), float(logit_scale),
+            ws.data_ptr(), ws.numel(), s))
+        return o
+
+
+class VerifyDraft:
+    """A reusable call of ``rpd_verify_draft`` on given tensors: outputs and workspace are allocated once and every
+    ``__call__`` only enqueues the library's kernels (on the tensors' values of that time).
+
+    target_logits [B][T+1][V] (bfloat16, float16 or float32; last dimension contiguous), draft_token int32 [B][T],
+    u float32 [B][T] and r float32 [B] in [0, 1) (neither with ``greedy``), optional draft_logits [B][T][V] of the
+    same type and draft_len int32 [B]. Returns token int32 [B][T+1] (the accepted tokens, the one drawn after them,
+    then -1), n_accept int32 [B] and accept float32 [B][T] (see include/rpd.h). The workspace and the outputs are
+    this object's: calls that overlap need objects of their own."""
+
+    def __init__(self, target_logits: torch.Tensor, draft_token: torch.Tensor, u: torch.Tensor | None = None,
+                 r: torch.Tensor | None = None, draft_logits: torch.Tensor | None = None,
+                 draft_len: torch.Tensor | None = None, target_scale: float = 1.0, draft_scale: float = 1.0,
+                 greedy: bool = False):
+        dev = self.device = _one_device("target_logits", target_logits, draft_token=draft_token, u=u, r=r,
+                                        draft_logits=draft_logits, draft_len=draft_len)
+        code = _float_code("target_logits", target_logits)
+        if target_logits.dim() != 3 or target_logits.shape[1] < 1:
+            raise ValueError("target_logits must be [B][T+1][V]")
+        B, T, V = target_logits.shape[0], target_logits.shape[1] - 1, target_logits.shape[2]
+        _check_dev("draft_token", draft_token, (B, T), (torch.int32,))
+        if not greedy and (u is None or r is None):
+            raise ValueError("u and r are required (without greedy)")
+        if u is not None:
+            _check_dev("u", u, (B, T), (torch.float32,))
+        if r is not None:
+            _check_dev("r", r, (B,), (torch.float32,))
+        if draft_len is not None:
+            _check_dev("draft_len", draft_len, (B,), (torch.int32,))
+        for name, t, shape in (("target_logits", target_logits, (B, T + 1, V)), ("draft_logits", draft_logits, (B, T, V))):
+            if t is None:
+                continue
+            if tuple(t.shape) != shape or t.dtype != target_logits.dtype:
+                raise ValueError(f"{name} has shape {tuple(t.shape)} and dtype {t.dtype}, expected {shape}")
+            if V > 1 and t.stride(2) != 1:
+                raise ValueError(f"{name} must be contiguous in its last dimension")
+        q = draft_logits if T > 0 else None
+        self.out = {"token": torch.empty((B, T + 1), dtype=torch.int32, device=dev),
+                    "n_accept": torch.empty((B,), dtype=torch.int32, device=dev),
+                    "accept": torch.empty((B, T), dtype=torch.float32, device=dev)}
+        self.problem = RpdVerify(B, T, V, code, target_logits.data_ptr(), target_logits.stride(0),
+                                 target_logits.stride(1), _ptr(q), 0 if q is None else q.stride(0),
+                                 0 if q is None else q.stride(1), draft_token.data_ptr(), _ptr(draft_len), _ptr(u),
+                                 _ptr(r), float(target_scale), float(draft_scale), VERIFY_GREEDY if greedy else 0,
+                                 self.out["token"].data_ptr(), self.out["n_accept"].data_ptr(),
+                                 self.out["accept"].data_ptr())
+        nbytes = int(lib().rpd_verify_workspace_size(ctypes.byref(self.problem)))
+        self.workspace = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=dev)
+        self._keep = (target_logits, draft_token, u, r, draft_logits, draft_len)
+
+    def __call__(self, stream=None) -> dict:
+        """Enqueue one call."""
+        _enqueue(self.device, stream, lambda s: lib().rpd_verify_draft(
+            ctypes.byref(self.problem), self.workspace.data_ptr(), self.workspace.numel(), s))
+        return self.out
+
+
+def verify_draft(target_logits: torch.Tensor, draft_token: torch.Tensor, u: torch.Tensor | None = None,
+                 r: torch.Tensor | None = None, draft_logits: torch.Tensor | None = None,
+                 draft_len: torch.Tensor | None = None, target_scale: float = 1.0, draft_scale: float = 1.0,
+                 greedy: bool = False, stream=None) -> dict:
+    """``rpd_verify_draft``: drafted tokens against a target's logits, from given random numbers (see
+    ``VerifyDraft``). Returns token, n_accept and accept, valid once the stream has run."""
+    call = VerifyDraft(target_logits, draft_token, u, r, draft_logits, draft_len, target_scale, draft_scale, greedy)
+    if stream is not None:
+        call.workspace.record_stream(stream)
+    return call(stream)
+
+
+def _distill_problem(logits, teacher_id, teacher_logit, teacher_lse, weight, logit_scale):
+    """The problem of [..., V] logits without its outputs, and the rows of the logits."""
+    _one_device("logits", logits, teacher_id=teacher_id, teacher_logit=teacher_logit, teacher_lse=teacher_lse,
+                weight=weight)
+    code = _float_code("logits", logits)
+    r = _rows("logits", logits)
+    lead, k = tuple(logits.shape[:-1]), teacher_id.shape[-1] if teacher_id.dim() else 0
+    _check_dev("teacher_id", teacher_id, (*lead, k), (torch.int32,))
+    _check_dev("teacher_logit", teacher_logit, (*lead, k), tuple(_FLOAT_CODES))
+    for name, t in (("teacher_lse", teacher_lse), ("weight", weight)):
+        if t is not None:
+            _check_dev(name, t, lead, (torch.float32,))
+    return RpdDistill(r.shape[0], r.shape[1], k, code, _FLOAT_CODES[teacher_logit.dtype], r.data_ptr(),
+                      _row_stride(r), teacher_id.data_ptr(), teacher_logit.data_ptr(), _ptr(teacher_lse),
+                      _ptr(weight), None, float(logit_scale), None, None, None, 0), r
+
+
+def _distill_loss(p: RpdDistill, logits: torch.Tensor, stream) -> tuple[torch.Tensor, torch.Tensor]:
+    loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
+    state = torch.empty((p.N, DISTILL_STATE), dtype=torch.float32, device=logits.device)
+    p.loss, p.state = loss.data_ptr(), state.data_ptr()
+    ws = torch.empty(int(lib().rpd_distill_workspace_size(ctypes.byref(p))), dtype=torch.uint8, device=logits.device)
+    if stream is not None:
+        ws.record_stream(stream)
+        state.record_stream(stream)
+    _enqueue(logits.device, stream,
+             lambda s: lib().rpd_distill_loss(ctypes.byref(p), ws.data_ptr(), ws.numel(), s))
+    return loss, state
+
+
+def _grad_like(logits: torch.Tensor, p: RpdDistill) -> torch.Tensor:
+    grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    p.grad, p.grad_stride = grad.data_ptr(), max(p.V, 1)
+    return grad
+
+
+class _Distill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, teacher_id, teacher_logit, teacher_lse, weight, logit_scale):
+        p, _ = _distill_problem(logits, teacher_id, teacher_logit, teacher_lse, weight, logit_scale)
+        loss, state = _distill_loss(p, logits, None)
+        ctx.save_for_backward(logits, teacher_id, teacher_logit, teacher_lse, weight, state)
+        ctx.logit_scale = logit_scale
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_loss):
+        logits, teacher_id, teacher_logit, teacher_lse, weight, state = ctx.saved_tensors
+        p, _ = _distill_problem(logits, teacher_id, teacher_logit, teacher_lse, weight, ctx.logit_scale)
+        grad = _grad_like(logits, p)
+        up = grad_loss.to(torch.float32).contiguous()   # a broadcast upstream gradient has stride 0
+        p.grad_loss, p.state = up.data_ptr(), state.data_ptr()
+        _enqueue(logits.device, None, lambda s: lib().rpd_distill_grad(ctypes.byref(p), s))
+        return grad, None, None, None, None, None
+
+
+def distill(logits: torch.Tensor, teacher_id: torch.Tensor, teacher_logit: torch.Tensor,
+            teacher_lse: torch.Tensor | None = None, weight: torch.Tensor | None = None,
+            logit_scale: float = 1.0) -> torch.Tensor:
+    """Distillation loss of every row against a teacher's top logits (``rpd_distill_loss``, and
+    ``rpd_distill_grad`` in the backward pass).
+
+    logits [..., V] (bfloat16, float16 or float32), teacher_id int32 [..., k] (entries outside 0..V-1 are no part of
+    the list), teacher_logit [..., k], optional teacher_lse and weight float32 [...]. Returns float32 [...],
+    differentiable once in ``logits`` (the teacher and the weights are constants)."""
+    return _Distill.apply(logits, teacher_id, teacher_logit, teacher_lse, weight, float(logit_scale))
+
+
+def distill_grad(logits: torch.Tensor, teacher_id: torch.Tensor, teacher_logit: torch.Tensor,
+                 teacher_lse: torch.Tensor | None = None, weight: torch.Tensor | None = None,
+                 grad_loss: torch.Tensor | None = None, logit_scale: float = 1.0,
+                 stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+    """Loss and gradient in one call, for a training step that knows the upstream gradient ``grad_loss`` (float32
+    [...], 1 if None) beforehand: (loss [...], gradient [..., V] of ``logits``'s type). Not recorded by autograd."""
+    logits = logits.detach()
+    p, _ = _distill_problem(logits, teacher_id, teacher_logit, teacher_lse, weight, logit_scale)
+    if grad_loss is not None:
+        _one_device("logits", logits, grad_loss=grad_loss)
+        _check_dev("grad_loss", grad_loss, tuple(logits.shape[:-1]), (torch.float32,))
+        p.grad_loss = grad_loss.data_ptr()
+    grad = _grad_like(logits, p)
+    loss, _ = _distill_loss(p, logits, stream)
+    return loss, grad

@@ -1,0 +1,263 @@
+// Distillation from a teacher's top logits: loss and gradient of a row z of
+// the student's logits, q = softmax(scale z).
+//
+//   p_j over the list of the teacher's tokens i_j: softmax of scale t_j over
+//   the list, or with the teacher's log-sum-exp e^(scale t_j - lse), the rest
+//   p_T = 1 - sum p_j being one entry for the tokens outside the list (mass
+//   q_T of the student)
+//   loss = sum_j p_j (ln p_j - ln q_{i_j}) + p_T (ln p_T - ln q_T)
+//   d loss / d z_v = scale [ P q_v - (sum of p_j with i_j = v) ]     in the list
+//                    scale [ (P - p_T / q_T) q_v ]                  outside
+//   with P = sum p_j + p_T
+//
+// Bound: one read of z for the loss, one read and one write for the gradient.
+// The student's mass outside the list is summed by itself (a bit of LDS per
+// vocabulary entry marks the list): what is left of 1 after the list's mass is
+// taken off would be rounding where the student is sure. The teacher's few
+// probabilities and the loss are float64.
+#include <cstdint>
+
+#include "logit_rows.h"
+#include "rpd_ops.h"
+
+namespace rpd {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxList = RPD_DISTILL_MAX_K;
+
+// a row's state between the loss and the gradient
+struct RowState {
+  float ref, in;   // in the list: in * e^(scale z - ref) - p, with in = P / S (S relative to ref)
+  float tail, out; // outside: out * e^(scale z - tail), tail the largest exponent there (a student that is
+                   // sure leaves e^(tail - ref) far below float32's range)
+  float tref;      // the teacher's p_j = tinv * e^(scale t_j - tref)
+  float tinv;
+  float any;       // 0: no gradient
+};
+static_assert(sizeof(RowState) <= RPD_DISTILL_STATE * sizeof(float), "the state that callers allocate");
+
+__device__ __forceinline__ float teacher_at(const DistillCall& a, long long i) {
+  if (a.teacher_dtype == RPD_DTYPE_F32) return static_cast<const float*>(a.teacher)[i];
+  return a.teacher_dtype == RPD_DTYPE_BF16 ? Bf16::one(static_cast<const uint16_t*>(a.teacher) + i)
+                                           : F16::one(static_cast<const uint16_t*>(a.teacher) + i);
+}
+
+__device__ __forceinline__ bool skipped(const DistillCall& a, int n) { return a.weight && a.weight[n] == 0.f; }
+
+// maximum and mass of the entries of a part of a row outside the list
+template <class E>
+__global__ __launch_bounds__(kThreads) void k_distill_part(DistillCall a) {
+  const int n = blockIdx.x / a.splits, split = blockIdx.x - n * a.splits;
+  if (skipped(a, n)) return;
+  extern __shared__ uint32_t s_mark[];   // a bit per entry of the part
+  __shared__ float2 s_part[kThreads / 64];
+  const int lo = split * a.chunk, hi = min(a.V, lo + a.chunk);
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  for (int i = threadIdx.x; i < (a.chunk + 31) / 32; i += kThreads) s_mark[i] = 0;
+  __syncthreads();
+  for (int j = threadIdx.x; j < a.k; j += kThreads) {
+    const int v = a.ids[(long long)n * a.k + j];
+    if (v >= lo && v < hi) atomicOr(&s_mark[(v - lo) >> 5], 1u << ((v - lo) & 31));
+  }
+  __syncthreads();
+  const typename E::t* p = static_cast<const typename E::t*>(a.logits) + n * a.stride;
+  MaxSum s{-INFINITY, 0.f};
+  for (int i = lo + 8 * threadIdx.x; i < hi; i += 8 * kThreads) {
+    float z[8];
+    if (i + 8 <= hi) {
+      Eight<E> v;
+      v.load(p + i);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = v.at(e);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = i + e < hi ? E::one(p + i + e) : -INFINITY;
+    }
+    const uint32_t mark = s_mark[(i - lo) >> 5] >> ((i - lo) & 31) & 255u;
+    if (mark) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = mark >> e & 1u ? -INFINITY : z[e];
+    }
+    maxsum_push(s, z, a.scale);
+  }
+  s = wave_maxsum(s, a.scale);
+  if (lane == 0) s_part[wid] = make_float2(s.m, s.S);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kThreads / 64; ++w) s = maxsum_merge(s, MaxSum{s_part[w].x, s_part[w].y}, a.scale);
+    a.partials[(long long)n * a.splits + split] = make_float2(s.m, s.S);
+  }
+}
+
+template <int N>
+__device__ __forceinline__ void wave_sum(double (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int k = 32; k >= 1; k >>= 1) v[i] += __shfl_xor(v[i], k);
+}
+
+// The row's loss and state from the maximum and mass of its entries outside the list; one wave.
+template <class E>
+__device__ __forceinline__ void row_loss(const DistillCall& a, int n, MaxSum s, int lane) {
+  constexpr int kEach = kMaxList / 64;
+  const typename E::t* p = static_cast<const typename E::t*>(a.logits) + n * a.stride;
+  const int32_t* ids = a.ids + (long long)n * a.k;
+  double t[kEach], z[kEach];
+  bool ok[kEach], first[kEach];
+  double tmax = -INFINITY, sums[2] = {0.0, 0.0};   // teacher's, student's mass in the list
+  float top = s.m;
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    const int j = lane + 64 * u;
+    const int v = j < a.k ? ids[j] : -1;
+    ok[u] = v >= 0 && v < a.V;
+    t[u] = ok[u] ? (double)teacher_at(a, (long long)n * a.k + j) * (double)a.scale : -INFINITY;
+    const float zj = ok[u] ? E::one(p + v) : -INFINITY;
+    z[u] = (double)zj * (double)a.scale;
+    tmax = fmax(tmax, t[u]);
+    top = fmaxf(top, zj);
+    first[u] = ok[u];   // a token listed twice is in the list once
+    for (int i = 0; i < j && first[u]; ++i) first[u] = ids[i] != v;
+  }
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
+  const float ref = ref_of(top, a.scale), tail = ref_of(s.m, a.scale);
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    z[u] -= (double)ref;
+    if (first[u]) sums[1] += exp(z[u]);
+  }
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) tmax = fmax(tmax, __shfl_xor(tmax, k));
+  const float tref = a.lse ? a.lse[n] : (float)(tmax == -INFINITY ? 0.0 : tmax);
+#pragma unroll
+  for (int u = 0; u < kEach; ++u)
+    if (ok[u]) sums[0] += exp(t[u] - (double)tref);
+  wave_sum(sums);
+  // a list without any mass: in list mode there is no teacher, and no loss
+  const bool none = !a.lse && sums[0] == 0.0;
+  const double tinv = a.lse ? 1.0 : none ? 0.0 : 1.0 / sums[0];
+  const double rest = a.lse ? fmax(0.0, 1.0 - sums[0]) : 0.0;   // NaN in the list shows in its own terms
+  const double drop = s.S == 0.f ? 0.0 : (double)tail - (double)ref;   // S_T's exponent in units of S's
+  const double S = (double)s.S * exp(drop) + sums[1], ln_S = log(S);
+  double l[1] = {0.0};
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    const double pj = ok[u] ? exp(t[u] - (double)tref) * tinv : 0.0;
+    if (pj != 0.0) l[0] += pj * ((t[u] - (double)tref + (a.lse ? 0.0 : log(tinv))) - (z[u] - ln_S));
+  }
+  wave_sum(l);
+  if (lane != 0) return;
+  if (rest > 0.0) l[0] += rest * (log(rest) - (log((double)s.S) + drop - ln_S));
+  const double P = (none ? 0.0 : sums[0] * tinv) + rest;
+  a.loss[n] = none ? 0.f : (float)((a.weight ? (double)a.weight[n] : 1.0) * l[0]);
+  RowState st;
+  st.ref = ref;
+  st.in = (float)(P / S);
+  st.tail = tail;
+  st.out = (float)(P * exp(drop) / S - (rest > 0.0 ? rest / (double)s.S : 0.0));
+  st.tref = tref;
+  st.tinv = (float)tinv;
+  st.any = none ? 0.f : 1.f;
+  *reinterpret_cast<RowState*>(a.state + (long long)n * RPD_DISTILL_STATE) = st;
+}
+
+template <class E>
+__global__ __launch_bounds__(64) void k_distill_loss(DistillCall a) {
+  const int n = blockIdx.x, lane = threadIdx.x;
+  if (skipped(a, n)) {
+    if (lane == 0) {
+      a.loss[n] = 0.f;
+      *reinterpret_cast<RowState*>(a.state + (long long)n * RPD_DISTILL_STATE) = RowState{};
+    }
+    return;
+  }
+  MaxSum s{-INFINITY, 0.f};
+  for (int i = lane; i < a.splits; i += 64) {
+    const float2 v = a.partials[(long long)n * a.splits + i];
+    s = maxsum_merge(s, MaxSum{v.x, v.y}, a.scale);
+  }
+  row_loss<E>(a, n, wave_maxsum(s, a.scale), lane);
+}
+
+// The part [lo, hi) of a row's gradient: the formula of the entries outside the
+// list everywhere, then those in the list over it.
+template <class E>
+__global__ __launch_bounds__(kThreads) void k_distill_grad(DistillCall a) {
+  typedef typename E::t T;
+  const int n = blockIdx.x / a.splits, split = blockIdx.x - n * a.splits;
+  const int lo = split * a.chunk, hi = min(a.V, lo + a.chunk);
+  const T* p = static_cast<const T*>(a.logits) + n * a.stride;
+  T* g = static_cast<T*>(a.grad) + n * a.grad_stride;
+  const RowState st = *reinterpret_cast<const RowState*>(a.state + (long long)n * RPD_DISTILL_STATE);
+  const float c = (a.weight ? a.weight[n] : 1.f) * (a.up ? a.up[n] : 1.f) * a.scale;
+  const bool zero = skipped(a, n) || st.any == 0.f;   // such a row is not read
+  const float co = c * st.out;
+  for (int i = lo + 8 * threadIdx.x; i < hi; i += 8 * kThreads) {
+    if (i + 8 <= hi) {
+      float d[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      Eight<E> v;
+      if (!zero) {
+        v.load(p + i);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] = co * __expf(fmaf(v.at(e), a.scale, -st.tail));
+      }
+      v.set(d);
+      v.store(g + i);
+    } else {
+      for (int v = i; v < hi; ++v) g[v] = E::to(zero ? 0.f : co * __expf(fmaf(E::one(p + v), a.scale, -st.tail)));
+    }
+  }
+  if (zero) return;
+  __syncthreads();
+  const int32_t* ids = a.ids + (long long)n * a.k;
+  for (int j = threadIdx.x; j < a.k; j += kThreads) {
+    const int v = ids[j];
+    if (v < lo || v >= hi) continue;
+    double pv = 0.0;
+    bool first = true;
+    for (int i = 0; i < a.k; ++i)
+      if (ids[i] == v) {
+        first &= i >= j;
+        pv += exp((double)teacher_at(a, (long long)n * a.k + i) * (double)a.scale - (double)st.tref);
+      }
+    if (first) g[v] = E::to(c * (st.in * __expf(fmaf(E::one(p + v), a.scale, -st.ref)) - (float)(pv * (double)st.tinv)));
+  }
+}
+
+template <class E>
+hipError_t loss_t(const DistillCall& a, hipStream_t s) {
+  k_distill_part<E><<<(unsigned)((long long)a.N * a.splits), kThreads, (size_t)(a.chunk + 31) / 32 * 4, s>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  k_distill_loss<E><<<a.N, 64, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <class E>
+hipError_t grad_t(const DistillCall& a, hipStream_t s) {
+  k_distill_grad<E><<<(unsigned)((long long)a.N * a.splits), kThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_distill_loss(const DistillCall& a, hipStream_t s) {
+  switch (a.dtype) {
+    case RPD_DTYPE_BF16: return loss_t<Bf16>(a, s);
+    case RPD_DTYPE_F16: return loss_t<F16>(a, s);
+    default: return loss_t<F32>(a, s);
+  }
+}
+
+hipError_t launch_distill_grad(const DistillCall& a, hipStream_t s) {
+  switch (a.dtype) {
+    case RPD_DTYPE_BF16: return grad_t<Bf16>(a, s);
+    case RPD_DTYPE_F16: return grad_t<F16>(a, s);
+    default: return grad_t<F32>(a, s);
+  }
+}
+
+}  // namespace rpd

@@ -1,0 +1,120 @@
+// Device pieces shared by the kernels that read rows of logits from memory:
+// eight elements of a row at a time, whatever its alignment, and running
+// softmax sums.
+#pragma once
+
+#include <cmath>
+#include <cstdint>
+
+#include "rpd_device.h"
+
+namespace rpd {
+namespace {
+
+// Rows of an odd length start at any element; wide global loads and stores
+// need no alignment beyond the element's here.
+struct __attribute__((packed, aligned(2))) Any16 {
+  u32x4 v;
+};
+struct __attribute__((packed, aligned(4))) Any32 {
+  u32x4 a, b;
+};
+
+struct Bf16 {
+  typedef uint16_t t;
+  static constexpr int bytes = 2;
+  static __device__ __forceinline__ float one(const t* p) { return __uint_as_float((uint32_t)*p << 16); }
+  static __device__ __forceinline__ t to(float x) { return __builtin_bit_cast(t, (__bf16)x); }
+};
+struct F16 {
+  typedef uint16_t t;
+  static constexpr int bytes = 2;
+  static __device__ __forceinline__ float one(const t* p) { return (float)__builtin_bit_cast(_Float16, *p); }
+  static __device__ __forceinline__ t to(float x) { return __builtin_bit_cast(t, (_Float16)x); }
+};
+struct F32 {
+  typedef float t;
+  static constexpr int bytes = 4;
+  static __device__ __forceinline__ float one(const t* p) { return *p; }
+  static __device__ __forceinline__ t to(float x) { return x; }
+};
+
+// eight elements as they lie in memory
+template <class E>
+struct Eight {
+  u32x4 v;
+  __device__ __forceinline__ void load(const typename E::t* p) { v = reinterpret_cast<const Any16*>(p)->v; }
+  __device__ __forceinline__ void store(typename E::t* p) const { reinterpret_cast<Any16*>(p)->v = v; }
+  __device__ __forceinline__ float at(int e) const;
+  __device__ __forceinline__ void set(const float (&z)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (uint32_t)E::to(z[2 * e]) | (uint32_t)E::to(z[2 * e + 1]) << 16;
+  }
+};
+template <>
+__device__ __forceinline__ float Eight<Bf16>::at(int e) const {
+  const uint32_t w = v[e >> 1];
+  return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+}
+template <>
+__device__ __forceinline__ float Eight<F16>::at(int e) const {
+  const uint32_t w = v[e >> 1];
+  return (float)__builtin_bit_cast(_Float16, (uint16_t)(e & 1 ? w >> 16 : w));
+}
+template <>
+struct Eight<F32> {
+  u32x4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = reinterpret_cast<const Any32*>(p)->a;
+    b = reinterpret_cast<const Any32*>(p)->b;
+  }
+  __device__ __forceinline__ void store(float* p) const {
+    reinterpret_cast<Any32*>(p)->a = a;
+    reinterpret_cast<Any32*>(p)->b = b;
+  }
+  __device__ __forceinline__ float at(int e) const { return __uint_as_float(e < 4 ? a[e & 3] : b[e & 3]); }
+  __device__ __forceinline__ void set(const float (&z)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      a[e] = __float_as_uint(z[e]);
+      b[e] = __float_as_uint(z[4 + e]);
+    }
+  }
+};
+
+// Maximum m of the raw logits and S = sum e^(scale z - r) with r the rounded
+// product scale m: one fused rounding an exponent, so that any scale is as
+// exact as 1. Nothing seen: m = -inf, S = 0; a row that is -inf throughout
+// keeps S = 0; NaN and +inf leave S NaN.
+struct MaxSum {
+  float m, S;
+};
+__device__ __forceinline__ float ref_of(float m, float scale) { return m == -INFINITY ? 0.f : m * scale; }
+// what a sum relative to m is worth relative to r (0 while nothing was seen, whatever r: rows far below 0)
+__device__ __forceinline__ float carry(float m, float r, float scale) {
+  return m == -INFINITY ? 0.f : __expf(ref_of(m, scale) - r);
+}
+__device__ __forceinline__ MaxSum maxsum_merge(MaxSum a, MaxSum b, float scale) {
+  const float m = fmaxf(a.m, b.m), r = ref_of(m, scale);
+  return MaxSum{m, a.S * carry(a.m, r, scale) + b.S * carry(b.m, r, scale)};
+}
+template <int N>
+__device__ __forceinline__ void maxsum_push(MaxSum& s, const float (&z)[N], float scale) {
+  float m = s.m;
+#pragma unroll
+  for (int e = 0; e < N; ++e) m = fmaxf(m, z[e]);
+  const float r = ref_of(m, scale);
+  float S = s.S * carry(s.m, r, scale);
+#pragma unroll
+  for (int e = 0; e < N; ++e) S += __expf(fmaf(z[e], scale, -r));
+  s.m = m;
+  s.S = S;
+}
+__device__ __forceinline__ MaxSum wave_maxsum(MaxSum s, float scale) {
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) s = maxsum_merge(s, MaxSum{__shfl_xor(s.m, k), __shfl_xor(s.S, k)}, scale);
+  return s;
+}
+
+}  // namespace
+}  // namespace rpd

@@ -12,10 +12,11 @@
 
 #include "rpd.h"
 #include "rpd_launch.h"
+#include "rpd_ops.h"
 
-namespace {
+static thread_local char g_err[512] = "";
 
-thread_local char g_err[512] = "";
+namespace rpd {
 
 rpd_status fail(rpd_status s, const char* fmt, ...) {
   va_list ap;
@@ -24,6 +25,14 @@ rpd_status fail(rpd_status s, const char* fmt, ...) {
   va_end(ap);
   return s;
 }
+
+void clear_error() { g_err[0] = '\0'; }
+
+}  // namespace rpd
+
+using rpd::fail;
+
+namespace {
 
 constexpr size_t kHeaderBytes = 256;   // n_masked (0), device status (4), the lazy pass's counts (12..47)
 constexpr long long kMaxBL = 1LL << 24;

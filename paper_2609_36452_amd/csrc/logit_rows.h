@@ -89,7 +89,12 @@ struct Eight<F32> {
 struct MaxSum {
   float m, S;
 };
-__device__ __forceinline__ float ref_of(float m, float scale) { return m == -INFINITY ? 0.f : m * scale; }
+__device__ __forceinline__ float ref_of(float m, float scale) {
+  // not to be fused with a subtraction that follows: two sums over the same m would differ by the product's
+  // rounding, some 1e-6 at every merge
+#pragma clang fp contract(off)
+  return m == -INFINITY ? 0.f : m * scale;
+}
 // what a sum relative to m is worth relative to r (0 while nothing was seen, whatever r: rows far below 0)
 __device__ __forceinline__ float carry(float m, float r, float scale) {
   return m == -INFINITY ? 0.f : __expf(ref_of(m, scale) - r);

@@ -180,6 +180,20 @@ def test_verify_greedy(B, T, V, dtype, draft, ragged, scale):
     _check_verify(o, R.verify(target, token, None, None, lens=lens, greedy=True), V)
 
 
+def test_verify_scales_that_round():
+    """Scaled maxima that are no float32 numbers, over rows of many merges: as exact as scale 1."""
+    for scale in (0.7, 1.3):
+        c = _verify_case(6, 4, 60001, F32, True, False, 41, scale)
+        d = [None if t is None else t.to(DEV) for t in c]
+        o = rpd.verify_draft(*d[:4], draft_logits=d[4], target_scale=scale, draft_scale=scale)
+        ref = R.verify(*c[:4], draft=c[4], target_scale=scale, draft_scale=scale)
+        _check_verify(o, ref, 60001)
+        err = (o["accept"].cpu().double() - ref[2]).abs() / ref[2].clamp_min(1e-30)
+        # a float32 sum whose terms and chains (12 additions a thread, 8 merges, 30 parts) each round: their errors
+        # have either sign, so twice the root of their number, and the exponentials' of arguments down to -16
+        assert float(err.max()) <= 2 * (2 * math.sqrt(50) + 16) * 2.0 ** -24
+
+
 def test_verify_masked_and_broken_rows():
     V = 3001
     g = torch.Generator().manual_seed(2)

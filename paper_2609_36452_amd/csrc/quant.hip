@@ -30,6 +30,7 @@ namespace rpd {
 namespace {
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
 
 constexpr int kTileV = 16;     // vocabulary rows of a tile
@@ -86,19 +87,6 @@ __global__ __launch_bounds__(256) void k_quant_pack_scales(QuantDims q, const ui
 
 // ---------------------------------------------------------------- project --
 
-__device__ __forceinline__ f16x2 as_h2(uint32_t u) { return __builtin_bit_cast(f16x2, u); }
-
-// 8 codes -> q - z in fp16; zl = -(1024 + z), zh = -(64 + z) in both halves
-__device__ __forceinline__ f16x8 decode(uint32_t w, f16x2 zl, f16x2 zh) {
-  const f16x2 sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
-  const uint32_t w8 = w >> 8;
-  const f16x2 a = as_h2((w & 0x000f000fu) | 0x64006400u) + zl;
-  const f16x2 b = __builtin_elementwise_fma(as_h2((w & 0x00f000f0u) | 0x64006400u), sixteenth, zh);
-  const f16x2 c = as_h2((w8 & 0x000f000fu) | 0x64006400u) + zl;
-  const f16x2 e = __builtin_elementwise_fma(as_h2((w8 & 0x00f000f0u) | 0x64006400u), sixteenth, zh);
-  return f16x8{a.x, a.y, b.x, b.y, c.x, c.y, e.x, e.y};
-}
-
 template <int N>
 struct Raw;
 template <>
@@ -110,43 +98,114 @@ struct Raw<4> { typedef uint32_t t; };
 template <>
 struct Raw<8> { typedef uint64_t t; };
 
-__device__ __forceinline__ float from_bits16(uint32_t b, bool bf16) {
-  return bf16 ? __uint_as_float(b << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)b);
+constexpr int kRsrcFlags = 0x00020000;
+constexpr int kNonTemporal = 2;   // a load's policy bits
+
+// N bytes at a lane's offset from a uniform base; 0 beyond the range
+template <int N>
+__device__ __forceinline__ typename Raw<N>::t load_bits(char* base, int range, uint32_t offset) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(base, (short)0, range, kRsrcFlags);
+  if constexpr (N == 1)
+    return __builtin_amdgcn_raw_buffer_load_b8(r, offset, 0, 0);
+  else if constexpr (N == 2)
+    return __builtin_amdgcn_raw_buffer_load_b16(r, offset, 0, 0);
+  else if constexpr (N == 4)
+    return __builtin_amdgcn_raw_buffer_load_b32(r, offset, 0, 0);
+  else
+    return __builtin_bit_cast(uint64_t, __builtin_amdgcn_raw_buffer_load_b64(r, offset, 0, 0));
 }
 
-// one logit into a running softmax state (an entry that is NaN leaves S and T NaN)
+// 8 codes as fp16 operands without a conversion: the bits of a nibble in the
+// low bits of a half are the subnormal q 2^-24, four bits up q 2^-20 (the x
+// that meet those are scaled down by 16), which the matrix cores take exactly
+__device__ __forceinline__ f16x8 decode(uint32_t w) {
+  const uint32_t w8 = w >> 8;
+  const u32x4 o = {w & 0x000f000fu, w & 0x00f000f0u, w8 & 0x000f000fu, w8 & 0x00f000f0u};
+  return __builtin_bit_cast(f16x8, o);
+}
+
+template <bool BF16>
+__device__ __forceinline__ float from_bits16(uint32_t b) {
+  return BF16 ? __uint_as_float(b << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)b);
+}
+
+// One logit into a running softmax state, with one exponential: of the
+// distance to the larger of z and m. NaN never becomes m and leaves S and T NaN.
 __device__ __forceinline__ void soft_push(Soft& s, float z, int v) {
   const bool up = z > s.m;
-  const float M = up ? z : s.m;
-  const float dm = s.S == 0.f ? 0.f : s.m - M, dz = z - M;
-  const float em = __expf(dm), ez = __expf(dz);
-  s.T = (s.T + dm * s.S) * em + ez * dz;
-  s.S = s.S * em + ez;
+  const float d = up ? s.m - z : z - s.m;       // <= 0, or NaN
+  const float e = __expf(d);
+  const float S0 = up ? s.S : 1.f, T0 = up ? s.T : 0.f;   // what is carried over to the new maximum
+  const float dt = S0 == 0.f ? 0.f : d;         // nothing seen yet: d is -inf
+  const float Sc = S0 * e, Tc = fmaf(dt, S0, T0) * e;
+  s.S = Sc + (up ? 1.f : s.S);
+  s.T = Tc + (up ? 0.f : s.T);
   s.idx = up ? v : s.idx;
-  s.m = M;
+  s.m = up ? z : s.m;
 }
 
-// NC chunks a wave, MT tiles of 16 rows, GPC groups a chunk, ZP: zero points
-template <int NC, int MT, int GPC, bool ZP>
+// NC chunks a wave, MT tiles of 16 rows, GPC groups a chunk, ZP: zero points,
+// LONG: rows longer than the waves hold, x loaded anew in every round, BF16: of that type, else fp16
+template <int NC, int MT, int GPC, bool ZP, bool LONG, bool BF16>
 __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, QuantCall a) {
-  constexpr int D = 2;   // tiles of codes in flight
+  constexpr int NB = quant_batch(NC, MT);       // tiles between two barriers; as many are in flight
+  constexpr int NG = NC * GPC, NX = (NG + 3) / 4;   // groups of a wave; of them four to a correction
   typedef typename Raw<2 * GPC>::t sraw_t;
   typedef typename Raw<GPC>::t zraw_t;
   extern __shared__ __align__(16) float lds[];
-  const int W = a.waves, tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+  const int W = a.waves, tid = threadIdx.x, lane = tid & 63;
+  const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int nthreads = W * 64;
-  // [2][W][NB][MT][64 lanes][4] partial sums, [MT*256] states, [W][MT*16] maxima, [MT*16] exponents
-  const int red_wave = a.nb * MT * 256, red_buf = W * red_wave;
+  // [2][W][NB][MT][64 lanes][4] partial sums, [NB][MT*256] states, [W][MT*16] maxima, [MT*16] exponents
+  constexpr int kRedWave = NB * MT * 256;
+  const int red_buf = W * kRedWave;
   float* red = lds;
   float4* states = reinterpret_cast<float4*>(lds + 2 * red_buf);
-  float* s_max = lds + 2 * red_buf + 4 * MT * 256;
+  uint32_t* s_max = reinterpret_cast<uint32_t*>(lds + 2 * red_buf + 4 * NB * MT * 256);
   int* s_exp = reinterpret_cast<int*>(s_max + kMaxWaves * MT * 16);
   // workgroup -> (row group, slot): the row groups of one slot run on one XCD, where they share the codes in its L2
   const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
   const int rg = local % a.row_groups, slot = local / a.row_groups * 8 + xcd;
   const int m0 = rg * MT * 16, M = min(a.M - m0, MT * 16);
   const int col = lane & 15, quad = lane >> 4;
-  const bool bf16 = a.bf16;
+  const int n_tiles = q.vt > slot ? (q.vt - slot + a.slots - 1) / a.slots : 0;
+  const int per_round = W * NC;
+
+  // step = (tile of this slot, round over the columns); tiles slot, slot + slots, ...
+  u32x4 wb[NB][NC];
+  sraw_t sb[NB][NC];
+  zraw_t zb[NB][NC];
+  const uint32_t w_lane = lane * 16, z_lane = (uint32_t)(col * q.nc * GPC);
+  const int s_range = ((kTileV - 1) * q.nc + 1) * 2 * GPC;   // bytes from a chunk's first scale to its last
+  // The step to be fetched next. Fetches are never skipped (the last tile is fetched again instead): with one that
+  // may be, the compiler cannot count the loads in flight and waits for all of them.
+  const int last_tile = n_tiles > 0 ? slot + (n_tiles - 1) * a.slots : 0;
+  int f_tile = min(slot, last_tile), f_round = 0;
+  auto fetch = [&](int c, u32x4& w, sraw_t& s, zraw_t& z) {
+    // chunks beyond the columns: the last one, whose scales are then not used
+    const int chunk = min((LONG ? f_round * per_round : 0) + wid * NC + c, q.nc - 1);
+    // buffer loads: a resource at the chunk and a lane's fixed offset, no 64-bit address a lane
+    char* w_base = const_cast<char*>(reinterpret_cast<const char*>(a.codes)) + ((long long)f_tile * q.nc + chunk) * 1024;
+    const long long entry = ((long long)f_tile * kTileV * q.nc + chunk) * GPC;
+    char* s_base = const_cast<char*>(reinterpret_cast<const char*>(a.scales)) + entry * 2;
+    char* z_base = const_cast<char*>(reinterpret_cast<const char*>(a.zeros)) + entry;
+    const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(w_base, (short)0, 1024, kRsrcFlags);
+    w = __builtin_amdgcn_raw_buffer_load_b128(wr, w_lane, 0, kNonTemporal);
+    s = load_bits<2 * GPC>(s_base, s_range, 2 * z_lane);
+    if (ZP) z = load_bits<GPC>(z_base, s_range / 2, z_lane);
+  };
+  auto fetched = [&]() {
+    if (!LONG || ++f_round == a.rounds) {
+      f_round = 0;
+      f_tile = min(f_tile + a.slots, last_tile);
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < NB; ++u) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) fetch(c, wb[u][c], sb[u][c], zb[u][c]);
+    fetched();
+  }
 
   auto x_piece = [&](int mt, int chunk, int u) {   // 8 elements of row 16 mt + col, 0 beyond the rows and columns
     const int m = 16 * mt + col, k = kChunk * chunk + 32 * u + 8 * quad;
@@ -162,184 +221,207 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, Q
     }
     return r;
   };
-  const int per_round = W * NC;
-  if (bf16) {
-    // the exponent that brings each row's largest finite element to 2^14..2^15
-    uint32_t big[MT];
+  u32x4 xf[MT][NC][4];   // as loaded, then the fp16 operands
+  auto load_x = [&](int round) {
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) big[mt] = 0;
-    for (int c = wid; c < q.nc; c += W)
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) xf[mt][c][u] = x_piece(mt, round * per_round + wid * NC + c, u);
+  };
+  // each row's largest magnitude (the bits of either type's magnitudes are in order; infinity and NaN count as the
+  // largest finite one, the row's logits being infinite or NaN anyway)
+  {
+    const u16x2 finite = {(uint16_t)(BF16 ? 0x7f7f : 0x7bff), (uint16_t)(BF16 ? 0x7f7f : 0x7bff)};
+    u16x2 big[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) big[mt] = u16x2{0, 0};
+    for (int round = 0; round < (LONG ? a.rounds : 1); ++round) {
+      load_x(round);
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const u32x4 r = x_piece(mt, c, u);
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t lo = r[e] & 0x7fffu, hi = r[e] >> 16 & 0x7fffu;
-            big[mt] = max(big[mt], max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
-          }
-        }
+          for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              big[mt] = __builtin_elementwise_max(big[mt], __builtin_bit_cast(u16x2, xf[mt][c][u][e] & 0x7fff7fffu));
+    }
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      big[mt] = max(big[mt], (uint32_t)__shfl_xor((int)big[mt], 16));
-      big[mt] = max(big[mt], (uint32_t)__shfl_xor((int)big[mt], 32));
-      if (quad == 0) s_max[wid * MT * 16 + mt * 16 + col] = __uint_as_float(big[mt] << 16);
+      big[mt] = __builtin_elementwise_min(big[mt], finite);
+      uint32_t m = max((uint32_t)big[mt].x, (uint32_t)big[mt].y);
+      m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+      m = max(m, (uint32_t)__shfl_xor((int)m, 32));
+      if (quad == 0) s_max[wid * MT * 16 + mt * 16 + col] = m;
     }
     __syncthreads();
     if (tid < MT * 16) {
-      float b = 0.f;
-      for (int w = 0; w < W; ++w) b = fmaxf(b, s_max[w * MT * 16 + tid]);
-      int e = 0;
-      if (b > 0.f) (void)frexpf(b, &e);   // b in [2^(e-1), 2^e)
-      s_exp[tid] = b > 0.f ? e - 15 : 0;
+      uint32_t b = 0;
+      for (int w = 0; w < W; ++w) b = max(b, s_max[w * MT * 16 + tid]);
+      int e = 15;
+      if (b) (void)frexpf(from_bits16<BF16>(b), &e);   // in [2^(e-1), 2^e): to be brought to 2^14..2^15
+      s_exp[tid] = e - 15;
     }
-  } else if (tid < MT * 16) {
-    s_exp[tid] = 0;
   }
-  for (int e = tid; e < MT * 256; e += nthreads) states[e] = soft_pack(soft_empty());
+  if (a.stats)
+    for (int e = tid; e < NB * MT * 256; e += nthreads) states[e] = soft_pack(soft_empty());
   __syncthreads();
 
-  f16x8 xf[MT][NC][4];
-  auto load_x = [&](int round) {
+  float xg[MT][NX];   // row col's sum over group 4 i + quad of this wave, in units of the products
+  auto convert_x = [&]() {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const int ex = s_exp[mt * 16 + col];
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const int chunk = round * per_round + wid * NC + c;
+      for (int i = 0; i < NX; ++i) xg[mt][i] = 0.f;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const u32x4 r = x_piece(mt, chunk, u);
-          if (bf16) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              xf[mt][c][u][2 * e] = (_Float16)ldexpf(__uint_as_float(r[e] << 16), -ex);
-              xf[mt][c][u][2 * e + 1] = (_Float16)ldexpf(__uint_as_float(r[e] & 0xffff0000u), -ex);
-            }
-          } else {
-            xf[mt][c][u] = __builtin_bit_cast(f16x8, r);
-          }
-        }
-      }
-    }
-  };
-  if (a.rounds == 1) load_x(0);
-
-  // step = (tile of this slot, round over the columns); tiles slot, slot + slots, ...
-  const int n_tiles = q.vt > slot ? (q.vt - slot + a.slots - 1) / a.slots : 0;
-  const int steps = n_tiles * a.rounds;
-  u32x4 wb[D][NC];
-  sraw_t sb[D][NC];
-  zraw_t zb[D][NC];
-  auto fetch = [&](int step, u32x4(&w)[NC], sraw_t(&s)[NC], zraw_t(&z)[NC]) {
-    const int ti = step / a.rounds, round = step - ti * a.rounds;
-    const long long tile = slot + (long long)ti * a.slots;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int chunk = round * per_round + wid * NC + c;
-      const bool in = chunk < q.nc;
-      const int cc = in ? chunk : 0;   // a wave beyond the columns reads chunk 0 and multiplies it by x = 0
-      w[c] = a.codes[(tile * q.nc + cc) * 64 + lane];
-      s[c] = reinterpret_cast<const sraw_t*>(a.scales)[(tile * kTileV + col) * q.nc + cc];
-      if (ZP) z[c] = reinterpret_cast<const zraw_t*>(a.zeros)[(tile * kTileV + col) * q.nc + cc];
-    }
-  };
-#pragma unroll
-  for (int u = 0; u < D; ++u)
-    if (u < steps) fetch(u, wb[u], sb[u], zb[u]);
-
-  int nb = 0, buf = 0, first_tile = 0;
-  f32x4 acc[MT];
-  // the sums of the last nb tiles over the waves, out to memory or into the states
-  auto finish = [&](int count) {
-    lds_barrier();
-    const float* src = red + buf * red_buf;
-    for (int e = tid; e < MT * 256; e += nthreads) {
-      // v fastest: 16 columns, then the 4 rows of a quad (64 consecutive words a wave), then quad and tile of rows
-      const int c16 = e & 15, i = e >> 4 & 3, qd = e >> 6 & 3, mt = e >> 8;
-      const int m = 16 * mt + 4 * qd + i;
-      if (m >= M) continue;
-      const int word = mt * 256 + (qd * 16 + c16) * 4 + i, ex = s_exp[m];
-      Soft st;
-      if (a.stats) st = soft_unpack(states[e]);
-      for (int b = 0; b < count; ++b) {
-        float z = 0.f;
-        for (int w = 0; w < W; ++w) z += src[w * red_wave + b * MT * 256 + word];
-        z = ldexpf(z, ex);
-        const long long v = (slot + (long long)(first_tile + b) * a.slots) * kTileV + c16;
-        if (v >= q.V) continue;
-        if (a.stats) {
-          soft_push(st, z * a.logit_scale, (int)v);
-        } else {
-          const long long at = (m0 + m) * a.out_stride + v;
-          if (a.out_type == 1)
-            static_cast<float*>(a.out)[at] = z;
-          else if (a.out_type == 0)
-            static_cast<__bf16*>(a.out)[at] = (__bf16)z;
-          else
-            static_cast<_Float16*>(a.out)[at] = (_Float16)z;
-        }
-      }
-      if (a.stats) states[e] = soft_pack(st);
-    }
-    buf ^= 1;
-    nb = 0;
-  };
-
-  for (int s0 = 0; s0 < steps; s0 += D) {
-#pragma unroll
-    for (int u = 0; u < D; ++u) {
-      const int step = s0 + u;
-      if (step >= steps) break;
-      const int ti = step / a.rounds, round = step - ti * a.rounds;
-      if (a.rounds > 1) load_x(round);
-      if (round == 0) {
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
-      }
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
+      for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int g = 0; g < GPC; ++g) {
-          _Float16 zf = (_Float16)8.f;
-          if (ZP) zf = (_Float16)(float)(uint32_t)(zb[u][c] >> (8 * g) & 255);
-          const _Float16 zl1 = (_Float16)-1024.f - zf, zh1 = (_Float16)-64.f - zf;
-          const f16x2 zl = {zl1, zl1}, zh = {zh1, zh1};
-          f32x4 part[MT];
+          float sum = 0.f;
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) part[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int u = g * 4 / GPC; u < (g + 1) * 4 / GPC; ++u) {
+            u32x4 o;
 #pragma unroll
-          for (int t = g * 4 / GPC; t < (g + 1) * 4 / GPC; ++t) {
-            const f16x8 wf = decode(wb[u][c][t], zl, zh);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-              part[mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xf[mt][c][t], wf, part[mt], 0, 0, 0);
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t r = xf[mt][c][u][e];
+              const f16x2 h = __builtin_bit_cast(f16x2, r);
+              const float lo = BF16 ? __uint_as_float(r << 16) : (float)h.x;
+              const float hi = BF16 ? __uint_as_float(r & 0xffff0000u) : (float)h.y;
+              const int shift = -ex - (e & 1 ? 4 : 0);   // columns 2, 3, 6, 7 meet codes four bits up
+              const f16x2 w = {(_Float16)ldexpf(lo, shift), (_Float16)ldexpf(hi, shift)};
+              const f16x2 unit = e & 1 ? f16x2{(_Float16)16.f, (_Float16)16.f} : f16x2{(_Float16)1.f, (_Float16)1.f};
+              sum = __builtin_amdgcn_fdot2(w, unit, sum, false);
+              o[e] = __builtin_bit_cast(uint32_t, w);
+            }
+            asm volatile("" : "+v"(o));   // packed here: one piece at a time in float beside the rows
+            xf[mt][c][u] = o;
           }
-          const float sc = from_bits16((uint32_t)(sb[u][c] >> (16 * g) & 0xffff), bf16);
+          sum += __shfl_xor(sum, 16);
+          sum += __shfl_xor(sum, 32);
+          if (quad == (c * GPC + g) % 4) xg[mt][(c * GPC + g) / 4] = sum * 0x1p-24f;
+        }
+    }
+  };
+  if (!LONG) convert_x();
+
+  auto row_of = [&](int e) { return 16 * (e >> 8) + 4 * (e >> 6 & 3) + (e >> 4 & 3); };
+  int buf = 0;
+  for (int ti = 0; ti < n_tiles; ti += NB) {
+    // a batch of tiles, over the end the last one again (its sums are then not used)
+    float* dst = red + buf * red_buf + wid * kRedWave + lane * 4;
+#pragma unroll
+    for (int u = 0; u < NB; ++u) {
+      f32x4 acc[MT];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int round = 0; round < (LONG ? a.rounds : 1); ++round) {
+        if (LONG) {
+          load_x(round);
+          convert_x();
+        }
+        // the scales, and -s z of this quad's groups
+        float sc[NC][GPC], zs[NX];
+#pragma unroll
+        for (int i = 0; i < NX; ++i) zs[i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const bool in = (LONG ? round * per_round : 0) + wid * NC + c < q.nc;
+#pragma unroll
+          for (int g = 0; g < GPC; ++g) {
+            const uint32_t bits = (uint32_t)(sb[u][c] >> (16 * g)) & 0xffffu;
+            sc[c][g] = from_bits16<BF16>(in ? bits : 0u);
+            const float z = ZP ? (float)(uint32_t)(zb[u][c] >> (8 * g) & 255) : 8.f;
+            if (quad == (c * GPC + g) % 4) zs[(c * GPC + g) / 4] = -sc[c][g] * z;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < NX; ++i)
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt)
+            acc[mt] = __builtin_amdgcn_mfma_f32_16x16x4f32(xg[mt][i], zs[i], acc[mt], 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[mt][i] = fmaf(sc, part[mt][i], acc[mt][i]);
+        for (int c = 0; c < NC; ++c) {
+#pragma unroll
+          for (int g = 0; g < GPC; ++g) {
+            f32x4 part[MT];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) part[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int t = g * 4 / GPC; t < (g + 1) * 4 / GPC; ++t) {
+              const f16x8 wf = decode(wb[u][c][t]);
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt)
+                part[mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, xf[mt][c][t]), wf, part[mt],
+                                                                  0, 0, 0);
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[mt][i] = fmaf(sc[c][g], part[mt][i], acc[mt][i]);
+            if (GPC > 1 && NC * MT > 2) {
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) asm volatile("" : "+v"(acc[mt]));
+            }
+          }
+          fetch(c, wb[u][c], sb[u][c], zb[u][c]);   // into the registers just read
         }
+        fetched();
       }
-      if (step + D < steps) fetch(step + D, wb[u], sb[u], zb[u]);
-      if (round + 1 < a.rounds) continue;
-      if (nb == 0) first_tile = ti;
-      float* dst = red + buf * red_buf + wid * red_wave + nb * MT * 256;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
-        if (16 * mt + 4 * quad < M) *reinterpret_cast<f32x4*>(dst + mt * 256 + lane * 4) = acc[mt];
-      if (++nb == a.nb || ti + 1 == n_tiles) finish(nb);
+        if (16 * mt + 4 * quad < M) *reinterpret_cast<f32x4*>(dst + (u * MT + mt) * 256) = acc[mt];
+    }
+    // the batch's sums over the waves, out to memory or into the states. The next batch's partial sums go to the
+    // other buffer, so one barrier a batch is enough.
+    lds_barrier();
+    const float* src = red + buf * red_buf;
+    buf ^= 1;
+    for (int i = tid; i < NB * MT * 256; i += nthreads) {
+      // entry of a tile: v fastest, 16 columns, then the 4 rows of a quad (a wave reads 64 consecutive words), then
+      // quad and tile of rows
+      const int b = i / (MT * 256), e = i - b * (MT * 256);
+      const int m = row_of(e);
+      const long long v = (slot + (long long)(ti + b) * a.slots) * kTileV + (e & 15);
+      if (m >= M || v >= q.V) continue;
+      const float* p = src + b * MT * 256 + (e >> 8) * 256 + ((e >> 6 & 3) * 16 + (e & 15)) * 4 + (e >> 4 & 3);
+      float z = 0.f;
+      int w = 0;
+      for (; w + 8 <= W; w += 8, p += 8 * kRedWave) {
+        float t[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t[k] = p[k * kRedWave];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) z += t[k];
+      }
+      for (; w < W; ++w, p += kRedWave) z += *p;
+      z = ldexpf(z, s_exp[m] + 24);
+      if (a.stats) {   // this thread has entry i in every batch
+        Soft st = soft_unpack(states[i]);
+        soft_push(st, z * a.logit_scale, (int)v);
+        states[i] = soft_pack(st);
+        continue;
+      }
+      const long long at = (m0 + m) * a.out_stride + v;
+      if (a.out_type == 1)
+        static_cast<float*>(a.out)[at] = z;
+      else if (a.out_type == 0)
+        static_cast<__bf16*>(a.out)[at] = (__bf16)z;
+      else
+        static_cast<_Float16*>(a.out)[at] = (_Float16)z;
     }
   }
   if (!a.stats) return;
-  // the 16 columns' states of each row, in a fixed order
+  // a row's states (of the batch's tiles, 16 columns each), in a fixed order
   __syncthreads();
   for (int m = tid; m < M; m += nthreads) {
     Soft st = soft_empty();
-    for (int c16 = 0; c16 < 16; ++c16)
-      st = soft_merge(st, soft_unpack(states[(m >> 4) * 256 + (m >> 2 & 3) * 64 + (m & 3) * 16 + c16]));
+#pragma unroll 1
+    for (int i = 0; i < NB * 16; ++i)
+      st = soft_merge(st, soft_unpack(states[(i >> 4) * MT * 256 + (m >> 4) * 256 + (m & 15) * 16 + (i & 15)]));
     a.partials[(long long)(m0 + m) * a.slots + slot] = soft_pack(st);
   }
 }
@@ -358,10 +440,13 @@ __global__ __launch_bounds__(64) void k_quant_stats(QuantCall a) {
   }
 }
 
-template <int NC, int MT, int GPC>
+template <int NC, int MT, int GPC, bool LONG>
 hipError_t project_z(const QuantDims& q, const QuantCall& a, hipStream_t s) {
   const size_t lds = quant_lds_bytes(a);
-  auto kernel = a.zeros ? k_quant_project<NC, MT, GPC, true> : k_quant_project<NC, MT, GPC, false>;
+  auto kernel = a.zeros ? (a.bf16 ? k_quant_project<NC, MT, GPC, true, LONG, true>
+                                  : k_quant_project<NC, MT, GPC, true, LONG, false>)
+                        : (a.bf16 ? k_quant_project<NC, MT, GPC, false, LONG, true>
+                                  : k_quant_project<NC, MT, GPC, false, LONG, false>);
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                      (int)lds);
   if (e != hipSuccess) return e;
@@ -369,12 +454,12 @@ hipError_t project_z(const QuantDims& q, const QuantCall& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int NC, int MT>
+template <int NC, int MT, bool LONG = false>
 hipError_t project_g(const QuantDims& q, const QuantCall& a, hipStream_t s) {
   switch (q.group) {
-    case 32: return project_z<NC, MT, 4>(q, a, s);
-    case 64: return project_z<NC, MT, 2>(q, a, s);
-    default: return project_z<NC, MT, 1>(q, a, s);
+    case 32: return project_z<NC, MT, 4, LONG>(q, a, s);
+    case 64: return project_z<NC, MT, 2, LONG>(q, a, s);
+    default: return project_z<NC, MT, 1, LONG>(q, a, s);
   }
 }
 
@@ -399,7 +484,7 @@ hipError_t launch_quant_project(const QuantDims& q, const QuantCall& a, hipStrea
   else if (a.nc_wave == 2)
     e = a.row_tiles == 1 ? project_g<2, 1>(q, a, s) : project_g<2, 2>(q, a, s);
   else
-    e = project_g<4, 1>(q, a, s);
+    e = a.rounds == 1 ? project_g<4, 1>(q, a, s) : project_g<4, 1, true>(q, a, s);
   if (e != hipSuccess || !a.stats) return e;
   k_quant_stats<<<a.M, 64, 0, s>>>(a);
   return hipGetLastError();

@@ -67,7 +67,6 @@ void quant_plan(const rpd::QuantDims& q, rpd::QuantCall& a) {
   const int per_cu = std::max(1, 16 / a.waves);
   const int most = std::max(8, 256 * per_cu / a.row_groups / 8 * 8);
   a.slots = std::min(most, (int)up_div(q.vt, 8) * 8);
-  a.nb = 1;
 }
 
 rpd_status check_head(const rpd_quant_head* h) {

@@ -49,11 +49,16 @@ struct QuantCall {
   int nc_wave, row_tiles; // template shape: chunks a wave, tiles of 16 rows a workgroup
   int waves, rounds;      // waves of a workgroup; passes of them over the columns
   int row_groups, slots;  // workgroups = row_groups x slots (a multiple of 8)
-  int nb;                 // tiles between two barriers
 };
 
+// tiles of 16 vocabulary rows between two barriers, for nc chunks a wave and
+// mt tiles of 16 rows (two buffers of their sums from 16 waves have to fit LDS)
+#ifndef QB22
+#define QB22 2
+#endif
+constexpr int quant_batch(int nc, int mt) { return mt == 1 ? 4 / nc : nc == 1 ? 2 : QB22; }
 inline size_t quant_lds_bytes(const QuantCall& a) {
-  return (size_t)2 * a.waves * a.nb * a.row_tiles * 1024 + (size_t)a.row_tiles * (4096 + 16 * 64 + 64);
+  return (size_t)2 * a.waves * quant_batch(a.nc_wave, a.row_tiles) * a.row_tiles * 1024 + (size_t)a.row_tiles * (quant_batch(a.nc_wave, a.row_tiles) * 4096 + 16 * 64 + 64);
 }
 
 hipError_t launch_quant_pack(const QuantDims& q, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros,

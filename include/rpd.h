@@ -400,8 +400,8 @@ size_t rpd_quant_packed_size(const rpd_quant_head* h);
 rpd_status rpd_quant_pack(const rpd_quant_head* h, const uint8_t* codes, const void* scales, const uint8_t* zeros,
                           void* packed, size_t packed_bytes, void* stream);
 
-/* Workspace bytes that rpd_quant_project needs for M rows (0 without the
- * statistics; 0 too if h or M is out of range). */
+/* Workspace bytes that rpd_quant_project needs for M rows (0 for the logits of
+ * up to 16 rows; 0 too if h or M is out of range). */
 size_t rpd_quant_workspace_size(const rpd_quant_head* h, int32_t M, int32_t statistics);
 
 /*
@@ -419,7 +419,7 @@ size_t rpd_quant_workspace_size(const rpd_quant_head* h, int32_t M, int32_t stat
  *              probability, nats); all given or all NULL
  *   logit_scale  finite and > 0, or 0 for 1; the statistics only
  *   workspace  rpd_quant_workspace_size bytes, 256-byte aligned (may be NULL
- *              for logits); its prior contents do not matter
+ *              where that is 0); its prior contents do not matter
  * The codes are streamed once for up to 32 rows (16 above d = 4096); the
  * workgroups of further rows read them at the same time, through the caches.
  */

@@ -616,6 +616,13 @@ class QuantHead:
             raise ValueError(f"x has {x.shape[-1]} columns, the head {self.d}")
         return _rows("x", x)
 
+    def _workspace(self, M: int, statistics: int, stream) -> torch.Tensor:
+        ws = torch.empty(int(lib().rpd_quant_workspace_size(ctypes.byref(self.head), M, statistics)),
+                         dtype=torch.uint8, device=self.device)
+        if stream is not None:
+            ws.record_stream(stream)
+        return ws
+
     def logits(self, x: torch.Tensor, out_dtype: torch.dtype | None = None, out: torch.Tensor | None = None,
                stream=None) -> torch.Tensor:
         """x [..., d] through the head: [..., V] of type ``out_dtype`` (x's, or float32), into ``out`` if given."""
@@ -627,9 +634,10 @@ class QuantHead:
         _one_device("out", out, x=x)
         o = _rows("out", out)
         code = _float_code("out", out)
+        ws = self._workspace(r.shape[0], 0, stream)
         _enqueue(x.device, stream, lambda s: lib().rpd_quant_project(
             ctypes.byref(self.head), self.packed.data_ptr(), r.shape[0], r.data_ptr(), _row_stride(r), o.data_ptr(),
-            _row_stride(o), code, None, None, None, 1.0, None, 0, s))
+            _row_stride(o), code, None, None, None, 1.0, ws.data_ptr(), ws.numel(), s))
         return out
 
     def stats(self, x: torch.Tensor, logit_scale: float = 1.0, stream=None) -> dict:
@@ -640,10 +648,7 @@ class QuantHead:
         o = {"argmax": torch.empty(x.shape[:-1], dtype=torch.int32, **e),
              "confidence": torch.empty(x.shape[:-1], dtype=torch.float32, **e),
              "entropy": torch.empty(x.shape[:-1], dtype=torch.float32, **e)}
-        ws = torch.empty(int(lib().rpd_quant_workspace_size(ctypes.byref(self.head), r.shape[0], 1)),
-                         dtype=torch.uint8, **e)
-        if stream is not None:
-            ws.record_stream(stream)
+        ws = self._workspace(r.shape[0], 1, stream)
         _enqueue(x.device, stream, lambda s: lib().rpd_quant_project(
             ctypes.byref(self.head), self.packed.data_ptr(), r.shape[0], r.data_ptr(), _row_stride(r), None, 0, 0,
             o["argmax"].data_ptr(), o["confidence"].data_ptr(), o["entropy"].data_ptr(), float(logit_scale),

@@ -129,6 +129,25 @@ __device__ __forceinline__ float from_bits16(uint32_t b) {
   return BF16 ? __uint_as_float(b << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)b);
 }
 
+// 8 elements of a row as operands, scaled by 2^-ex, and their sum added to `sum`
+template <bool BF16>
+__device__ __forceinline__ u32x4 to_operand(const u32x4 r, int ex, float& sum) {
+  u32x4 o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t two = r[e];   // (a bit_cast of the vector's element itself takes the wrong one)
+    const f16x2 h = __builtin_bit_cast(f16x2, two);
+    const float lo = BF16 ? __uint_as_float(two << 16) : (float)h.x;
+    const float hi = BF16 ? __uint_as_float(two & 0xffff0000u) : (float)h.y;
+    const int shift = -ex - (e & 1 ? 4 : 0);   // columns 2, 3, 6, 7 meet codes four bits up
+    const f16x2 w = {(_Float16)ldexpf(lo, shift), (_Float16)ldexpf(hi, shift)};
+    const _Float16 unit = (_Float16)(e & 1 ? 16.f : 1.f);
+    sum = __builtin_amdgcn_fdot2(w, f16x2{unit, unit}, sum, false);
+    o[e] = __builtin_bit_cast(uint32_t, w);
+  }
+  return o;
+}
+
 // One logit into a running softmax state, with one exponential: of the
 // distance to the larger of z and m. NaN never becomes m and leaves S and T NaN.
 __device__ __forceinline__ void soft_push(Soft& s, float z, int v) {
@@ -145,8 +164,9 @@ __device__ __forceinline__ void soft_push(Soft& s, float z, int v) {
 }
 
 // NC chunks a wave, MT tiles of 16 rows, GPC groups a chunk, ZP: zero points,
-// LONG: rows longer than the waves hold, x loaded anew in every round, BF16: of that type, else fp16
-template <int NC, int MT, int GPC, bool ZP, bool LONG, bool BF16>
+// LONG: rows longer than the waves hold, x loaded anew in every round, PRE: x laid out by k_quant_rows (else the
+// workgroup converts it), BF16: of that type, else fp16
+template <int NC, int MT, int GPC, bool ZP, bool LONG, bool PRE, bool BF16>
 __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, QuantCall a) {
   constexpr int NB = quant_batch(NC, MT);       // tiles between two barriers; as many are in flight
   constexpr int NG = NC * GPC, NX = (NG + 3) / 4;   // groups of a wave; of them four to a correction
@@ -228,11 +248,21 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, Q
 #pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) xf[mt][c][u] = x_piece(mt, round * per_round + wid * NC + c, u);
+        for (int u = 0; u < 4; ++u) {
+          const int chunk = round * per_round + wid * NC + c;
+          if (!PRE) {
+            xf[mt][c][u] = x_piece(mt, chunk, u);
+          } else {
+            xf[mt][c][u] = u32x4{0u, 0u, 0u, 0u};
+            if (chunk < q.nc) xf[mt][c][u] = a.xrows[((long long)(rg * MT + mt) * q.nc + chunk) * 256 + u * 64 + lane];
+          }
+        }
   };
-  // each row's largest magnitude (the bits of either type's magnitudes are in order; infinity and NaN count as the
-  // largest finite one, the row's logits being infinite or NaN anyway)
-  {
+  if (PRE) {
+    if (tid < MT * 16) s_exp[tid] = a.xexp[rg * MT * 16 + tid];
+  } else {
+    // each row's largest magnitude (the bits of either type's magnitudes are in order; infinity and NaN count as
+    // the largest finite one, the row's logits being infinite or NaN anyway)
     const u16x2 finite = {(uint16_t)(BF16 ? 0x7f7f : 0x7bff), (uint16_t)(BF16 ? 0x7f7f : 0x7bff)};
     u16x2 big[MT];
 #pragma unroll
@@ -271,7 +301,17 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, Q
   __syncthreads();
 
   float xg[MT][NX];   // row col's sum over group 4 i + quad of this wave, in units of the products
-  auto convert_x = [&]() {
+  auto convert_x = [&](int round) {
+    if (PRE) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int i = 0; i < NX; ++i) {
+          const int g = round * per_round * GPC + wid * NG + 4 * i + quad;
+          xg[mt][i] = 4 * i + quad < NG && g < q.ngp ? a.xsum[((long long)(rg * MT + mt) * q.ngp + g) * 16 + col] : 0.f;
+        }
+      return;
+    }
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const int ex = s_exp[mt * 16 + col];
@@ -284,19 +324,7 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, Q
           float sum = 0.f;
 #pragma unroll
           for (int u = g * 4 / GPC; u < (g + 1) * 4 / GPC; ++u) {
-            u32x4 o;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t r = xf[mt][c][u][e];
-              const f16x2 h = __builtin_bit_cast(f16x2, r);
-              const float lo = BF16 ? __uint_as_float(r << 16) : (float)h.x;
-              const float hi = BF16 ? __uint_as_float(r & 0xffff0000u) : (float)h.y;
-              const int shift = -ex - (e & 1 ? 4 : 0);   // columns 2, 3, 6, 7 meet codes four bits up
-              const f16x2 w = {(_Float16)ldexpf(lo, shift), (_Float16)ldexpf(hi, shift)};
-              const f16x2 unit = e & 1 ? f16x2{(_Float16)16.f, (_Float16)16.f} : f16x2{(_Float16)1.f, (_Float16)1.f};
-              sum = __builtin_amdgcn_fdot2(w, unit, sum, false);
-              o[e] = __builtin_bit_cast(uint32_t, w);
-            }
+            u32x4 o = to_operand<BF16>(xf[mt][c][u], ex, sum);
             asm volatile("" : "+v"(o));   // packed here: one piece at a time in float beside the rows
             xf[mt][c][u] = o;
           }
@@ -306,7 +334,8 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, Q
         }
     }
   };
-  if (!LONG) convert_x();
+  if (PRE && !LONG) load_x(0);
+  if (!LONG) convert_x(0);
 
   auto row_of = [&](int e) { return 16 * (e >> 8) + 4 * (e >> 6 & 3) + (e >> 4 & 3); };
   int buf = 0;
@@ -321,7 +350,7 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, Q
       for (int round = 0; round < (LONG ? a.rounds : 1); ++round) {
         if (LONG) {
           load_x(round);
-          convert_x();
+          convert_x(round);
         }
         // the scales, and -s z of this quad's groups
         float sc[NC][GPC], zs[NX];
@@ -415,14 +444,64 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, Q
     }
   }
   if (!a.stats) return;
-  // a row's states (of the batch's tiles, 16 columns each), in a fixed order
+  // a row's states, of the batch's tiles and then of 16 columns, in a fixed order
   __syncthreads();
-  for (int m = tid; m < M; m += nthreads) {
-    Soft st = soft_empty();
-#pragma unroll 1
-    for (int i = 0; i < NB * 16; ++i)
-      st = soft_merge(st, soft_unpack(states[(i >> 4) * MT * 256 + (m >> 4) * 256 + (m & 15) * 16 + (i & 15)]));
-    a.partials[(long long)(m0 + m) * a.slots + slot] = soft_pack(st);
+  for (int e = tid; e < MT * 256; e += nthreads) {
+    Soft st = soft_unpack(states[e]);
+#pragma unroll
+    for (int b = 1; b < NB; ++b) st = soft_merge(st, soft_unpack(states[b * MT * 256 + e]));
+#pragma unroll
+    for (int k = 1; k < 16; k <<= 1) st = soft_merge(st, soft_shfl_xor(st, k));
+    if ((e & 15) == 0 && row_of(e) < M) a.partials[(long long)(m0 + row_of(e)) * a.slots + slot] = soft_pack(st);
+  }
+}
+
+// Rows of x as fp16 operands in the order in which k_quant_project reads them,
+// one workgroup a row (rows past the last as zeros): for more than 16 rows,
+// where every workgroup converting all of them for itself cost it 12 us (32
+// rows of 4096: the loads, 64 bytes a row, crowd the caches, and 2.6 us of
+// conversion).
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_quant_rows(QuantDims q, QuantCall a) {
+  const int m = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  __shared__ uint32_t s_max[4];
+  const uint16_t* x = a.x + m * a.x_stride;
+  auto piece = [&](int k) {
+    u32x4 r = {0u, 0u, 0u, 0u};
+    if (m >= a.M || k >= q.d) return r;
+    if (a.x_vec) return *reinterpret_cast<const u32x4*>(x + k);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = (uint32_t)x[k + 2 * e] | (uint32_t)x[k + 2 * e + 1] << 16;
+    return r;
+  };
+  const int pieces = q.nc * 16;
+  u16x2 big = {0, 0};
+  for (int p = tid; p < pieces; p += 256) {
+    const u32x4 r = piece(8 * p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) big = __builtin_elementwise_max(big, __builtin_bit_cast(u16x2, r[e] & 0x7fff7fffu));
+  }
+  uint32_t top = min((uint32_t)max(big.x, big.y), BF16 ? 0x7f7fu : 0x7bffu);
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, k));
+  if (lane == 0) s_max[tid >> 6] = top;
+  __syncthreads();
+  top = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+  int ex = 15;
+  if (top) (void)frexpf(from_bits16<BF16>(top), &ex);
+  ex -= 15;
+  if (tid == 0) a.xexp[m] = ex;
+  const int rt = m >> 4, col = m & 15, per_group = q.group / 8;   // a group is 4, 8 or 16 neighbouring lanes' pieces
+  for (int p0 = 0; p0 < pieces; p0 += 256) {
+    const int p = p0 + tid;
+    float sum = 0.f;
+    if (p < pieces) {
+      const u32x4 o = to_operand<BF16>(piece(8 * p), ex, sum);
+      a.xrows[((long long)rt * q.nc + (p >> 4)) * 256 + (p >> 2 & 3) * 64 + (p & 3) * 16 + col] = o;
+    }
+    for (int k = 1; k < per_group; k <<= 1) sum += __shfl_xor(sum, k);
+    if (p < pieces && p % per_group == 0)
+      a.xsum[((long long)rt * q.ngp + p / per_group) * 16 + col] = sum * 0x1p-24f;
   }
 }
 
@@ -440,13 +519,13 @@ __global__ __launch_bounds__(64) void k_quant_stats(QuantCall a) {
   }
 }
 
-template <int NC, int MT, int GPC, bool LONG>
+template <int NC, int MT, int GPC, bool LONG, bool PRE>
 hipError_t project_z(const QuantDims& q, const QuantCall& a, hipStream_t s) {
   const size_t lds = quant_lds_bytes(a);
-  auto kernel = a.zeros ? (a.bf16 ? k_quant_project<NC, MT, GPC, true, LONG, true>
-                                  : k_quant_project<NC, MT, GPC, true, LONG, false>)
-                        : (a.bf16 ? k_quant_project<NC, MT, GPC, false, LONG, true>
-                                  : k_quant_project<NC, MT, GPC, false, LONG, false>);
+  auto kernel = a.zeros ? (a.bf16 ? k_quant_project<NC, MT, GPC, true, LONG, PRE, true>
+                                  : k_quant_project<NC, MT, GPC, true, LONG, PRE, false>)
+                        : (a.bf16 ? k_quant_project<NC, MT, GPC, false, LONG, PRE, true>
+                                  : k_quant_project<NC, MT, GPC, false, LONG, PRE, false>);
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                      (int)lds);
   if (e != hipSuccess) return e;
@@ -454,12 +533,12 @@ hipError_t project_z(const QuantDims& q, const QuantCall& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int NC, int MT, bool LONG = false>
+template <int NC, int MT, bool PRE, bool LONG = false>
 hipError_t project_g(const QuantDims& q, const QuantCall& a, hipStream_t s) {
   switch (q.group) {
-    case 32: return project_z<NC, MT, 4, LONG>(q, a, s);
-    case 64: return project_z<NC, MT, 2, LONG>(q, a, s);
-    default: return project_z<NC, MT, 1, LONG>(q, a, s);
+    case 32: return project_z<NC, MT, 4, LONG, PRE>(q, a, s);
+    case 64: return project_z<NC, MT, 2, LONG, PRE>(q, a, s);
+    default: return project_z<NC, MT, 1, LONG, PRE>(q, a, s);
   }
 }
 
@@ -479,12 +558,23 @@ hipError_t launch_quant_pack(const QuantDims& q, const uint8_t* codes, const uin
 
 hipError_t launch_quant_project(const QuantDims& q, const QuantCall& a, hipStream_t s) {
   hipError_t e;
+  const bool pre = a.xrows != nullptr;
+  if (pre) {
+    const int rows = a.row_groups * a.row_tiles * 16;
+    if (a.bf16)
+      k_quant_rows<true><<<rows, 256, 0, s>>>(q, a);
+    else
+      k_quant_rows<false><<<rows, 256, 0, s>>>(q, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
   if (a.nc_wave == 1)
-    e = a.row_tiles == 1 ? project_g<1, 1>(q, a, s) : project_g<1, 2>(q, a, s);
+    e = pre ? project_g<1, 2, true>(q, a, s) : project_g<1, 1, false>(q, a, s);
   else if (a.nc_wave == 2)
-    e = a.row_tiles == 1 ? project_g<2, 1>(q, a, s) : project_g<2, 2>(q, a, s);
+    e = pre ? project_g<2, 2, true>(q, a, s) : project_g<2, 1, false>(q, a, s);
+  else if (a.rounds == 1)
+    e = pre ? project_g<4, 1, true>(q, a, s) : project_g<4, 1, false>(q, a, s);
   else
-    e = a.rounds == 1 ? project_g<4, 1>(q, a, s) : project_g<4, 1, true>(q, a, s);
+    e = pre ? project_g<4, 1, true, true>(q, a, s) : project_g<4, 1, false, true>(q, a, s);
   if (e != hipSuccess || !a.stats) return e;
   k_quant_stats<<<a.M, 64, 0, s>>>(a);
   return hipGetLastError();

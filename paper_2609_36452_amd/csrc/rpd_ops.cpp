@@ -69,6 +69,22 @@ void quant_plan(const rpd::QuantDims& q, rpd::QuantCall& a) {
   a.slots = std::min(most, (int)up_div(q.vt, 8) * 8);
 }
 
+// Workspace of a call: the laid out rows (more than 16 of them), then the states of the statistics.
+struct QuantSpace {
+  size_t rows, sums, exps, states, bytes;   // offsets
+};
+QuantSpace quant_space(const rpd::QuantDims& q, const rpd::QuantCall& a) {
+  QuantSpace w{};
+  if (a.M > 16) {
+    const size_t tiles = (size_t)a.row_groups * a.row_tiles;
+    w.sums = round256(tiles * q.nc * 4096);
+    w.exps = w.sums + round256(tiles * q.ngp * 64);
+    w.states = w.exps + round256(tiles * 64);
+  }
+  w.bytes = w.states + (a.stats ? round256((size_t)a.M * a.slots * 16) : 0);
+  return w;
+}
+
 rpd_status check_head(const rpd_quant_head* h) {
   if (!h) return fail(RPD_ERR_NULL_POINTER, "head is NULL");
   if (!quant_shape_ok(h))
@@ -204,11 +220,13 @@ rpd_status rpd_quant_pack(const rpd_quant_head* h, const uint8_t* codes, const v
 }
 
 size_t rpd_quant_workspace_size(const rpd_quant_head* h, int32_t M, int32_t statistics) {
-  if (!h || !quant_ok(h) || M < 1 || M > 1 << 20 || !statistics) return 0;
+  if (!h || !quant_ok(h) || M < 1 || M > 1 << 20) return 0;
   rpd::QuantCall a{};
   a.M = M;
-  quant_plan(quant_dims(h), a);
-  return round256((size_t)M * a.slots * 16);
+  a.stats = statistics != 0;
+  const rpd::QuantDims q = quant_dims(h);
+  quant_plan(q, a);
+  return quant_space(q, a).bytes;
 }
 
 rpd_status rpd_quant_project(const rpd_quant_head* h, const void* packed, int32_t M, const void* x, int64_t x_stride,
@@ -254,10 +272,17 @@ rpd_status rpd_quant_project(const rpd_quant_head* h, const void* packed, int32_
   a.confidence = confidence;
   a.entropy = entropy;
   quant_plan(q, a);
-  if (a.stats) {
-    st = check_workspace(workspace, workspace_bytes, round256((size_t)M * a.slots * 16));
+  const QuantSpace w = quant_space(q, a);
+  if (w.bytes > 0) {
+    st = check_workspace(workspace, workspace_bytes, w.bytes);
     if (st != RPD_OK) return st;
-    a.partials = static_cast<float4*>(workspace);
+    char* ws = static_cast<char*>(workspace);
+    if (M > 16) {
+      a.xrows = reinterpret_cast<rpd::codes_t*>(ws);
+      a.xsum = reinterpret_cast<float*>(ws + w.sums);
+      a.xexp = reinterpret_cast<int32_t*>(ws + w.exps);
+    }
+    a.partials = reinterpret_cast<float4*>(ws + w.states);
   }
   const hipError_t e = rpd::launch_quant_project(q, a, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(RPD_ERR_HIP, "launch: %s", hipGetErrorString(e));

@@ -23,7 +23,7 @@
 // is the same for every vocabulary row (equal rows give equal logits).
 #include <cstdint>
 
-#include "rpd_device.h"
+#include "reduce_device.h"
 #include "rpd_ops.h"
 
 namespace rpd {
@@ -71,15 +71,19 @@ __global__ __launch_bounds__(256) void k_quant_pack(QuantDims q, const uint8_t* 
   reinterpret_cast<u32x4*>(out)[i] = o;
 }
 
-// scales and zero points: [16 vt][ngp], rows padded to whole chunks
+// Scales and zero points of tile t, chunk c: [16 rows][groups of a chunk], so that a chunk's are one or two lines
+// (row by row they were 16 lines a load).
 __global__ __launch_bounds__(256) void k_quant_pack_scales(QuantDims q, const uint16_t* __restrict__ scales,
                                                            const uint8_t* __restrict__ zeros,
                                                            uint16_t* __restrict__ s_out, uint8_t* __restrict__ z_out) {
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
   const long long n = (long long)q.vt * kTileV * q.ngp;
   if (i >= n) return;
-  const long long v = i / q.ngp;
-  const int g = (int)(i - v * q.ngp);
+  const int gpc = kChunk / q.group;
+  const long long tc = i / (kTileV * gpc);
+  const int c = (int)(tc % q.nc), in_chunk = (int)(i - tc * (kTileV * gpc));
+  const long long v = tc / q.nc * kTileV + in_chunk / gpc;
+  const int g = c * gpc + in_chunk % gpc;
   const bool in = v < q.V && g < q.ng;
   s_out[i] = in ? scales[v * q.ng + g] : (uint16_t)0;
   if (z_out) z_out[i] = in ? zeros[v * q.ng + g] & 15 : (uint8_t)0;
@@ -195,8 +199,8 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, Q
   u32x4 wb[NB][NC];
   sraw_t sb[NB][NC];
   zraw_t zb[NB][NC];
-  const uint32_t w_lane = lane * 16, z_lane = (uint32_t)(col * q.nc * GPC);
-  const int s_range = ((kTileV - 1) * q.nc + 1) * 2 * GPC;   // bytes from a chunk's first scale to its last
+  const uint32_t w_lane = lane * 16, z_lane = col * GPC;
+  constexpr int s_range = kTileV * GPC * 2;
   // The step to be fetched next. Fetches are never skipped (the last tile is fetched again instead): with one that
   // may be, the compiler cannot count the loads in flight and waits for all of them.
   const int last_tile = n_tiles > 0 ? slot + (n_tiles - 1) * a.slots : 0;
@@ -206,7 +210,7 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, Q
     const int chunk = min((LONG ? f_round * per_round : 0) + wid * NC + c, q.nc - 1);
     // buffer loads: a resource at the chunk and a lane's fixed offset, no 64-bit address a lane
     char* w_base = const_cast<char*>(reinterpret_cast<const char*>(a.codes)) + ((long long)f_tile * q.nc + chunk) * 1024;
-    const long long entry = ((long long)f_tile * kTileV * q.nc + chunk) * GPC;
+    const long long entry = ((long long)f_tile * q.nc + chunk) * (kTileV * GPC);
     char* s_base = const_cast<char*>(reinterpret_cast<const char*>(a.scales)) + entry * 2;
     char* z_base = const_cast<char*>(reinterpret_cast<const char*>(a.zeros)) + entry;
     const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(w_base, (short)0, 1024, kRsrcFlags);
@@ -475,12 +479,18 @@ __global__ __launch_bounds__(256) void k_quant_rows(QuantDims q, QuantCall a) {
     return r;
   };
   const int pieces = q.nc * 16;
+  constexpr int kHeld = 4;   // a thread's first pieces are read once (rows of up to 8192)
+  u32x4 held[kHeld];
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) held[j] = piece(8 * (tid + 256 * j));
   u16x2 big = {0, 0};
-  for (int p = tid; p < pieces; p += 256) {
-    const u32x4 r = piece(8 * p);
+  auto grow = [&](const u32x4 r) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) big = __builtin_elementwise_max(big, __builtin_bit_cast(u16x2, r[e] & 0x7fff7fffu));
-  }
+  };
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) grow(held[j]);
+  for (int p = tid + 256 * kHeld; p < pieces; p += 256) grow(piece(8 * p));
   uint32_t top = min((uint32_t)max(big.x, big.y), BF16 ? 0x7f7fu : 0x7bffu);
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, k));
@@ -492,26 +502,27 @@ __global__ __launch_bounds__(256) void k_quant_rows(QuantDims q, QuantCall a) {
   ex -= 15;
   if (tid == 0) a.xexp[m] = ex;
   const int rt = m >> 4, col = m & 15, per_group = q.group / 8;   // a group is 4, 8 or 16 neighbouring lanes' pieces
-  for (int p0 = 0; p0 < pieces; p0 += 256) {
-    const int p = p0 + tid;
+  auto put = [&](int p, const u32x4 r) {
     float sum = 0.f;
     if (p < pieces) {
-      const u32x4 o = to_operand<BF16>(piece(8 * p), ex, sum);
+      const u32x4 o = to_operand<BF16>(r, ex, sum);
       a.xrows[((long long)rt * q.nc + (p >> 4)) * 256 + (p >> 2 & 3) * 64 + (p & 3) * 16 + col] = o;
     }
     for (int k = 1; k < per_group; k <<= 1) sum += __shfl_xor(sum, k);
     if (p < pieces && p % per_group == 0)
       a.xsum[((long long)rt * q.ngp + p / per_group) * 16 + col] = sum * 0x1p-24f;
-  }
+  };
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if (256 * j < pieces) put(tid + 256 * j, held[j]);
+  for (int p0 = 256 * kHeld; p0 < pieces; p0 += 256) put(p0 + tid, piece(8 * (p0 + tid)));
 }
 
 // one wave a row: the slots' states -> argmax, top probability, entropy
 __global__ __launch_bounds__(64) void k_quant_stats(QuantCall a) {
   const int m = blockIdx.x, lane = threadIdx.x;
-  Soft st = soft_empty();
-  for (int i = lane; i < a.slots; i += 64) st = soft_merge(st, soft_unpack(a.partials[(long long)m * a.slots + i]));
-#pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) st = soft_merge(st, soft_shfl_xor(st, k));
+  float4 keep[8];
+  const Soft st = wave_merge_row(a.partials + (long long)m * a.slots, a.slots, lane, keep);
   if (lane == 0) {
     a.argmax[m] = st.idx;
     a.confidence[m] = 1.f / st.S;

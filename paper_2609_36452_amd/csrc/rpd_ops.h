@@ -54,14 +54,13 @@ struct QuantCall {
   int row_groups, slots;  // workgroups = row_groups x slots (a multiple of 8)
 };
 
-// tiles of 16 vocabulary rows between two barriers, for nc chunks a wave and
-// mt tiles of 16 rows (two buffers of their sums from 16 waves have to fit LDS)
-#ifndef QB22
-#define QB22 2
-#endif
-constexpr int quant_batch(int nc, int mt) { return mt == 1 ? 4 / nc : nc == 1 ? 2 : QB22; }
+// tiles of 16 vocabulary rows between two barriers (and in flight), for nc
+// chunks a wave and mt tiles of 16 rows: two buffers of their sums from 16 waves
+// have to fit LDS
+constexpr int quant_batch(int nc, int mt) { return mt == 1 ? 4 / nc : 2; }
 inline size_t quant_lds_bytes(const QuantCall& a) {
-  return (size_t)2 * a.waves * quant_batch(a.nc_wave, a.row_tiles) * a.row_tiles * 1024 + (size_t)a.row_tiles * (quant_batch(a.nc_wave, a.row_tiles) * 4096 + 16 * 64 + 64);
+  const int nb = quant_batch(a.nc_wave, a.row_tiles);
+  return (size_t)2 * a.waves * nb * a.row_tiles * 1024 + (size_t)a.row_tiles * (nb * 4096 + 16 * 64 + 64);
 }
 
 hipError_t launch_quant_pack(const QuantDims& q, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros,

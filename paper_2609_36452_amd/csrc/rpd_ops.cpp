@@ -9,6 +9,9 @@
 using rpd::fail;
 using rpd::round256;
 
+#ifndef SINGLE
+#define SINGLE 12000000
+#endif
 namespace {
 
 constexpr long long kMaxBlocks = (1LL << 24) - 1;   // workgroups of 256 threads: a launch holds fewer than 2^32 threads
@@ -103,22 +106,36 @@ bool verify_shape_ok(const rpd_verify* p) {
   return p->B >= 1 && p->T >= 0 && p->V >= 1 && p->V <= (1 << 28) && (long long)p->B * ((long long)p->T + 1) <= 1 << 20;
 }
 
+constexpr long long kFill = 4096;   // workgroups of 256 threads: 256 CUs, 8 on each, twice
+
+// logits from which float32 statistics and a pass of float64 sums over the sampled rows beat float64 statistics
+constexpr long long kSingleStats = SINGLE;
+
 struct VerifyPlan {
   int splits, chunk, parts, part;
   long long rows;
-  size_t bytes;
+  bool single;                         // statistics in float32
+  size_t picks, sums, totals, bytes;   // workspace offsets
 };
 
 VerifyPlan verify_plan(const rpd_verify* p) {
   VerifyPlan v{};
   const bool greedy = (p->flags & RPD_VERIFY_GREEDY) != 0;
   v.rows = (long long)p->B * (p->T + 1) + (p->draft && !greedy ? (long long)p->B * p->T : 0);
-  // parts of whole 2048 elements (8 a thread); at most 64, which one wave merges in a step
+  // Parts of whole 2048 entries (8 a thread), at most 64 of them, which one wave merges in a step. For the
+  // statistics, as long as the launch fills the GPU's workgroups twice over, longer ones of up to 8192, which a
+  // thread holds in registers (a workgroup's start and merges cost about as much as 2048 entries).
   v.part = (int)up_div(up_div(p->V, 64), 2048) * 2048;
   v.parts = (int)up_div(p->V, v.part);
   v.chunk = v.part;
-  v.splits = v.parts;
-  v.bytes = round256((size_t)v.rows * v.splits * 8) + (greedy ? 0 : round256((size_t)3 * p->B * v.parts * 8));
+  while (v.chunk < 8192 && v.rows * up_div(p->V, 2 * v.chunk) >= kFill) v.chunk *= 2;
+  v.splits = (int)up_div(p->V, v.chunk);
+  v.picks = round256((size_t)v.rows * v.splits * sizeof(rpd::RowPart));
+  v.sums = v.picks + round256((size_t)p->B * sizeof(rpd::VerifyPick));
+  const size_t sums = round256((size_t)2 * p->B * v.parts * sizeof(double));
+  v.single = v.rows * p->V >= kSingleStats;
+  v.totals = v.sums + sums;
+  v.bytes = greedy ? v.picks : v.totals + (v.single ? sums : 0);
   return v;
 }
 
@@ -342,8 +359,11 @@ rpd_status rpd_verify_draft(const rpd_verify* p, void* workspace, size_t workspa
   a.out_token = p->out_token;
   a.n_accept = p->n_accept;
   a.accept = p->accept;
-  a.stats = static_cast<float2*>(workspace);
-  a.sums = reinterpret_cast<double*>(static_cast<char*>(workspace) + round256((size_t)v.rows * v.splits * 8));
+  char* ws = static_cast<char*>(workspace);
+  a.stats = reinterpret_cast<rpd::RowPart*>(ws);
+  a.picks = reinterpret_cast<rpd::VerifyPick*>(ws + v.picks);
+  a.sums = reinterpret_cast<double*>(ws + v.sums);
+  a.totals = v.single ? reinterpret_cast<double*>(ws + v.totals) : nullptr;
   a.splits = v.splits;
   a.chunk = v.chunk;
   a.parts = v.parts;

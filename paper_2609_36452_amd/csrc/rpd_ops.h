@@ -69,6 +69,21 @@ hipError_t launch_quant_project(const QuantDims& q, const QuantCall& a, hipStrea
 
 // ------------------------------------------------------------ verify.hip --
 
+// a part of a row of logits: its maximum, and the sum of e^(scale (z - m)) or the maximum's lowest index
+struct RowPart {
+  double S;
+  float m;
+  int idx;
+};
+
+// the rows that a sequence draws its further token from
+struct VerifyPick {
+  double sp, sq;          // sums of the target's row n and, if token n was turned down, of the draft's
+  float mp, mq;           // their maxima
+  int x;                  // the token turned down, or -1
+  int down;
+};
+
 struct VerifyCall {
   int B, T, V, dtype;
   const void* target;     // [B][T+1][V]
@@ -85,10 +100,12 @@ struct VerifyCall {
   int32_t* n_accept;      // [B]
   float* accept;          // [B][T]
   // workspace
-  float2* stats;          // [rows][splits]: maximum and sum, or maximum and index
-  double* sums;           // [3][B][parts]
-  int splits, chunk;      // of a row, for the statistics
-  int parts, part;        // of a sampled row, in the float64 sums
+  RowPart* stats;         // [rows][splits]
+  VerifyPick* picks;      // [B]
+  double* sums;           // [2][B][parts]: of p, of max(0, p - q)
+  double* totals;         // [2][B][parts]: of the exponentials of the sampled rows; NULL: the statistics are float64
+  int splits, chunk;      // parts of a row, of `chunk` entries, for the statistics
+  int parts, part;        // and for the sums of a sampled row
 };
 
 hipError_t launch_verify(const VerifyCall& a, hipStream_t s);

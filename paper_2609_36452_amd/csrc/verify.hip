@@ -7,16 +7,20 @@
 //   where that is empty), p_n if the draft ended; the next token is the lowest
 //   v with w_0 + .. + w_v > r sum w
 //
-// Bound: one read of the rows. The steps:
+// Bound: one read of the rows, and for the small calls the latency of the
+// launches. The steps:
 //   k_verify_stats   maximum and sum of a part of a row, every row at once
-//                    (float32: an acceptance is off by about 1e-7)
-//   k_verify_pick    each workgroup merges its sequence's statistics, finds n,
-//                    and sums its part of row n in float64
-//   k_verify_rest    the parts of sum w, float64 (only with draft logits)
+//   k_verify_decide  a sequence's acceptance probabilities, n, and the row that
+//                    the further token is drawn from
+//   k_verify_totals  float64 sums of that row (after float32 statistics)
+//   k_verify_parts   sums of max(0, p - q), and of p, over parts of that row
 //   k_verify_token   the part that r falls in, then the token in it
-// The token's border lies among up to V cumulative sums a few 1e-6 apart, so
-// these are float64 throughout, exponentials included: in float32 a draw in a
-// hundred of a flat row would fall on the neighbour of the right token.
+// The draw is float64, exponentials included: the token's border lies among up
+// to V cumulative sums a few 1e-6 apart, and in float32 a draw in a hundred of
+// a flat row would fall on the neighbour of the right token. Few rows take
+// their statistics in float64 as well, which saves a launch; many rows do not
+// (a float64 exponential is 12 double operations at half the rate of single
+// ones: 288 target and 130 draft rows of 152064 bf16 take 39 us, 18 in float32).
 #include <cstdint>
 
 #include "logit_rows.h"
@@ -25,7 +29,58 @@
 namespace rpd {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr double k32PerLn2 = 46.166241308446828384;   // 32 / ln 2
+
+// e^(scale z - scale m) in float64, to about 1e-12: with z in units of 1/32
+// octave, n the nearest whole one and f the rest, 2^(n >> 5) by the exponent,
+// 2^((n & 31) / 32) from a table of 32 (one entry per pair of LDS banks: no
+// conflicts) and e^(f ln 2 / 32) by its series to the fourth power.
+struct Exp64 {
+  static constexpr double kLow = -31800.0;   // 1/32 octaves below which it is 0 (the exponent stays a normal one)
+  double k, m;
+  const double* table;
+  __device__ __forceinline__ Exp64(float top, float scale, const double* t)
+      : k((double)scale * k32PerLn2), m(top == -INFINITY ? 0.0 : (double)top), table(t) {}
+  // the difference first: rows far from 0 lose nothing
+  __device__ __forceinline__ double octaves(float z) const { return ((double)z - m) * k; }
+  // t at least kLow
+  __device__ __forceinline__ double power(double t) const {
+    constexpr double u = 0.021660849392498290;   // ln 2 / 32
+    constexpr double kShift = 6755399441055744.0;   // 1.5 * 2^52: the sum's low word is the nearest integer
+    const double s = t + kShift, f = t - (s - kShift);
+    double p = fma(f, u * u * u * u / 24, u * u * u / 6);
+    p = fma(f, p, u * u / 2);
+    p = fma(f, p, u);
+    p = fma(f, p, 1.0);
+    const int n = __double2loint(s);
+    const double w = table[n & 31];
+    return p * __hiloint2double(__double2hiint(w) + ((n >> 5) << 20), __double2loint(w));
+  }
+  __device__ __forceinline__ double operator()(float z) const {
+    const double t = octaves(z);
+    return t < kLow ? 0.0 : power(t);
+  }
+  // for sums: below kLow what is added is less than 1e-299 (NaN stays NaN)
+  __device__ __forceinline__ double about(float z) const {
+    const double t = octaves(z);
+    return power(t < kLow ? kLow : t);
+  }
+};
+// 2^(j / 32)
+__device__ const double kPowers[32] = {
+    1.0, 1.0218971486541166, 1.0442737824274138, 1.0671404006768237,
+    1.0905077326652577, 1.1143867425958924, 1.1387886347566916, 1.1637248587775775,
+    1.189207115002721, 1.215247359980469, 1.241857812073484, 1.2690509571917332,
+    1.2968395546510096, 1.3252366431597413, 1.3542555469368927, 1.383909881963832,
+    1.4142135623730951, 1.4451808069770467, 1.4768261459394993, 1.5091644275934228,
+    1.5422108254079407, 1.5759808451078865, 1.6104903319492543, 1.645755478153965,
+    1.681792830507429, 1.718619298122478, 1.7562521603732995, 1.7947090750031072,
+    1.8340080864093424, 1.8741676341103, 1.9152065613971474, 1.9571441241754002,
+};
+__device__ __forceinline__ void fill_table(double* t) {
+  if (threadIdx.x < 32) t[threadIdx.x] = kPowers[threadIdx.x];
+}
 
 template <class E>
 __device__ __forceinline__ const typename E::t* target_row(const VerifyCall& a, int b, int t) {
@@ -40,7 +95,8 @@ __device__ __forceinline__ int draft_len(const VerifyCall& a, int b) {
 }
 
 // rows: the target's B (T + 1), then the draft's B T
-template <class E>
+enum Stats { kGreedy, kDouble, kSingle };   // maximum and its lowest index; maximum and sum in float64 or float32
+template <class E, Stats KIND>
 __global__ __launch_bounds__(kThreads) void k_verify_stats(VerifyCall a) {
   const int split = blockIdx.x % a.splits, row = blockIdx.x / a.splits;
   const bool is_draft = row >= a.B * (a.T + 1);
@@ -48,280 +104,418 @@ __global__ __launch_bounds__(kThreads) void k_verify_stats(VerifyCall a) {
   const int b = rr / per, t = rr - b * per;
   if (is_draft ? t >= draft_len(a, b) : t > draft_len(a, b)) return;   // rows behind the draft are not read
   const typename E::t* p = is_draft ? draft_row<E>(a, b, t) : target_row<E>(a, b, t);
-  const float scale = is_draft ? a.draft_scale : a.target_scale;
   const int lo = split * a.chunk, hi = min(a.V, lo + a.chunk);
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-  __shared__ float2 s_part[kThreads / 64];
-  if (a.greedy) {
-    float m = -INFINITY;
-    int idx = INT_MAX;
-    for (int i = lo + threadIdx.x; i < hi; i += kThreads) {
-      const float z = E::one(p + i);
-      const bool up = z > m;
-      m = up ? z : m;
-      idx = up ? i : idx;
-    }
-#pragma unroll
-    for (int k = 32; k >= 1; k >>= 1) {
-      const float om = __shfl_xor(m, k);
-      const int oi = __shfl_xor(idx, k);
-      idx = om > m ? oi : om < m ? idx : min(idx, oi);
-      m = fmaxf(m, om);
-    }
-    if (lane == 0) s_part[wid] = make_float2(m, __int_as_float(idx));
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      for (int w = 1; w < kThreads / 64; ++w) {
-        const float om = s_part[w].x;
-        const int oi = __float_as_int(s_part[w].y);
-        idx = om > m ? oi : om < m ? idx : min(idx, oi);
-        m = fmaxf(m, om);
-      }
-      a.stats[(long long)row * a.splits + split] = make_float2(m, __int_as_float(idx));
-    }
-    return;
-  }
-  MaxSum s{-INFINITY, 0.f};
-  for (int i = lo + 8 * threadIdx.x; i < hi; i += 8 * kThreads) {
-    float z[8];
+  __shared__ float s_max[kWaves];
+  __shared__ int s_idx[kWaves];
+  __shared__ double s_sum[kWaves], s_table[32];
+  // the part's first vectors are held, a longer part's others read again
+  constexpr int kHeld = 4;
+  Eight<E> held[kHeld];
+  auto get = [&](int i, Eight<E>& v) {
     if (i + 8 <= hi) {
-      Eight<E> v;
       v.load(p + i);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = v.at(e);
     } else {
+      float z[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) z[e] = i + e < hi ? E::one(p + i + e) : -INFINITY;
+      v.set(z);
     }
-    maxsum_push(s, z, scale);
+  };
+  const int first = lo + 8 * threadIdx.x;
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if (first + j * 8 * kThreads < hi) get(first + j * 8 * kThreads, held[j]);
+  if (KIND == kDouble) fill_table(s_table);
+  float m = -INFINITY;
+  int idx = INT_MAX;
+  auto top = [&](int i, const Eight<E>& v) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float z = v.at(e);
+      if (KIND == kGreedy) idx = z > m ? i + e : idx;
+      m = fmaxf(m, z);
+    }
+  };
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if (first + j * 8 * kThreads < hi) top(first + j * 8 * kThreads, held[j]);
+  for (int i = first + kHeld * 8 * kThreads; i < hi; i += 8 * kThreads) {
+    Eight<E> v;
+    get(i, v);
+    top(i, v);
   }
-  s = wave_maxsum(s, scale);
-  if (lane == 0) s_part[wid] = make_float2(s.m, s.S);
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) {
+    const float om = __shfl_xor(m, k);
+    if (KIND == kGreedy) {
+      const int oi = __shfl_xor(idx, k);
+      idx = om > m ? oi : om < m ? idx : min(idx, oi);
+    }
+    m = fmaxf(m, om);
+  }
+  if (lane == 0) {
+    s_max[wid] = m;
+    s_idx[wid] = idx;
+  }
+  __syncthreads();
+  for (int w = 0; w < kWaves; ++w) {
+    const float om = s_max[w];
+    if (KIND == kGreedy) idx = om > m ? s_idx[w] : om < m ? idx : min(idx, s_idx[w]);
+    m = fmaxf(m, om);
+  }
+  RowPart& out = a.stats[(long long)row * a.splits + split];
+  if (KIND == kGreedy) {
+    if (threadIdx.x == 0) out = RowPart{0.0, m, idx};
+    return;
+  }
+  const float scale = is_draft ? a.draft_scale : a.target_scale, ref = ref_of(m, scale);
+  const Exp64 ex(m, scale, s_table);
+  double sum = 0.0;
+  float single = 0.f;
+  auto add = [&](const Eight<E>& v) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (KIND == kDouble)
+        sum += ex.about(v.at(e));
+      else
+        single += __expf(fmaf(v.at(e), scale, -ref));
+    }
+  };
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if (first + j * 8 * kThreads < hi) add(held[j]);
+  for (int i = first + kHeld * 8 * kThreads; i < hi; i += 8 * kThreads) {
+    Eight<E> v;
+    get(i, v);
+    add(v);
+  }
+  if (KIND == kSingle) sum = single;
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) sum += __shfl_xor(sum, k);
+  if (lane == 0) s_sum[wid] = sum;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < kThreads / 64; ++w) s = maxsum_merge(s, MaxSum{s_part[w].x, s_part[w].y}, scale);
-    a.stats[(long long)row * a.splits + split] = make_float2(s.m, s.S);
+    for (int w = 1; w < kWaves; ++w) sum += s_sum[w];
+    if (KIND == kSingle && m > -INFINITY) sum *= exp((double)ref - (double)m * (double)scale);   // the reference's rounding
+    // a part of nothing but -inf has no sum (one of NaN does not end here: its sum is NaN)
+    out = RowPart{m == -INFINITY && sum == sum ? 0.0 : sum, m, 0};
   }
 }
 
-// a row's statistics, merged by one wave in a fixed order
-__device__ __forceinline__ MaxSum row_stats(const VerifyCall& a, long long row, float scale, int lane) {
-  MaxSum s{-INFINITY, 0.f};
-  for (int i = lane; i < a.splits; i += 64) {
-    const float2 v = a.stats[row * a.splits + i];
-    s = maxsum_merge(s, MaxSum{v.x, v.y}, scale);
-  }
-  return wave_maxsum(s, scale);
-}
-
-struct Pick {
-  int n;           // accepted tokens
-  int len;
-  float mp, mq;    // references (scaled maxima) of the target's row n and, if turned down, the draft's
+// a row's maximum and sum, by one wave in a fixed order
+struct Row {
+  float m;
+  double S;
 };
+__device__ __forceinline__ Row row_stats(const VerifyCall& a, long long row, float scale, int lane) {
+  float m = -INFINITY;
+  for (int i = lane; i < a.splits; i += 64) m = fmaxf(m, a.stats[row * a.splits + i].m);
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+  double S = 0.0;
+  for (int i = lane; i < a.splits; i += 64) {
+    const RowPart v = a.stats[row * a.splits + i];
+    S += v.m == -INFINITY ? v.S : v.S * exp(((double)v.m - (double)m) * (double)scale);
+  }
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) S += __shfl_xor(S, k);
+  return Row{m, S};
+}
 
-// what the sequence b comes to (the whole workgroup; s_acc: T + 1 floats of LDS, s_pick: one Pick)
+// One workgroup a sequence, a wave a row in turn. A wave keeps the statistics of the first token it turns down (and
+// of the row behind the draft, which ends it as well); the one with the first of all writes the pick.
+constexpr int kDecideWaves = 8;
 template <class E>
-__device__ __forceinline__ void decide(const VerifyCall& a, int b, bool write, Pick* s_pick) {
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+__global__ __launch_bounds__(kDecideWaves * 64) void k_verify_decide(VerifyCall a) {
+  const int b = blockIdx.x, lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
   const int len = draft_len(a, b);
   __shared__ int s_first;
   if (threadIdx.x == 0) s_first = len;
   __syncthreads();
-  for (int t = wid; t < len; t += kThreads / 64) {
-    const MaxSum p = row_stats(a, (long long)b * (a.T + 1) + t, a.target_scale, lane);
-    const int x = a.token[(long long)b * a.T + t];
-    double l = -INFINITY;
-    if (x >= 0 && x < a.V) {
-      l = (double)E::one(target_row<E>(a, b, t) + x) * (double)a.target_scale - ref_of(p.m, a.target_scale) - log((double)p.S);
-      if (a.draft) {
-        const MaxSum q = row_stats(a, (long long)a.B * (a.T + 1) + (long long)b * a.T + t, a.draft_scale, lane);
-        l -= (double)E::one(draft_row<E>(a, b, t) + x) * (double)a.draft_scale - ref_of(q.m, a.draft_scale) - log((double)q.S);
+  const long long t0 = (long long)b * (a.T + 1), d0 = (long long)a.B * (a.T + 1) + (long long)b * a.T;
+  int mine = INT_MAX;
+  VerifyPick pick;
+  for (int t = wid; t <= len; t += kDecideWaves) {
+    const bool drafted = t < len;
+    const int x = drafted ? a.token[(long long)b * a.T + t] : -1;
+    const float u = drafted ? a.u[(long long)b * a.T + t] : 0.f;
+    const bool valid = x >= 0 && x < a.V;
+    const float zp = valid ? E::one(target_row<E>(a, b, t) + x) : -INFINITY;
+    const float zq = valid && a.draft ? E::one(draft_row<E>(a, b, t) + x) : 0.f;
+    const Row p = row_stats(a, t0 + t, a.target_scale, lane);
+    Row q{0.f, 1.0};
+    if (a.draft && drafted) q = row_stats(a, d0 + t, a.draft_scale, lane);
+    float acc = 0.f;
+    if (drafted) {
+      double l = ((double)zp - (double)p.m) * (double)a.target_scale - log(p.S);
+      if (a.draft) l -= ((double)zq - (double)q.m) * (double)a.draft_scale - log(q.S);
+      acc = !valid ? 0.f : l > 0.0 ? 1.f : (float)exp(l);
+      if (lane == 0) a.accept[(long long)b * a.T + t] = acc;
+    }
+    if (mine == INT_MAX && !(drafted && u < acc)) {
+      mine = t;
+      pick = VerifyPick{p.S, q.S, p.m, q.m, x, drafted};
+      if (lane == 0) atomicMin(&s_first, t);
+    }
+  }
+  for (int t = len + threadIdx.x; t < a.T; t += kDecideWaves * 64) a.accept[(long long)b * a.T + t] = 0.f;
+  __syncthreads();
+  if (lane == 0 && mine == s_first) {
+    a.n_accept[b] = mine;
+    a.picks[b] = pick;
+  }
+}
+
+// max(0, p - q) of a sequence whose token n was turned down
+template <class E>
+struct Rest {
+  const typename E::t *p, *q;   // q NULL: 1 at x
+  Exp64 ep, eq;
+  double ip, iq;
+  int x;
+  __device__ __forceinline__ Rest(const VerifyCall& a, int b, int n, const VerifyPick& k, double sp, double sq,
+                                  const double* table)
+      : p(target_row<E>(a, b, n)), q(a.draft ? draft_row<E>(a, b, n) : nullptr), ep(k.mp, a.target_scale, table),
+        eq(k.mq, a.draft_scale, table), ip(1.0 / sp), iq(1.0 / sq), x(k.x) {}
+  // p of the 8 entries from i on (0 past the row's end) and, of a token turned down, the rest
+  __device__ __forceinline__ void eight(int i, int V, bool down, double (&p8)[8], double (&w)[8]) const {
+    Eight<E> vp, vq;
+    const bool whole = i + 8 <= V;
+    if (whole) {
+      vp.load(p + i);
+      if (down && q) vq.load(q + i);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p8[e] = w[e] = 0.0;
+      if (!whole && i + e >= V) continue;
+      p8[e] = ep(whole ? vp.at(e) : E::one(p + i + e)) * ip;
+      if (!down) continue;
+      if (q)
+        w[e] = p8[e] - eq(whole ? vq.at(e) : E::one(q + i + e)) * iq;
+      else
+        w[e] = i + e == x ? 0.0 : p8[e];
+      w[e] = w[e] > 0.0 ? w[e] : 0.0;
+    }
+  }
+};
+
+// Float64 sums over parts of the sampled rows, where the statistics are float32.
+template <class E>
+__global__ __launch_bounds__(kThreads) void k_verify_totals(VerifyCall a) {
+  const int part = blockIdx.x % a.parts, b = blockIdx.x / a.parts, n = a.n_accept[b];
+  const VerifyPick k = a.picks[b];
+  __shared__ double s_sum[kWaves][2], s_table[32];
+  fill_table(s_table);
+  __syncthreads();
+  const Exp64 ep(k.mp, a.target_scale, s_table), eq(k.mq, a.draft_scale, s_table);
+  const typename E::t* p = target_row<E>(a, b, n);
+  const typename E::t* q = a.draft && k.down ? draft_row<E>(a, b, n) : nullptr;
+  const int hi = min(a.V, (part + 1) * a.part);
+  double sum[2] = {0.0, 0.0};
+  for (int i = part * a.part + 8 * threadIdx.x; i < hi; i += 8 * kThreads) {
+    if (i + 8 <= hi) {
+      Eight<E> vp, vq;
+      vp.load(p + i);
+      if (q) vq.load(q + i);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[0] += ep.about(vp.at(e));
+      if (q) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[1] += eq.about(vq.at(e));
+      }
+    } else {
+      for (int v = i; v < hi; ++v) {
+        sum[0] += ep.about(E::one(p + v));
+        if (q) sum[1] += eq.about(E::one(q + v));
       }
     }
-    const float acc = l > 0.0 ? 1.f : (float)exp(l);
-    if (lane == 0) {
-      if (write) a.accept[(long long)b * a.T + t] = acc;
-      if (!(a.u[(long long)b * a.T + t] < acc)) atomicMin(&s_first, t);
+  }
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+#pragma unroll
+    for (int j = 32; j >= 1; j >>= 1) sum[c] += __shfl_xor(sum[c], j);
+    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6][c] = sum[c];
+  }
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    double t = 0.0;
+    for (int w = 0; w < kWaves; ++w) t += s_sum[w][threadIdx.x];
+    a.totals[((long long)threadIdx.x * a.B + b) * a.parts + part] = t;
+  }
+}
+
+// the sums of the sampled rows, by each wave in a fixed order (NaN and an empty row end as in the statistics)
+__device__ __forceinline__ void sampled_sums(const VerifyCall& a, int b, const VerifyPick& k, int lane, double& sp,
+                                             double& sq) {
+  sp = k.sp;
+  sq = k.sq;
+  if (!a.totals) return;
+  double t[2] = {0.0, 0.0};
+  for (int i = lane; i < a.parts; i += 64)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) t[c] += a.totals[((long long)c * a.B + b) * a.parts + i];
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int j = 32; j >= 1; j >>= 1) t[c] += __shfl_xor(t[c], j);
+  if (k.mp > -INFINITY) sp = t[0];
+  if (a.draft && k.down && k.mq > -INFINITY) sq = t[1];
+}
+
+// the parts of sum p and, where a token was turned down, of sum max(0, p - q)
+template <class E>
+__global__ __launch_bounds__(kThreads) void k_verify_parts(VerifyCall a) {
+  const int part = blockIdx.x % a.parts, b = blockIdx.x / a.parts;
+  const VerifyPick k = a.picks[b];
+  __shared__ double s_sum[kWaves][2], s_table[32];
+  fill_table(s_table);
+  __syncthreads();
+  double sp, sq;
+  sampled_sums(a, b, k, threadIdx.x & 63, sp, sq);
+  const Rest<E> rest(a, b, a.n_accept[b], k, sp, sq, s_table);
+  const int hi = min(a.V, (part + 1) * a.part);
+  double sum[2] = {0.0, 0.0};
+  for (int i = part * a.part + 8 * threadIdx.x; i < hi; i += 8 * kThreads) {
+    double p[8], w[8];
+    rest.eight(i, a.V, k.down, p, w);   // (a part ends at the row's end or at a whole vector)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      sum[0] += p[e];
+      sum[1] += w[e];
     }
   }
-  if (write)
-    for (int t = len + threadIdx.x; t < a.T; t += kThreads) a.accept[(long long)b * a.T + t] = 0.f;
-  __syncthreads();
-  if (wid == 0) {
-    const int n = s_first;
-    const MaxSum p = row_stats(a, (long long)b * (a.T + 1) + n, a.target_scale, lane);
-    MaxSum q{0.f, 0.f};
-    if (a.draft && n < len) q = row_stats(a, (long long)a.B * (a.T + 1) + (long long)b * a.T + n, a.draft_scale, lane);
-    if (lane == 0) *s_pick = Pick{n, len, ref_of(p.m, a.target_scale), ref_of(q.m, a.draft_scale)};
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+#pragma unroll
+    for (int j = 32; j >= 1; j >>= 1) sum[c] += __shfl_xor(sum[c], j);
+    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6][c] = sum[c];
   }
   __syncthreads();
+  if (threadIdx.x < 2) {
+    double t = 0.0;
+    for (int w = 0; w < kWaves; ++w) t += s_sum[w][threadIdx.x];
+    a.sums[((long long)threadIdx.x * a.B + b) * a.parts + part] = t;
+  }
 }
 
-template <int N>
-__device__ __forceinline__ void block_sum(double (&v)[N], double (*s)[N]) {
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+__device__ __forceinline__ double wave_scan(double v, int lane) {   // inclusive
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-#pragma unroll
-    for (int k = 32; k >= 1; k >>= 1) v[i] += __shfl_xor(v[i], k);
-    if (lane == 0) s[wid][i] = v[i];
+  for (int k = 1; k < 64; k <<= 1) {
+    const double o = __shfl_up(v, k);
+    v += lane >= k ? o : 0.0;
   }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    v[i] = 0.0;
-    for (int w = 0; w < kThreads / 64; ++w) v[i] += s[w][i];
-  }
-}
-
-// e^(scale z - m) of element v of a row
-template <class E>
-__device__ __forceinline__ double mass(const typename E::t* row, int v, float scale, float m) {
-  return exp((double)E::one(row + v) * (double)scale - (double)m);
-}
-
-template <class E>
-__global__ __launch_bounds__(kThreads) void k_verify_pick(VerifyCall a) {
-  const int part = blockIdx.x % a.parts, b = blockIdx.x / a.parts;
-  __shared__ Pick s_pick;
-  __shared__ double s_sum[kThreads / 64][3];
-  decide<E>(a, b, part == 0, &s_pick);
-  const Pick k = s_pick;
-  const bool down = k.n < k.len;
-  if (part == 0) {
-    if (threadIdx.x == 0) a.n_accept[b] = k.n;
-  }
-  const int x = down ? a.token[(long long)b * a.T + k.n] : -1;
-  const typename E::t* p = target_row<E>(a, b, k.n);
-  const typename E::t* q = a.draft && down ? draft_row<E>(a, b, k.n) : nullptr;
-  double v[3] = {0.0, 0.0, 0.0};   // target, draft, target without the drafted token
-  const int hi = min(a.V, (part + 1) * a.part);
-  for (int i = part * a.part + threadIdx.x; i < hi; i += kThreads) {
-    const double e = mass<E>(p, i, a.target_scale, k.mp);
-    v[0] += e;
-    if (q) v[1] += mass<E>(q, i, a.draft_scale, k.mq);
-    v[2] += i == x ? 0.0 : e;
-  }
-  block_sum(v, s_sum);
-  if (threadIdx.x < 3) a.sums[((long long)threadIdx.x * a.B + b) * a.parts + part] = v[threadIdx.x];
-}
-
-// the total over the parts, in a fixed order
-__device__ __forceinline__ double total(const VerifyCall& a, int which, int b) {
-  double t = 0.0;
-  for (int i = 0; i < a.parts; ++i) t += a.sums[((long long)which * a.B + b) * a.parts + i];
-  return t;
-}
-
-struct Row {
-  float mp, mq;
-  double sp, sq;
-};
-// maxima and float64 sums of the rows that sequence b samples from
-template <class E>
-__device__ __forceinline__ Row sampled_row(const VerifyCall& a, int b, int n, bool down) {
-  const int lane = threadIdx.x & 63;
-  Row r;
-  r.mp = ref_of(row_stats(a, (long long)b * (a.T + 1) + n, a.target_scale, lane).m, a.target_scale);
-  r.mq = a.draft && down
-             ? ref_of(row_stats(a, (long long)a.B * (a.T + 1) + (long long)b * a.T + n, a.draft_scale, lane).m, a.draft_scale)
-             : 0.f;
-  r.sp = total(a, 0, b);
-  r.sq = total(a, 1, b);
-  return r;
-}
-
-template <class E>
-__device__ __forceinline__ double rest(const VerifyCall& a, const typename E::t* p, const typename E::t* q, int v,
-                                       const Row& r) {
-  const double w = mass<E>(p, v, a.target_scale, r.mp) / r.sp - mass<E>(q, v, a.draft_scale, r.mq) / r.sq;
-  return w > 0.0 ? w : 0.0;
-}
-
-// the parts of sum max(0, p - q), over the sums of the target without the drafted token
-template <class E>
-__global__ __launch_bounds__(kThreads) void k_verify_rest(VerifyCall a) {
-  const int part = blockIdx.x % a.parts, b = blockIdx.x / a.parts;
-  const int n = a.n_accept[b];
-  if (n >= draft_len(a, b)) return;
-  __shared__ double s_sum[kThreads / 64][1];
-  const Row r = sampled_row<E>(a, b, n, true);
-  const typename E::t *p = target_row<E>(a, b, n), *q = draft_row<E>(a, b, n);
-  double v[1] = {0.0};
-  const int hi = min(a.V, (part + 1) * a.part);
-  for (int i = part * a.part + threadIdx.x; i < hi; i += kThreads) v[0] += rest<E>(a, p, q, i, r);
-  block_sum(v, s_sum);
-  if (threadIdx.x == 0) a.sums[(2LL * a.B + b) * a.parts + part] = v[0];
+  return v;
 }
 
 template <class E>
 __global__ __launch_bounds__(kThreads) void k_verify_token(VerifyCall a) {
-  const int b = blockIdx.x, n = a.n_accept[b];
-  const bool down = n < draft_len(a, b);
-  const int x = down ? a.token[(long long)b * a.T + n] : -1;
-  __shared__ double s_scan[kThreads];
-  __shared__ int s_part, s_token, s_last;
-  __shared__ double s_left;
-  const Row r = sampled_row<E>(a, b, n, down);
-  const double sw = down ? total(a, 2, b) : 0.0;
-  const bool use_rest = down && sw > 0.0;
-  const double all = use_rest ? sw : r.sp;
-  const double* parts = a.sums + ((use_rest ? 2LL : 0LL) * a.B + b) * a.parts;
-  if (threadIdx.x == 0) {
-    // the part in which the running sum passes r of the whole; by rounding alone, the last one that holds anything
+  const int b = blockIdx.x, n = a.n_accept[b], lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  const VerifyPick k = a.picks[b];
+  __shared__ double s_table[32], s_wave[kWaves], s_left;
+  __shared__ int s_part, s_rest, s_token, s_last;
+  fill_table(s_table);
+  if (wid == 0) {
+    // the part in which the running sum passes r of the whole (by rounding alone, the last that holds anything), a
+    // lane having `per` neighbouring parts; of the draft's rest, or where there is none of the target's row
+    const int per = (a.parts + 63) / 64, i0 = min(lane * per, a.parts), i1 = min(i0 + per, a.parts);
+    auto weight = [&](int i, bool rest) { return a.sums[((long long)rest * a.B + b) * a.parts + i]; };
+    bool rest = k.down;
+    double mine = 0.0, all = 0.0;
+    for (int attempt = 0; attempt < 2; ++attempt) {
+      mine = 0.0;
+      for (int i = i0; i < i1; ++i) mine += weight(i, rest);
+      mine = wave_scan(mine, lane);
+      all = __shfl(mine, 63);
+      if (!rest || all > 0.0) break;
+      rest = false;
+    }
     const double at = (double)a.r[b] * all;
-    double before = 0.0;
-    int pick = -1;
-    s_left = 0.0;
+    double before = __shfl_up(mine, 1);
+    if (lane == 0) before = 0.0;
+    int pick = INT_MAX, last = -1;
+    double pick_before = 0.0, last_before = 0.0;
     if (all > 0.0 && all <= 1.7976931348623157e308)
-      for (int i = 0; i < a.parts; ++i) {
-        if (parts[i] > 0.0) {
-          pick = i;
-          s_left = at - before;
-          if (before + parts[i] > at) break;
+      for (int i = i0; i < i1; ++i) {
+        const double w = weight(i, rest);
+        if (w > 0.0) {
+          last = i;
+          last_before = before;
+          if (pick == INT_MAX && before + w > at) {
+            pick = i;
+            pick_before = before;
+          }
         }
-        before += parts[i];
+        before += w;
       }
-    s_part = pick;
-    s_token = INT_MAX;
-    s_last = -1;
+    // the first lane that has one, else the last part that holds anything
+    const unsigned long long hit = __ballot(pick != INT_MAX), any = __ballot(last >= 0);
+    const int from = hit ? __builtin_ctzll(hit) : any ? 63 - __builtin_clzll(any) : 0;
+    const int part = __shfl(hit ? pick : last, from);
+    const double pb = __shfl(hit ? pick_before : last_before, from);
+    if (lane == 0) {
+      s_part = part;
+      s_rest = rest;
+      s_left = at - pb;
+      s_token = INT_MAX;
+      s_last = -1;
+    }
   }
   __syncthreads();
   const int part = s_part;
   if (part >= 0) {
-    const typename E::t* p = target_row<E>(a, b, n);
-    const typename E::t* q = a.draft && down ? draft_row<E>(a, b, n) : nullptr;
-    auto weight = [&](int v) -> double {
-      if (!use_rest) return mass<E>(p, v, a.target_scale, r.mp);
-      if (q) return rest<E>(a, p, q, v, r);
-      return v == x ? 0.0 : mass<E>(p, v, a.target_scale, r.mp);
-    };
-    const int each = a.part / kThreads, lo = part * a.part + threadIdx.x * each, hi = min(a.V, lo + each);
-    double mine = 0.0;
+    // the same inside the part, 2048 entries at a time
+    const bool use_rest = s_rest;
+    double sp, sq;
+    sampled_sums(a, b, k, lane, sp, sq);
+    const Rest<E> rest(a, b, n, k, sp, sq, s_table);
+    const double left = s_left;
+    const int hi = min(a.V, (part + 1) * a.part);
+    double done = 0.0;
     int last = -1;
-    for (int v = lo; v < hi; ++v) {
-      const double w = weight(v);
-      mine += w;
-      last = w > 0.0 ? v : last;
-    }
-    s_scan[threadIdx.x] = mine;
-    if (last >= 0) atomicMax(&s_last, last);
-    __syncthreads();
-    double before = 0.0;
-    for (int i = 0; i < (int)threadIdx.x; ++i) before += s_scan[i];
-    if (before + mine > s_left) {
-      double run = before;
-      for (int v = lo; v < hi; ++v) {
-        const double w = weight(v);
-        run += w;
-        if (w > 0.0 && run > s_left) {
-          atomicMin(&s_token, v);
-          break;
-        }
+    for (int i0 = part * a.part; i0 < hi; i0 += 8 * kThreads) {
+      const int i = i0 + 8 * threadIdx.x;
+      double p8[8], w[8], mine = 0.0;
+      int hit = -1;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p8[e] = w[e] = 0.0;
+      if (i < hi) rest.eight(i, a.V, use_rest, p8, w);
+      if (!use_rest) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = p8[e];
       }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        last = w[e] > 0.0 ? i + e : last;
+        mine += w[e];
+      }
+      const double scan = wave_scan(mine, lane);
+      if (lane == 63) s_wave[wid] = scan;
+      __syncthreads();
+      double before = done + (scan - mine);
+      for (int v = 0; v < kWaves; ++v) {
+        before += v < wid ? s_wave[v] : 0.0;
+        done += s_wave[v];
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        before += w[e];
+        hit = hit < 0 && w[e] > 0.0 && before > left ? i + e : hit;
+      }
+      // the first lane's (a wave's lanes hold neighbouring entries), then the first wave's
+      const unsigned long long hits = __ballot(hit >= 0);
+      if (hits && lane == __builtin_ctzll(hits)) atomicMin(&s_token, hit);
+      __syncthreads();
+      if (s_token != INT_MAX) break;
+      __syncthreads();
     }
-    __syncthreads();
+    if (s_token == INT_MAX) {   // by rounding alone
+#pragma unroll
+      for (int j = 32; j >= 1; j >>= 1) last = max(last, __shfl_xor(last, j));
+      if (lane == 0) atomicMax(&s_last, last);
+      __syncthreads();
+    }
   }
   const int token = part < 0 ? -1 : s_token == INT_MAX ? s_last : s_token;
   for (int t = threadIdx.x; t <= a.T; t += kThreads)
@@ -336,10 +530,9 @@ __global__ __launch_bounds__(64) void k_verify_greedy(VerifyCall a) {
     float m = -INFINITY;
     int idx = INT_MAX;
     for (int i = lane; i < a.splits; i += 64) {
-      const float2 v = a.stats[((long long)b * (a.T + 1) + t) * a.splits + i];
-      const int oi = __float_as_int(v.y);
-      idx = v.x > m ? oi : v.x < m ? idx : min(idx, oi);
-      m = fmaxf(m, v.x);
+      const RowPart v = a.stats[((long long)b * (a.T + 1) + t) * a.splits + i];
+      idx = v.m > m ? v.idx : v.m < m ? idx : min(idx, v.idx);
+      m = fmaxf(m, v.m);
     }
 #pragma unroll
     for (int k = 32; k >= 1; k >>= 1) {
@@ -367,18 +560,25 @@ template <class E>
 hipError_t verify(const VerifyCall& a, hipStream_t s) {
   hipError_t e;
   const long long rows = (long long)a.B * (a.T + 1) + (a.draft && !a.greedy ? (long long)a.B * a.T : 0);
-  k_verify_stats<E><<<(unsigned)(rows * a.splits), kThreads, 0, s>>>(a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
   if (a.greedy) {
+    k_verify_stats<E, kGreedy><<<(unsigned)(rows * a.splits), kThreads, 0, s>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
     k_verify_greedy<<<a.B, 64, 0, s>>>(a);
     return hipGetLastError();
   }
-  k_verify_pick<E><<<(unsigned)(a.B * a.parts), kThreads, 0, s>>>(a);
+  if (a.totals)
+    k_verify_stats<E, kSingle><<<(unsigned)(rows * a.splits), kThreads, 0, s>>>(a);
+  else
+    k_verify_stats<E, kDouble><<<(unsigned)(rows * a.splits), kThreads, 0, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (a.draft && a.T > 0) {
-    k_verify_rest<E><<<(unsigned)(a.B * a.parts), kThreads, 0, s>>>(a);
+  k_verify_decide<E><<<a.B, kDecideWaves * 64, 0, s>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (a.totals) {
+    k_verify_totals<E><<<(unsigned)(a.B * a.parts), kThreads, 0, s>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
+  k_verify_parts<E><<<(unsigned)(a.B * a.parts), kThreads, 0, s>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
   k_verify_token<E><<<a.B, kThreads, 0, s>>>(a);
   return hipGetLastError();
 }

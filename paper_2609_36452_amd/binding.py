@@ -568,13 +568,13 @@ def _row_stride(r: torch.Tensor) -> int:
     return r.stride(0) if r.shape[0] > 1 else max(r.shape[1], 1)
 
 
-def _enqueue(device: torch.device, stream, call) -> None:
-    """call(stream handle) with ``device`` current, on ``stream`` or that device's current stream."""
-    if device.index == torch.cuda.current_device():
-        _check(call((torch.cuda.current_stream() if stream is None else stream).cuda_stream or None))
-        return
-    with torch.cuda.device(device):
-        _check(call((torch.cuda.current_stream() if stream is None else stream).cuda_stream or None))
+def _enqueue(device: torch.device, stream, entry, *args) -> None:
+    """entry(*args, stream handle) with ``device`` current, on ``stream`` or that device's current stream."""
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _enqueue(device, stream, entry, *args)
+    handle = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+    _check(entry(*args, handle or None))
 
 
 class QuantHead:
@@ -604,9 +604,8 @@ class QuantHead:
         # an invalid head has size 0, and the call below says what is wrong with it
         self.packed = torch.empty(max(int(lib().rpd_quant_packed_size(ctypes.byref(self.head))), 1),
                                   dtype=torch.uint8, device=self.device)
-        _enqueue(self.device, None, lambda s: lib().rpd_quant_pack(
-            ctypes.byref(self.head), codes.data_ptr(), scales.data_ptr(), _ptr(zeros), self.packed.data_ptr(),
-            self.packed.numel(), s))
+        _enqueue(self.device, None, lib().rpd_quant_pack, ctypes.byref(self.head), codes.data_ptr(),
+                 scales.data_ptr(), _ptr(zeros), self.packed.data_ptr(), self.packed.numel())
 
     def _x(self, x: torch.Tensor) -> torch.Tensor:
         _one_device("x", x, packed=self.packed)
@@ -635,9 +634,9 @@ class QuantHead:
         o = _rows("out", out)
         code = _float_code("out", out)
         ws = self._workspace(r.shape[0], 0, stream)
-        _enqueue(x.device, stream, lambda s: lib().rpd_quant_project(
-            ctypes.byref(self.head), self.packed.data_ptr(), r.shape[0], r.data_ptr(), _row_stride(r), o.data_ptr(),
-            _row_stride(o), code, None, None, None, 1.0, ws.data_ptr(), ws.numel(), s))
+        _enqueue(x.device, stream, lib().rpd_quant_project, ctypes.byref(self.head), self.packed.data_ptr(),
+                 r.shape[0], r.data_ptr(), _row_stride(r), o.data_ptr(), _row_stride(o), code, None, None, None, 1.0,
+                 ws.data_ptr(), ws.numel())
         return out
 
     def stats(self, x: torch.Tensor, logit_scale: float = 1.0, stream=None) -> dict:
@@ -649,10 +648,9 @@ class QuantHead:
              "confidence": torch.empty(x.shape[:-1], dtype=torch.float32, **e),
              "entropy": torch.empty(x.shape[:-1], dtype=torch.float32, **e)}
         ws = self._workspace(r.shape[0], 1, stream)
-        _enqueue(x.device, stream, lambda s: lib().rpd_quant_project(
-            ctypes.byref(self.head), self.packed.data_ptr(), r.shape[0], r.data_ptr(), _row_stride(r), None, 0, 0,
-            o["argmax"].data_ptr(), o["confidence"].data_ptr(), o["entropy"].data_ptr(), float(logit_scale),
-            ws.data_ptr(), ws.numel(), s))
+        _enqueue(x.device, stream, lib().rpd_quant_project, ctypes.byref(self.head), self.packed.data_ptr(),
+                 r.shape[0], r.data_ptr(), _row_stride(r), None, 0, 0, o["argmax"].data_ptr(),
+                 o["confidence"].data_ptr(), o["entropy"].data_ptr(), float(logit_scale), ws.data_ptr(), ws.numel())
         return o
 
 
@@ -708,8 +706,8 @@ class VerifyDraft:
 
     def __call__(self, stream=None) -> dict:
         """Enqueue one call."""
-        _enqueue(self.device, stream, lambda s: lib().rpd_verify_draft(
-            ctypes.byref(self.problem), self.workspace.data_ptr(), self.workspace.numel(), s))
+        _enqueue(self.device, stream, lib().rpd_verify_draft, ctypes.byref(self.problem),
+                 self.workspace.data_ptr(), self.workspace.numel())
         return self.out
 
 
@@ -725,8 +723,8 @@ def verify_draft(target_logits: torch.Tensor, draft_token: torch.Tensor, u: torc
     return call(stream)
 
 
-def _distill_problem(logits, teacher_id, teacher_logit, teacher_lse, weight, logit_scale):
-    """The problem of [..., V] logits without its outputs, and the rows of the logits."""
+def _distill_problem(logits, teacher_id, teacher_logit, teacher_lse, weight, logit_scale) -> RpdDistill:
+    """The problem of [..., V] logits without its outputs."""
     _one_device("logits", logits, teacher_id=teacher_id, teacher_logit=teacher_logit, teacher_lse=teacher_lse,
                 weight=weight)
     code = _float_code("logits", logits)
@@ -739,20 +737,20 @@ def _distill_problem(logits, teacher_id, teacher_logit, teacher_lse, weight, log
             _check_dev(name, t, lead, (torch.float32,))
     return RpdDistill(r.shape[0], r.shape[1], k, code, _FLOAT_CODES[teacher_logit.dtype], r.data_ptr(),
                       _row_stride(r), teacher_id.data_ptr(), teacher_logit.data_ptr(), _ptr(teacher_lse),
-                      _ptr(weight), None, float(logit_scale), None, None, None, 0), r
+                      _ptr(weight), None, float(logit_scale), None, None, None, 0)
 
 
 def _distill_loss(p: RpdDistill, logits: torch.Tensor, stream) -> tuple[torch.Tensor, torch.Tensor]:
+    """The loss, and the buffer that begins with the rows' state (then the workspace)."""
     loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
-    state = torch.empty((p.N, DISTILL_STATE), dtype=torch.float32, device=logits.device)
-    p.loss, p.state = loss.data_ptr(), state.data_ptr()
-    ws = torch.empty(int(lib().rpd_distill_workspace_size(ctypes.byref(p))), dtype=torch.uint8, device=logits.device)
+    at = -(-p.N * DISTILL_STATE * 4 // 256) * 256
+    nbytes = int(lib().rpd_distill_workspace_size(ctypes.byref(p)))
+    buf = torch.empty(at + nbytes, dtype=torch.uint8, device=logits.device)
     if stream is not None:
-        ws.record_stream(stream)
-        state.record_stream(stream)
-    _enqueue(logits.device, stream,
-             lambda s: lib().rpd_distill_loss(ctypes.byref(p), ws.data_ptr(), ws.numel(), s))
-    return loss, state
+        buf.record_stream(stream)
+    p.loss, p.state = loss.data_ptr(), buf.data_ptr()
+    _enqueue(logits.device, stream, lib().rpd_distill_loss, ctypes.byref(p), (p.state or 0) + at, nbytes)
+    return loss, buf
 
 
 def _grad_like(logits: torch.Tensor, p: RpdDistill) -> torch.Tensor:
@@ -764,21 +762,26 @@ def _grad_like(logits: torch.Tensor, p: RpdDistill) -> torch.Tensor:
 class _Distill(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, teacher_id, teacher_logit, teacher_lse, weight, logit_scale):
-        p, _ = _distill_problem(logits, teacher_id, teacher_logit, teacher_lse, weight, logit_scale)
+        p = _distill_problem(logits, teacher_id, teacher_logit, teacher_lse, weight, logit_scale)
         loss, state = _distill_loss(p, logits, None)
         ctx.save_for_backward(logits, teacher_id, teacher_logit, teacher_lse, weight, state)
-        ctx.logit_scale = logit_scale
+        ctx.problem = p
         return loss
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad_loss):
-        logits, teacher_id, teacher_logit, teacher_lse, weight, state = ctx.saved_tensors
-        p, _ = _distill_problem(logits, teacher_id, teacher_logit, teacher_lse, weight, ctx.logit_scale)
+        *inputs, state = ctx.saved_tensors
+        p = ctx.problem
+        if [_ptr(t) for t in inputs] == [p.logits, p.id, p.teacher, p.teacher_lse, p.weight]:
+            p = RpdDistill.from_buffer_copy(p)
+        else:   # the saved tensors were moved meanwhile
+            p = _distill_problem(*inputs, p.logit_scale)
+        logits = inputs[0]
         grad = _grad_like(logits, p)
         up = grad_loss.to(torch.float32).contiguous()   # a broadcast upstream gradient has stride 0
-        p.grad_loss, p.state = up.data_ptr(), state.data_ptr()
-        _enqueue(logits.device, None, lambda s: lib().rpd_distill_grad(ctypes.byref(p), s))
+        p.grad_loss, p.state, p.loss = up.data_ptr(), state.data_ptr(), None
+        _enqueue(logits.device, None, lib().rpd_distill_grad, ctypes.byref(p))
         return grad, None, None, None, None, None
 
 
@@ -801,7 +804,7 @@ def distill_grad(logits: torch.Tensor, teacher_id: torch.Tensor, teacher_logit: 
     """Loss and gradient in one call, for a training step that knows the upstream gradient ``grad_loss`` (float32
     [...], 1 if None) beforehand: (loss [...], gradient [..., V] of ``logits``'s type). Not recorded by autograd."""
     logits = logits.detach()
-    p, _ = _distill_problem(logits, teacher_id, teacher_logit, teacher_lse, weight, logit_scale)
+    p = _distill_problem(logits, teacher_id, teacher_logit, teacher_lse, weight, logit_scale)
     if grad_loss is not None:
         _one_device("logits", logits, grad_loss=grad_loss)
         _check_dev("grad_loss", grad_loss, tuple(logits.shape[:-1]), (torch.float32,))

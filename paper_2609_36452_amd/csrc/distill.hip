@@ -24,6 +24,7 @@ namespace rpd {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kHeld = 4;   // vectors that a thread holds
 constexpr int kMaxList = RPD_DISTILL_MAX_K;
 
 // a row's state between the loss and the gradient
@@ -45,48 +46,100 @@ __device__ __forceinline__ float teacher_at(const DistillCall& a, long long i) {
 
 __device__ __forceinline__ bool skipped(const DistillCall& a, int n) { return a.weight && a.weight[n] == 0.f; }
 
+template <class E>
+__device__ __forceinline__ const typename E::t* row_of(const DistillCall& a, int n) {
+  return static_cast<const typename E::t*>(a.logits) + n * a.stride;
+}
+
+// the row's list into LDS; with `marks` (a bit per entry of [lo, hi)), those in it marked. Ends with a barrier.
+__device__ __forceinline__ void load_list(const DistillCall& a, int n, int* s_ids, uint32_t* s_mark, int lo, int hi) {
+  if (s_mark)
+    for (int i = threadIdx.x; i < (hi - lo + 31) / 32; i += blockDim.x) s_mark[i] = 0;
+  for (int j = threadIdx.x; j < a.k; j += blockDim.x) s_ids[j] = a.ids[(long long)n * a.k + j];
+  __syncthreads();
+  if (!s_mark) return;
+  for (int j = threadIdx.x; j < a.k; j += blockDim.x) {
+    const int v = s_ids[j];
+    if (v >= lo && v < hi) atomicOr(&s_mark[(v - lo) >> 5], 1u << ((v - lo) & 31));
+  }
+  __syncthreads();
+}
+
+// 8 entries of a row from i on, -inf past `hi`
+template <class E>
+__device__ __forceinline__ void load_eight(const typename E::t* p, int i, int hi, Eight<E>& v) {
+  if (i + 8 <= hi) {
+    v.load(p + i);
+  } else {
+    float z[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = i + e < hi ? E::one(p + i + e) : -INFINITY;
+    v.set(z);
+  }
+}
+
 // maximum and mass of the entries of a part of a row outside the list
 template <class E>
 __global__ __launch_bounds__(kThreads) void k_distill_part(DistillCall a) {
   const int n = blockIdx.x / a.splits, split = blockIdx.x - n * a.splits;
   if (skipped(a, n)) return;
   extern __shared__ uint32_t s_mark[];   // a bit per entry of the part
-  __shared__ float2 s_part[kThreads / 64];
+  __shared__ int s_ids[kMaxList];
+  __shared__ float s_max[kThreads / 64], s_sum[kThreads / 64];
   const int lo = split * a.chunk, hi = min(a.V, lo + a.chunk);
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-  for (int i = threadIdx.x; i < (a.chunk + 31) / 32; i += kThreads) s_mark[i] = 0;
-  __syncthreads();
-  for (int j = threadIdx.x; j < a.k; j += kThreads) {
-    const int v = a.ids[(long long)n * a.k + j];
-    if (v >= lo && v < hi) atomicOr(&s_mark[(v - lo) >> 5], 1u << ((v - lo) & 31));
-  }
-  __syncthreads();
-  const typename E::t* p = static_cast<const typename E::t*>(a.logits) + n * a.stride;
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, first = lo + 8 * threadIdx.x;
+  const typename E::t* p = row_of<E>(a, n);
+  // (a part is at most kHeld vectors a thread, or read in rounds of as many)
   MaxSum s{-INFINITY, 0.f};
-  for (int i = lo + 8 * threadIdx.x; i < hi; i += 8 * kThreads) {
-    float z[8];
-    if (i + 8 <= hi) {
-      Eight<E> v;
-      v.load(p + i);
+  bool listed = false;
+  for (int base = first; base - 8 * (int)threadIdx.x < hi; base += kHeld * 8 * kThreads) {
+    Eight<E> held[kHeld];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = v.at(e);
-    } else {
+    for (int j = 0; j < kHeld; ++j)
+      if (base + j * 8 * kThreads < hi) load_eight<E>(p, base + j * 8 * kThreads, hi, held[j]);
+    if (!listed) load_list(a, n, s_ids, s_mark, lo, hi);
+    listed = true;
+    // the list's entries out, then one maximum and one sum over all that are held
+    float m = s.m;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = i + e < hi ? E::one(p + i + e) : -INFINITY;
+    for (int j = 0; j < kHeld; ++j) {
+      const int i = base + j * 8 * kThreads;
+      if (i >= hi) continue;
+      const uint32_t mark = s_mark[(i - lo) >> 5] >> ((i - lo) & 31) & 255u;
+      if (mark) {
+        float z[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = mark >> e & 1u ? -INFINITY : held[j].at(e);
+        held[j].set(z);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m = fmaxf(m, held[j].at(e));
     }
-    const uint32_t mark = s_mark[(i - lo) >> 5] >> ((i - lo) & 31) & 255u;
-    if (mark) {
+    const float ref = ref_of(m, a.scale);
+    s.S *= carry(s.m, ref, a.scale);
+    s.m = m;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = mark >> e & 1u ? -INFINITY : z[e];
+    for (int j = 0; j < kHeld; ++j) {
+      if (base + j * 8 * kThreads >= hi) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s.S += __expf(fmaf(held[j].at(e), a.scale, -ref));
     }
-    maxsum_push(s, z, a.scale);
   }
-  s = wave_maxsum(s, a.scale);
-  if (lane == 0) s_part[wid] = make_float2(s.m, s.S);
+  float m = s.m;
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+  if (lane == 0) s_max[wid] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) m = fmaxf(m, s_max[w]);
+  float S = s.S * carry(s.m, ref_of(m, a.scale), a.scale);
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) S += __shfl_xor(S, k);
+  if (lane == 0) s_sum[wid] = S;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < kThreads / 64; ++w) s = maxsum_merge(s, MaxSum{s_part[w].x, s_part[w].y}, a.scale);
-    a.partials[(long long)n * a.splits + split] = make_float2(s.m, s.S);
+    for (int w = 1; w < kThreads / 64; ++w) S += s_sum[w];
+    a.partials[(long long)n * a.splits + split] = make_float2(m, S);
   }
 }
 
@@ -100,32 +153,40 @@ __device__ __forceinline__ void wave_sum(double (&v)[N]) {
 
 // The row's loss and state from the maximum and mass of its entries outside the list; one wave.
 template <class E>
-__device__ __forceinline__ void row_loss(const DistillCall& a, int n, MaxSum s, int lane) {
+__device__ __forceinline__ void row_loss(const DistillCall& a, int n, MaxSum s, const int* s_ids, int lane) {
   constexpr int kEach = kMaxList / 64;
-  const typename E::t* p = static_cast<const typename E::t*>(a.logits) + n * a.stride;
-  const int32_t* ids = a.ids + (long long)n * a.k;
-  double t[kEach], z[kEach];
+  const typename E::t* p = row_of<E>(a, n);
+  double t[kEach], z[kEach], pj[kEach];
+  int at[kEach];
   bool ok[kEach], first[kEach];
   double tmax = -INFINITY, sums[2] = {0.0, 0.0};   // teacher's, student's mass in the list
   float top = s.m;
 #pragma unroll
   for (int u = 0; u < kEach; ++u) {
     const int j = lane + 64 * u;
-    const int v = j < a.k ? ids[j] : -1;
+    const int v = j < a.k ? s_ids[j] : -1;
+    at[u] = v;
     ok[u] = v >= 0 && v < a.V;
     t[u] = ok[u] ? (double)teacher_at(a, (long long)n * a.k + j) * (double)a.scale : -INFINITY;
     const float zj = ok[u] ? E::one(p + v) : -INFINITY;
     z[u] = (double)zj * (double)a.scale;
     tmax = fmax(tmax, t[u]);
     top = fmaxf(top, zj);
-    first[u] = ok[u];   // a token listed twice is in the list once
-    for (int i = 0; i < j && first[u]; ++i) first[u] = ids[i] != v;
+    first[u] = ok[u];
+  }
+  // a token listed twice is in the list once
+#pragma unroll 4
+  for (int i = 0; i < a.k; ++i) {
+    const int v = s_ids[i];
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) first[u] &= !(i < lane + 64 * u && v == at[u]);
   }
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
   const float ref = ref_of(top, a.scale), tail = ref_of(s.m, a.scale);
 #pragma unroll
   for (int u = 0; u < kEach; ++u) {
+    if (64 * u >= a.k) continue;
     z[u] -= (double)ref;
     if (first[u]) sums[1] += exp(z[u]);
   }
@@ -133,8 +194,13 @@ __device__ __forceinline__ void row_loss(const DistillCall& a, int n, MaxSum s, 
   for (int k = 32; k >= 1; k >>= 1) tmax = fmax(tmax, __shfl_xor(tmax, k));
   const float tref = a.lse ? a.lse[n] : (float)(tmax == -INFINITY ? 0.0 : tmax);
 #pragma unroll
-  for (int u = 0; u < kEach; ++u)
-    if (ok[u]) sums[0] += exp(t[u] - (double)tref);
+  for (int u = 0; u < kEach; ++u) {
+    pj[u] = 0.0;
+    if (64 * u >= a.k) continue;
+    t[u] -= (double)tref;
+    if (ok[u]) pj[u] = exp(t[u]);
+    sums[0] += pj[u];
+  }
   wave_sum(sums);
   // a list without any mass: in list mode there is no teacher, and no loss
   const bool none = !a.lse && sums[0] == 0.0;
@@ -143,11 +209,10 @@ __device__ __forceinline__ void row_loss(const DistillCall& a, int n, MaxSum s, 
   const double drop = s.S == 0.f ? 0.0 : (double)tail - (double)ref;   // S_T's exponent in units of S's
   const double S = (double)s.S * exp(drop) + sums[1], ln_S = log(S);
   double l[1] = {0.0};
+  const double ln_tinv = a.lse ? 0.0 : log(tinv);
 #pragma unroll
-  for (int u = 0; u < kEach; ++u) {
-    const double pj = ok[u] ? exp(t[u] - (double)tref) * tinv : 0.0;
-    if (pj != 0.0) l[0] += pj * ((t[u] - (double)tref + (a.lse ? 0.0 : log(tinv))) - (z[u] - ln_S));
-  }
+  for (int u = 0; u < kEach; ++u)
+    if (pj[u] != 0.0) l[0] += pj[u] * tinv * ((t[u] + ln_tinv) - (z[u] - ln_S));
   wave_sum(l);
   if (lane != 0) return;
   if (rest > 0.0) l[0] += rest * (log(rest) - (log((double)s.S) + drop - ln_S));
@@ -174,65 +239,102 @@ __global__ __launch_bounds__(64) void k_distill_loss(DistillCall a) {
     }
     return;
   }
-  MaxSum s{-INFINITY, 0.f};
+  __shared__ int s_ids[kMaxList];
+  load_list(a, n, s_ids, nullptr, 0, 0);
+  float m = -INFINITY, S = 0.f;
+  for (int i = lane; i < a.splits; i += 64) m = fmaxf(m, a.partials[(long long)n * a.splits + i].x);
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+  const float ref = ref_of(m, a.scale);
   for (int i = lane; i < a.splits; i += 64) {
     const float2 v = a.partials[(long long)n * a.splits + i];
-    s = maxsum_merge(s, MaxSum{v.x, v.y}, a.scale);
+    S += v.y * carry(v.x, ref, a.scale);
   }
-  row_loss<E>(a, n, wave_maxsum(s, a.scale), lane);
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) S += __shfl_xor(S, k);
+  row_loss<E>(a, n, MaxSum{m, S}, s_ids, lane);
 }
 
-// The part [lo, hi) of a row's gradient: the formula of the entries outside the
-// list everywhere, then those in the list over it.
+// The part [lo, hi) of a row's gradient: the formula of the entries outside the list everywhere, then those in the
+// list over it. Streamed past the caches, which keep the logits between the loss and the gradient (1024 rows of
+// 126464 bf16, three quarters of them read: 50 us for the sums and 75 here, 64 and 77 with ordinary stores).
 template <class E>
-__global__ __launch_bounds__(kThreads) void k_distill_grad(DistillCall a) {
+__device__ __forceinline__ void row_grad(const DistillCall& a, int n, int lo, int hi, const RowState& st,
+                                         const int* s_ids) {
   typedef typename E::t T;
-  const int n = blockIdx.x / a.splits, split = blockIdx.x - n * a.splits;
-  const int lo = split * a.chunk, hi = min(a.V, lo + a.chunk);
-  const T* p = static_cast<const T*>(a.logits) + n * a.stride;
+  const T* p = row_of<E>(a, n);
   T* g = static_cast<T*>(a.grad) + n * a.grad_stride;
-  const RowState st = *reinterpret_cast<const RowState*>(a.state + (long long)n * RPD_DISTILL_STATE);
-  const float c = (a.weight ? a.weight[n] : 1.f) * (a.up ? a.up[n] : 1.f) * a.scale;
-  const bool zero = skipped(a, n) || st.any == 0.f;   // such a row is not read
-  const float co = c * st.out;
-  for (int i = lo + 8 * threadIdx.x; i < hi; i += 8 * kThreads) {
-    if (i + 8 <= hi) {
-      float d[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      Eight<E> v;
-      if (!zero) {
-        v.load(p + i);
+  const float c = (a.weight ? a.weight[n] : 1.f) * (a.up ? a.up[n] : 1.f) * a.scale, co = c * st.out;
+  const int first = lo + 8 * threadIdx.x;
+  for (int base = first; base < hi; base += kHeld * 8 * kThreads) {
+    Eight<E> held[kHeld];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] = co * __expf(fmaf(v.at(e), a.scale, -st.tail));
+    for (int j = 0; j < kHeld; ++j)
+      if (base + j * 8 * kThreads < hi) load_eight<E>(p, base + j * 8 * kThreads, hi, held[j]);
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+      const int i = base + j * 8 * kThreads;
+      if (i >= hi) continue;
+      float d[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d[e] = co * __expf(fmaf(held[j].at(e), a.scale, -st.tail));
+      if (i + 8 <= hi) {
+        held[j].set(d);
+        held[j].stream(g + i);
+      } else {
+        for (int e = 0; e < hi - i; ++e) g[i + e] = E::to(d[e]);
       }
-      v.set(d);
-      v.store(g + i);
-    } else {
-      for (int v = i; v < hi; ++v) g[v] = E::to(zero ? 0.f : co * __expf(fmaf(E::one(p + v), a.scale, -st.tail)));
     }
   }
-  if (zero) return;
   __syncthreads();
-  const int32_t* ids = a.ids + (long long)n * a.k;
   for (int j = threadIdx.x; j < a.k; j += kThreads) {
-    const int v = ids[j];
+    const int v = s_ids[j];
     if (v < lo || v >= hi) continue;
     double pv = 0.0;
-    bool first = true;
+    bool first_of = true;
     for (int i = 0; i < a.k; ++i)
-      if (ids[i] == v) {
-        first &= i >= j;
+      if (s_ids[i] == v) {
+        first_of &= i >= j;
         pv += exp((double)teacher_at(a, (long long)n * a.k + i) * (double)a.scale - (double)st.tref);
       }
-    if (first) g[v] = E::to(c * (st.in * __expf(fmaf(E::one(p + v), a.scale, -st.ref)) - (float)(pv * (double)st.tinv)));
+    if (first_of)
+      g[v] = E::to(c * (st.in * __expf(fmaf(E::one(p + v), a.scale, -st.ref)) - (float)(pv * (double)st.tinv)));
   }
+}
+template <class E>
+__device__ __forceinline__ void row_zero(const DistillCall& a, int n, int lo, int hi) {
+  typedef typename E::t T;
+  T* g = static_cast<T*>(a.grad) + n * a.grad_stride;
+  const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  Eight<E> v;
+  v.set(none);
+  for (int i = lo + 8 * threadIdx.x; i < hi; i += 8 * kThreads) {
+    if (i + 8 <= hi)
+      v.stream(g + i);
+    else
+      for (int e = i; e < hi; ++e) g[e] = E::to(0.f);
+  }
+}
+
+template <class E>
+__global__ __launch_bounds__(kThreads) void k_distill_grad(DistillCall a) {
+  const int n = blockIdx.x / a.splits, split = blockIdx.x - n * a.splits;
+  const int lo = split * a.chunk, hi = min(a.V, lo + a.chunk);
+  __shared__ int s_ids[kMaxList];
+  const RowState st = *reinterpret_cast<const RowState*>(a.state + (long long)n * RPD_DISTILL_STATE);
+  if (skipped(a, n) || st.any == 0.f) return row_zero<E>(a, n, lo, hi);   // such a row is not read
+  load_list(a, n, s_ids, nullptr, 0, 0);
+  row_grad<E>(a, n, lo, hi, st, s_ids);
 }
 
 template <class E>
 hipError_t loss_t(const DistillCall& a, hipStream_t s) {
+  hipError_t e;
   k_distill_part<E><<<(unsigned)((long long)a.N * a.splits), kThreads, (size_t)(a.chunk + 31) / 32 * 4, s>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if ((e = hipGetLastError()) != hipSuccess) return e;
   k_distill_loss<E><<<a.N, 64, 0, s>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess || !a.grad) return e;
+  k_distill_grad<E><<<(unsigned)((long long)a.N * a.splits), kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 

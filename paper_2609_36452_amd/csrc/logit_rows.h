@@ -44,7 +44,10 @@ template <class E>
 struct Eight {
   u32x4 v;
   __device__ __forceinline__ void load(const typename E::t* p) { v = reinterpret_cast<const Any16*>(p)->v; }
-  __device__ __forceinline__ void store(typename E::t* p) const { reinterpret_cast<Any16*>(p)->v = v; }
+  // past the caches
+  __device__ __forceinline__ void stream(typename E::t* p) const {
+    __builtin_nontemporal_store(v, &reinterpret_cast<Any16*>(p)->v);
+  }
   __device__ __forceinline__ float at(int e) const;
   __device__ __forceinline__ void set(const float (&z)[8]) {
 #pragma unroll
@@ -68,9 +71,9 @@ struct Eight<F32> {
     a = reinterpret_cast<const Any32*>(p)->a;
     b = reinterpret_cast<const Any32*>(p)->b;
   }
-  __device__ __forceinline__ void store(float* p) const {
-    reinterpret_cast<Any32*>(p)->a = a;
-    reinterpret_cast<Any32*>(p)->b = b;
+  __device__ __forceinline__ void stream(float* p) const {
+    __builtin_nontemporal_store(a, &reinterpret_cast<Any32*>(p)->a);
+    __builtin_nontemporal_store(b, &reinterpret_cast<Any32*>(p)->b);
   }
   __device__ __forceinline__ float at(int e) const { return __uint_as_float(e < 4 ? a[e & 3] : b[e & 3]); }
   __device__ __forceinline__ void set(const float (&z)[8]) {
@@ -98,27 +101,6 @@ __device__ __forceinline__ float ref_of(float m, float scale) {
 // what a sum relative to m is worth relative to r (0 while nothing was seen, whatever r: rows far below 0)
 __device__ __forceinline__ float carry(float m, float r, float scale) {
   return m == -INFINITY ? 0.f : __expf(ref_of(m, scale) - r);
-}
-__device__ __forceinline__ MaxSum maxsum_merge(MaxSum a, MaxSum b, float scale) {
-  const float m = fmaxf(a.m, b.m), r = ref_of(m, scale);
-  return MaxSum{m, a.S * carry(a.m, r, scale) + b.S * carry(b.m, r, scale)};
-}
-template <int N>
-__device__ __forceinline__ void maxsum_push(MaxSum& s, const float (&z)[N], float scale) {
-  float m = s.m;
-#pragma unroll
-  for (int e = 0; e < N; ++e) m = fmaxf(m, z[e]);
-  const float r = ref_of(m, scale);
-  float S = s.S * carry(s.m, r, scale);
-#pragma unroll
-  for (int e = 0; e < N; ++e) S += __expf(fmaf(z[e], scale, -r));
-  s.m = m;
-  s.S = S;
-}
-__device__ __forceinline__ MaxSum wave_maxsum(MaxSum s, float scale) {
-#pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) s = maxsum_merge(s, MaxSum{__shfl_xor(s.m, k), __shfl_xor(s.S, k)}, scale);
-  return s;
 }
 
 }  // namespace

@@ -9,9 +9,6 @@
 using rpd::fail;
 using rpd::round256;
 
-#ifndef SINGLE
-#define SINGLE 12000000
-#endif
 namespace {
 
 constexpr long long kMaxBlocks = (1LL << 24) - 1;   // workgroups of 256 threads: a launch holds fewer than 2^32 threads
@@ -109,7 +106,7 @@ bool verify_shape_ok(const rpd_verify* p) {
 constexpr long long kFill = 4096;   // workgroups of 256 threads: 256 CUs, 8 on each, twice
 
 // logits from which float32 statistics and a pass of float64 sums over the sampled rows beat float64 statistics
-constexpr long long kSingleStats = SINGLE;
+constexpr long long kSingleStats = 12000000;
 
 struct VerifyPlan {
   int splits, chunk, parts, part;
@@ -152,7 +149,9 @@ struct DistillPlan {
 
 DistillPlan distill_plan(const rpd_distill* p) {
   DistillPlan d{};
+  // parts as the verification's statistics are cut
   d.chunk = (int)up_div(up_div(p->V, 64), 2048) * 2048;
+  while (d.chunk < 8192 && p->N * up_div(p->V, 2 * d.chunk) >= kFill) d.chunk *= 2;
   d.splits = (int)up_div(p->V, d.chunk);
   d.bytes = round256((size_t)p->N * d.splits * 8);
   return d;
@@ -386,9 +385,7 @@ rpd_status rpd_distill_loss(const rpd_distill* p, void* workspace, size_t worksp
   if (!p->loss) return fail(RPD_ERR_NULL_POINTER, "loss is required");
   st = check_workspace(workspace, workspace_bytes, distill_plan(p).bytes);
   if (st != RPD_OK) return st;
-  const rpd::DistillCall a = distill_call(p, workspace);
-  hipError_t e = rpd::launch_distill_loss(a, static_cast<hipStream_t>(stream));
-  if (e == hipSuccess && a.grad) e = rpd::launch_distill_grad(a, static_cast<hipStream_t>(stream));
+  const hipError_t e = rpd::launch_distill_loss(distill_call(p, workspace), static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(RPD_ERR_HIP, "launch: %s", hipGetErrorString(e));
   return RPD_OK;
 }

@@ -127,10 +127,10 @@ struct DistillCall {
   void* grad;             // [N][V] or NULL
   long long grad_stride;
   float2* partials;       // [N][splits]
-  int splits, chunk;
+  int splits, chunk;      // parts of a row, of `chunk` entries
 };
 
-hipError_t launch_distill_loss(const DistillCall& a, hipStream_t s);
+hipError_t launch_distill_loss(const DistillCall& a, hipStream_t s);   // with a.grad the gradient as well
 hipError_t launch_distill_grad(const DistillCall& a, hipStream_t s);
 
 }  // namespace rpd

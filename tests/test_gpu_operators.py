@@ -194,7 +194,18 @@ def test_verify_scales_that_round():
         assert float(err.max()) <= 2 * (2 * math.sqrt(50) + 16) * 2.0 ** -24
 
 
-def test_verify_masked_and_broken_rows():
+def test_verify_many_rows():
+    """Enough logits for float32 statistics (with float64 sums of the sampled rows)."""
+    c = _verify_case(48, 7, 32003, BF, True, True, 51, 0.7)
+    d = [None if t is None else t.to(DEV) for t in c]
+    o = rpd.verify_draft(*d[:4], draft_logits=d[4], draft_len=d[5], target_scale=0.7, draft_scale=0.7)
+    _check_verify(o, R.verify(*c[:4], draft=c[4], lens=c[5], target_scale=0.7, draft_scale=0.7), 32003)
+    o = rpd.verify_draft(*d[:4], draft_len=d[5], target_scale=0.7)
+    _check_verify(o, R.verify(*c[:4], lens=c[5], target_scale=0.7), 32003)
+
+
+@pytest.mark.parametrize("copies", [1, 900])   # 900: as many rows as take float32 statistics
+def test_verify_masked_and_broken_rows(copies):
     V = 3001
     g = torch.Generator().manual_seed(2)
     B, T = 9, 2
@@ -212,12 +223,15 @@ def test_verify_masked_and_broken_rows():
     target[6, 0, 7], draft[6, 0, 9] = 0.0, 0.0          # disjoint
     token[7] = torch.tensor([V, -1], dtype=torch.int32)  # outside the vocabulary
     draft[8, 0, 3] = math.inf
-    o = rpd.verify_draft(target.to(DEV), token.to(DEV), u.to(DEV), r.to(DEV), draft_logits=draft.to(DEV))
-    _check_verify(o, R.verify(target, token, u, r, draft=draft), V)
-    o = rpd.verify_draft(target.to(DEV), token.to(DEV), u.to(DEV), r.to(DEV))
-    _check_verify(o, R.verify(target, token, u, r), V)
-    o = rpd.verify_draft(target.to(DEV), token.to(DEV), greedy=True)
-    _check_verify(o, R.verify(target, token, None, None, greedy=True), V)
+    many = lambda t: t.to(DEV).repeat(copies, *[1] * (t.dim() - 1))   # noqa: E731
+
+    def check(o, ref):
+        for i in range(0, 9 * copies, 9):
+            _check_verify({k: v[i:i + 9] for k, v in o.items()}, ref, V)
+    a = [many(t) for t in (target, token, u, r)]
+    check(rpd.verify_draft(*a, draft_logits=many(draft)), R.verify(target, token, u, r, draft=draft))
+    check(rpd.verify_draft(*a), R.verify(target, token, u, r))
+    check(rpd.verify_draft(*a[:2], greedy=True), R.verify(target, token, None, None, greedy=True))
 
 
 def test_verify_rows_behind_the_draft_are_not_read():

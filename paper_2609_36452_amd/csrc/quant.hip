@@ -14,7 +14,8 @@
 // The matrix operands are exact: a code nibble put into the mantissa of fp16
 // 1024 is 1024 + q, and one packed subtraction leaves q - z, an integer in
 // -15..15. Bits 4..7 of each half are 1024 + 16 q and take one packed
-// multiply-add instead, which saves their shift: 9 instructions for 8 weights.
+// multiply-add instead, which saves their shift: 9 instructions for 8 weights,
+// masking and setting the exponent being one.
 // bf16 rows become fp16 by a power of two per row (the largest finite |x| comes
 // to 2^14..2^15): their 8 bits fit, and an element so small that it falls among
 // fp16's subnormals is off by at most 2^-40 of the row's largest, far below
@@ -119,13 +120,27 @@ __device__ __forceinline__ typename Raw<N>::t load_bits(char* base, int range, u
     return __builtin_bit_cast(uint64_t, __builtin_amdgcn_raw_buffer_load_b64(r, offset, 0, 0));
 }
 
-// 8 codes as fp16 operands without a conversion: the bits of a nibble in the
-// low bits of a half are the subnormal q 2^-24, four bits up q 2^-20 (the x
-// that meet those are scaled down by 16), which the matrix cores take exactly
-__device__ __forceinline__ f16x8 decode(uint32_t w) {
+// 8 codes as q - z in fp16, exactly; zl and zh hold -(1024 + z) and -(64 + z).
+// A nibble in the low mantissa bits of 1024 is 1024 + q, four bits up
+// 1024 + 16 q: one mask-and-or each, one subtraction or multiply-add for a
+// pair, one shift for the other two pairs. masks: 0x000f000f and 0x00f000f0,
+// one: 1024 in both halves, in registers (as literals they do not fit into one
+// instruction: 107.6 us instead of 96.2 at 32 rows). As subnormals, q 2^-24,
+// the codes would need no subtraction, 5 instructions, and the zero points a
+// correction by the sums of x; but the matrix cores keep fewer bits of such
+// products: logits were off by 4e-6 of their size, 1e-7 so, for 4% of the time
+// at 32 rows.
+__device__ __forceinline__ f16x8 decode(uint32_t w, f16x2 zl, f16x2 zh, uint32_t mask_low, uint32_t mask_high,
+                                        uint32_t one) {
+  const f16x2 sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
   const uint32_t w8 = w >> 8;
-  const u32x4 o = {w & 0x000f000fu, w & 0x00f000f0u, w8 & 0x000f000fu, w8 & 0x00f000f0u};
-  return __builtin_bit_cast(f16x8, o);
+  const uint32_t u0 = (w & mask_low) | one, u1 = (w & mask_high) | one;
+  const uint32_t u2 = (w8 & mask_low) | one, u3 = (w8 & mask_high) | one;
+  const f16x2 a = __builtin_bit_cast(f16x2, u0) + zl;
+  const f16x2 b = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, u1), sixteenth, zh);
+  const f16x2 c = __builtin_bit_cast(f16x2, u2) + zl;
+  const f16x2 e = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, u3), sixteenth, zh);
+  return f16x8{a.x, a.y, b.x, b.y, c.x, c.y, e.x, e.y};
 }
 
 template <bool BF16>
@@ -133,20 +148,14 @@ __device__ __forceinline__ float from_bits16(uint32_t b) {
   return BF16 ? __uint_as_float(b << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)b);
 }
 
-// 8 elements of a row as operands, scaled by 2^-ex, and their sum added to `sum`
-template <bool BF16>
-__device__ __forceinline__ u32x4 to_operand(const u32x4 r, int ex, float& sum) {
+// 8 bf16 elements of a row as fp16 operands, scaled by 2^-ex
+__device__ __forceinline__ u32x4 to_operand(const u32x4 r, int ex) {
   u32x4 o;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const uint32_t two = r[e];   // (a bit_cast of the vector's element itself takes the wrong one)
-    const f16x2 h = __builtin_bit_cast(f16x2, two);
-    const float lo = BF16 ? __uint_as_float(two << 16) : (float)h.x;
-    const float hi = BF16 ? __uint_as_float(two & 0xffff0000u) : (float)h.y;
-    const int shift = -ex - (e & 1 ? 4 : 0);   // columns 2, 3, 6, 7 meet codes four bits up
-    const f16x2 w = {(_Float16)ldexpf(lo, shift), (_Float16)ldexpf(hi, shift)};
-    const _Float16 unit = (_Float16)(e & 1 ? 16.f : 1.f);
-    sum = __builtin_amdgcn_fdot2(w, f16x2{unit, unit}, sum, false);
+    const uint32_t two = r[e];
+    const f16x2 w = {(_Float16)ldexpf(__uint_as_float(two << 16), -ex),
+                     (_Float16)ldexpf(__uint_as_float(two & 0xffff0000u), -ex)};
     o[e] = __builtin_bit_cast(uint32_t, w);
   }
   return o;
@@ -173,7 +182,6 @@ __device__ __forceinline__ void soft_push(Soft& s, float z, int v) {
 template <int NC, int MT, int GPC, bool ZP, bool LONG, bool PRE, bool BF16>
 __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, QuantCall a) {
   constexpr int NB = quant_batch(NC, MT);       // tiles between two barriers; as many are in flight
-  constexpr int NG = NC * GPC, NX = (NG + 3) / 4;   // groups of a wave; of them four to a correction
   typedef typename Raw<2 * GPC>::t sraw_t;
   typedef typename Raw<GPC>::t zraw_t;
   extern __shared__ __align__(16) float lds[];
@@ -262,12 +270,15 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, Q
           }
         }
   };
-  if (PRE) {
+  if (!BF16) {
+    if (tid < MT * 16) s_exp[tid] = 0;
+    if (!PRE && !LONG) load_x(0);
+  } else if (PRE) {
     if (tid < MT * 16) s_exp[tid] = a.xexp[rg * MT * 16 + tid];
   } else {
-    // each row's largest magnitude (the bits of either type's magnitudes are in order; infinity and NaN count as
-    // the largest finite one, the row's logits being infinite or NaN anyway)
-    const u16x2 finite = {(uint16_t)(BF16 ? 0x7f7f : 0x7bff), (uint16_t)(BF16 ? 0x7f7f : 0x7bff)};
+    // each row's largest magnitude (the bits of magnitudes are in order; infinity and NaN count as the largest finite
+    // one, the row's logits being infinite or NaN anyway)
+    const u16x2 finite = {(uint16_t)0x7f7f, (uint16_t)0x7f7f};
     u16x2 big[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) big[mt] = u16x2{0, 0};
@@ -296,7 +307,7 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, Q
       uint32_t b = 0;
       for (int w = 0; w < W; ++w) b = max(b, s_max[w * MT * 16 + tid]);
       int e = 15;
-      if (b) (void)frexpf(from_bits16<BF16>(b), &e);   // in [2^(e-1), 2^e): to be brought to 2^14..2^15
+      if (b) (void)frexpf(__uint_as_float(b << 16), &e);   // in [2^(e-1), 2^e): to be brought to 2^14..2^15
       s_exp[tid] = e - 15;
     }
   }
@@ -304,44 +315,28 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, Q
     for (int e = tid; e < NB * MT * 256; e += nthreads) states[e] = soft_pack(soft_empty());
   __syncthreads();
 
-  float xg[MT][NX];   // row col's sum over group 4 i + quad of this wave, in units of the products
-  auto convert_x = [&](int round) {
-    if (PRE) {
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int i = 0; i < NX; ++i) {
-          const int g = round * per_round * GPC + wid * NG + 4 * i + quad;
-          xg[mt][i] = 4 * i + quad < NG && g < q.ngp ? a.xsum[((long long)(rg * MT + mt) * q.ngp + g) * 16 + col] : 0.f;
-        }
-      return;
-    }
+  auto convert_x = [&]() {
+    if (PRE || !BF16) return;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const int ex = s_exp[mt * 16 + col];
 #pragma unroll
-      for (int i = 0; i < NX; ++i) xg[mt][i] = 0.f;
-#pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int g = 0; g < GPC; ++g) {
-          float sum = 0.f;
-#pragma unroll
-          for (int u = g * 4 / GPC; u < (g + 1) * 4 / GPC; ++u) {
-            u32x4 o = to_operand<BF16>(xf[mt][c][u], ex, sum);
-            asm volatile("" : "+v"(o));   // packed here: one piece at a time in float beside the rows
-            xf[mt][c][u] = o;
-          }
-          sum += __shfl_xor(sum, 16);
-          sum += __shfl_xor(sum, 32);
-          if (quad == (c * GPC + g) % 4) xg[mt][(c * GPC + g) / 4] = sum * 0x1p-24f;
+        for (int u = 0; u < 4; ++u) {
+          u32x4 o = to_operand(xf[mt][c][u], ex);
+          asm volatile("" : "+v"(o));   // packed here: one piece at a time in float beside the rows
+          xf[mt][c][u] = o;
         }
     }
   };
   if (PRE && !LONG) load_x(0);
-  if (!LONG) convert_x(0);
+  if (!LONG) convert_x();
 
   auto row_of = [&](int e) { return 16 * (e >> 8) + 4 * (e >> 6 & 3) + (e >> 4 & 3); };
+  // not literals, see decode
+  uint32_t mask = 0x000f000fu, one = 0x64006400u;
+  asm("" : "+s"(mask), "+v"(one));
   int buf = 0;
   for (int ti = 0; ti < n_tiles; ti += NB) {
     // a batch of tiles, over the end the last one again (its sums are then not used)
@@ -354,38 +349,23 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, Q
       for (int round = 0; round < (LONG ? a.rounds : 1); ++round) {
         if (LONG) {
           load_x(round);
-          convert_x(round);
+          convert_x();
         }
-        // the scales, and -s z of this quad's groups
-        float sc[NC][GPC], zs[NX];
-#pragma unroll
-        for (int i = 0; i < NX; ++i) zs[i] = 0.f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-          const bool in = (LONG ? round * per_round : 0) + wid * NC + c < q.nc;
 #pragma unroll
           for (int g = 0; g < GPC; ++g) {
             const uint32_t bits = (uint32_t)(sb[u][c] >> (16 * g)) & 0xffffu;
-            sc[c][g] = from_bits16<BF16>(in ? bits : 0u);
-            const float z = ZP ? (float)(uint32_t)(zb[u][c] >> (8 * g) & 255) : 8.f;
-            if (quad == (c * GPC + g) % 4) zs[(c * GPC + g) / 4] = -sc[c][g] * z;
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < NX; ++i)
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
-            acc[mt] = __builtin_amdgcn_mfma_f32_16x16x4f32(xg[mt][i], zs[i], acc[mt], 0, 0, 0);
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-#pragma unroll
-          for (int g = 0; g < GPC; ++g) {
+            const float sc = from_bits16<BF16>((LONG ? round * per_round : 0) + wid * NC + c < q.nc ? bits : 0u);
+            const _Float16 z = ZP ? (_Float16)(float)(uint32_t)(zb[u][c] >> (8 * g) & 255) : (_Float16)8.f;
+            const _Float16 zl1 = (_Float16)-1024.f - z, zh1 = (_Float16)-64.f - z;
+            const f16x2 zl = {zl1, zl1}, zh = {zh1, zh1};
             f32x4 part[MT];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) part[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int t = g * 4 / GPC; t < (g + 1) * 4 / GPC; ++t) {
-              const f16x8 wf = decode(wb[u][c][t]);
+              const f16x8 wf = decode(wb[u][c][t], zl, zh, mask, mask << 4, one);
 #pragma unroll
               for (int mt = 0; mt < MT; ++mt)
                 part[mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, xf[mt][c][t]), wf, part[mt],
@@ -394,7 +374,7 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, Q
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) acc[mt][i] = fmaf(sc[c][g], part[mt][i], acc[mt][i]);
+              for (int i = 0; i < 4; ++i) acc[mt][i] = fmaf(sc, part[mt][i], acc[mt][i]);
             if (GPC > 1 && NC * MT > 2) {
 #pragma unroll
               for (int mt = 0; mt < MT; ++mt) asm volatile("" : "+v"(acc[mt]));
@@ -431,7 +411,7 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_quant_project(QuantDims q, Q
         for (int k = 0; k < 8; ++k) z += t[k];
       }
       for (; w < W; ++w, p += kRedWave) z += *p;
-      z = ldexpf(z, s_exp[m] + 24);
+      z = ldexpf(z, s_exp[m]);
       if (a.stats) {   // this thread has entry i in every batch
         Soft st = soft_unpack(states[i]);
         soft_push(st, z * a.logit_scale, (int)v);
@@ -478,44 +458,40 @@ __global__ __launch_bounds__(256) void k_quant_rows(QuantDims q, QuantCall a) {
     for (int e = 0; e < 4; ++e) r[e] = (uint32_t)x[k + 2 * e] | (uint32_t)x[k + 2 * e + 1] << 16;
     return r;
   };
-  const int pieces = q.nc * 16;
+  const int pieces = q.nc * 16, rt = m >> 4, col = m & 15;
   constexpr int kHeld = 4;   // a thread's first pieces are read once (rows of up to 8192)
   u32x4 held[kHeld];
 #pragma unroll
   for (int j = 0; j < kHeld; ++j) held[j] = piece(8 * (tid + 256 * j));
-  u16x2 big = {0, 0};
-  auto grow = [&](const u32x4 r) {
+  int ex = 0;
+  if (BF16) {
+    u16x2 big = {0, 0};
+    auto grow = [&](const u32x4 r) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) big = __builtin_elementwise_max(big, __builtin_bit_cast(u16x2, r[e] & 0x7fff7fffu));
-  };
+      for (int e = 0; e < 4; ++e) big = __builtin_elementwise_max(big, __builtin_bit_cast(u16x2, r[e] & 0x7fff7fffu));
+    };
 #pragma unroll
-  for (int j = 0; j < kHeld; ++j) grow(held[j]);
-  for (int p = tid + 256 * kHeld; p < pieces; p += 256) grow(piece(8 * p));
-  uint32_t top = min((uint32_t)max(big.x, big.y), BF16 ? 0x7f7fu : 0x7bffu);
+    for (int j = 0; j < kHeld; ++j) grow(held[j]);
+    for (int p = tid + 256 * kHeld; p < pieces; p += 256) grow(piece(8 * p));
+    uint32_t top = min((uint32_t)max(big.x, big.y), 0x7f7fu);
 #pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, k));
-  if (lane == 0) s_max[tid >> 6] = top;
-  __syncthreads();
-  top = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
-  int ex = 15;
-  if (top) (void)frexpf(from_bits16<BF16>(top), &ex);
-  ex -= 15;
-  if (tid == 0) a.xexp[m] = ex;
-  const int rt = m >> 4, col = m & 15, per_group = q.group / 8;   // a group is 4, 8 or 16 neighbouring lanes' pieces
+    for (int k = 32; k >= 1; k >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, k));
+    if (lane == 0) s_max[tid >> 6] = top;
+    __syncthreads();
+    top = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+    int e = 15;
+    if (top) (void)frexpf(__uint_as_float(top << 16), &e);
+    ex = e - 15;
+    if (tid == 0) a.xexp[m] = ex;
+  }
   auto put = [&](int p, const u32x4 r) {
-    float sum = 0.f;
-    if (p < pieces) {
-      const u32x4 o = to_operand<BF16>(r, ex, sum);
-      a.xrows[((long long)rt * q.nc + (p >> 4)) * 256 + (p >> 2 & 3) * 64 + (p & 3) * 16 + col] = o;
-    }
-    for (int k = 1; k < per_group; k <<= 1) sum += __shfl_xor(sum, k);
-    if (p < pieces && p % per_group == 0)
-      a.xsum[((long long)rt * q.ngp + p / per_group) * 16 + col] = sum * 0x1p-24f;
+    if (p < pieces)
+      a.xrows[((long long)rt * q.nc + (p >> 4)) * 256 + (p >> 2 & 3) * 64 + (p & 3) * 16 + col] =
+          BF16 ? to_operand(r, ex) : r;
   };
 #pragma unroll
-  for (int j = 0; j < kHeld; ++j)
-    if (256 * j < pieces) put(tid + 256 * j, held[j]);
-  for (int p0 = 256 * kHeld; p0 < pieces; p0 += 256) put(p0 + tid, piece(8 * (p0 + tid)));
+  for (int j = 0; j < kHeld; ++j) put(tid + 256 * j, held[j]);
+  for (int p = tid + 256 * kHeld; p < pieces; p += 256) put(p, piece(8 * p));
 }
 
 // one wave a row: the slots' states -> argmax, top probability, entropy

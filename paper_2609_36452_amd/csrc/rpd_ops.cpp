@@ -71,14 +71,13 @@ void quant_plan(const rpd::QuantDims& q, rpd::QuantCall& a) {
 
 // Workspace of a call: the laid out rows (more than 16 of them), then the states of the statistics.
 struct QuantSpace {
-  size_t rows, sums, exps, states, bytes;   // offsets
+  size_t exps, states, bytes;   // offsets (the rows come first)
 };
 QuantSpace quant_space(const rpd::QuantDims& q, const rpd::QuantCall& a) {
   QuantSpace w{};
   if (a.M > 16) {
     const size_t tiles = (size_t)a.row_groups * a.row_tiles;
-    w.sums = round256(tiles * q.nc * 4096);
-    w.exps = w.sums + round256(tiles * q.ngp * 64);
+    w.exps = tiles * q.nc * 4096;
     w.states = w.exps + round256(tiles * 64);
   }
   w.bytes = w.states + (a.stats ? round256((size_t)a.M * a.slots * 16) : 0);
@@ -295,7 +294,6 @@ rpd_status rpd_quant_project(const rpd_quant_head* h, const void* packed, int32_
     char* ws = static_cast<char*>(workspace);
     if (M > 16) {
       a.xrows = reinterpret_cast<rpd::codes_t*>(ws);
-      a.xsum = reinterpret_cast<float*>(ws + w.sums);
       a.xexp = reinterpret_cast<int32_t*>(ws + w.exps);
     }
     a.partials = reinterpret_cast<float4*>(ws + w.states);

@@ -42,8 +42,7 @@ struct QuantCall {
   int out_type;           // RPD_DTYPE_*
   float logit_scale;
   codes_t* xrows;         // [16-row tile][chunk][4][64] operands; NULL: the workgroups convert x (at most 16 rows)
-  float* xsum;            // [16-row tile][padded group][16] sums of a group, in units of the products
-  int32_t* xexp;          // [rows] binary exponent taken out of a row
+  int32_t* xexp;          // [rows] binary exponent taken out of a bf16 row
   float4* partials;       // [M][slots]
   int32_t* argmax;
   float* confidence;

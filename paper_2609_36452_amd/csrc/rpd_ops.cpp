@@ -104,7 +104,9 @@ bool verify_shape_ok(const rpd_verify* p) {
 
 constexpr long long kFill = 4096;   // workgroups of 256 threads: 256 CUs, 8 on each, twice
 
-// logits from which float32 statistics and a pass of float64 sums over the sampled rows beat float64 statistics
+// Logits from which float32 statistics, and a pass of float64 sums over the sampled rows, beat float64 statistics:
+// 4 drafted tokens, V = 126464, bf16: 8 sequences (9.1 million logits) take 30.5 us so and 28.0 in float64, 16 take
+// 36.4 and 41.0, 32 take 45.7 and 64.2.
 constexpr long long kSingleStats = 12000000;
 
 struct VerifyPlan {
@@ -332,7 +334,8 @@ rpd_status rpd_verify_draft(const rpd_verify* p, void* workspace, size_t workspa
       misaligned(p->accept, 3))
     return fail(RPD_ERR_UNSUPPORTED, "a pointer is not aligned to its element");
   const VerifyPlan v = verify_plan(p);
-  if (v.rows * v.splits > kMaxBlocks) return fail(RPD_ERR_BAD_SHAPE, "B * T * V is too large");
+  if (v.rows * v.splits > kMaxBlocks || (!greedy && (long long)p->B * v.parts > kMaxBlocks))
+    return fail(RPD_ERR_BAD_SHAPE, "B * T * V is too large");
   rpd_status st = check_workspace(workspace, workspace_bytes, v.bytes);
   if (st != RPD_OK) return st;
   rpd::VerifyCall a{};

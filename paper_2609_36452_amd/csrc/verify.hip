@@ -11,14 +11,20 @@
 // launches. The steps:
 //   k_verify_stats   maximum and sum of a part of a row, every row at once
 //   k_verify_decide  a sequence's acceptance probabilities, n, and the row that
-//                    the further token is drawn from
+//                    the further token is drawn from (many rows; of few rows
+//                    every workgroup of k_verify_parts does that for itself)
 //   k_verify_totals  float64 sums of that row (after float32 statistics)
 //   k_verify_parts   sums of max(0, p - q), and of p, over parts of that row
 //   k_verify_token   the part that r falls in, then the token in it
+// A launch that waits for the one before it takes 4 us however little it does.
+// 5 target and 4 draft rows of 126464 bf16: 16.9 us in three launches, 19.3
+// with the decision as a fourth. (A draw by the last workgroup to finish its
+// part needs no launch either, but the release and acquire cost 62 parts as
+// much as it, and 32 x 38 parts 14 us more.)
 // The draw is float64, exponentials included: the token's border lies among up
 // to V cumulative sums a few 1e-6 apart, and in float32 a draw in a hundred of
 // a flat row would fall on the neighbour of the right token. Few rows take
-// their statistics in float64 as well, which saves a launch; many rows do not
+// their statistics in float64 as well, which saves two launches; many do not
 // (a float64 exponential is 12 double operations at half the rate of single
 // ones: 288 target and 130 draft rows of 152064 bf16 take 39 us, 18 in float32).
 #include <cstdint>
@@ -223,20 +229,24 @@ __device__ __forceinline__ Row row_stats(const VerifyCall& a, long long row, flo
   return Row{m, S};
 }
 
-// One workgroup a sequence, a wave a row in turn. A wave keeps the statistics of the first token it turns down (and
-// of the row behind the draft, which ends it as well); the one with the first of all writes the pick.
-constexpr int kDecideWaves = 8;
-template <class E>
-__global__ __launch_bounds__(kDecideWaves * 64) void k_verify_decide(VerifyCall a) {
-  const int b = blockIdx.x, lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+// A sequence's acceptance probabilities, n and the rows that its further token is drawn from, by a workgroup, a wave a
+// row in turn. A wave keeps the statistics of the first token it turns down (and of the row behind the draft, which
+// ends it as well); the one with the first of all has the pick. Of several workgroups that do this for one sequence,
+// one writes the results.
+struct Decision {
+  VerifyPick pick;
+  int n;
+};
+template <class E, int WAVES>
+__device__ __forceinline__ void decide(const VerifyCall& a, int b, bool write, Decision& s) {
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
   const int len = draft_len(a, b);
-  __shared__ int s_first;
-  if (threadIdx.x == 0) s_first = len;
+  if (threadIdx.x == 0) s.n = len;
   __syncthreads();
   const long long t0 = (long long)b * (a.T + 1), d0 = (long long)a.B * (a.T + 1) + (long long)b * a.T;
   int mine = INT_MAX;
   VerifyPick pick;
-  for (int t = wid; t <= len; t += kDecideWaves) {
+  for (int t = wid; t <= len; t += WAVES) {
     const bool drafted = t < len;
     const int x = drafted ? a.token[(long long)b * a.T + t] : -1;
     const float u = drafted ? a.u[(long long)b * a.T + t] : 0.f;
@@ -251,20 +261,30 @@ __global__ __launch_bounds__(kDecideWaves * 64) void k_verify_decide(VerifyCall 
       double l = ((double)zp - (double)p.m) * (double)a.target_scale - log(p.S);
       if (a.draft) l -= ((double)zq - (double)q.m) * (double)a.draft_scale - log(q.S);
       acc = !valid ? 0.f : l > 0.0 ? 1.f : (float)exp(l);
-      if (lane == 0) a.accept[(long long)b * a.T + t] = acc;
+      if (write && lane == 0) a.accept[(long long)b * a.T + t] = acc;
     }
     if (mine == INT_MAX && !(drafted && u < acc)) {
       mine = t;
       pick = VerifyPick{p.S, q.S, p.m, q.m, x, drafted};
-      if (lane == 0) atomicMin(&s_first, t);
+      if (lane == 0) atomicMin(&s.n, t);
     }
   }
-  for (int t = len + threadIdx.x; t < a.T; t += kDecideWaves * 64) a.accept[(long long)b * a.T + t] = 0.f;
+  if (write)
+    for (int t = len + threadIdx.x; t < a.T; t += WAVES * 64) a.accept[(long long)b * a.T + t] = 0.f;
   __syncthreads();
-  if (lane == 0 && mine == s_first) {
-    a.n_accept[b] = mine;
-    a.picks[b] = pick;
+  if (lane == 0 && mine == s.n) {
+    s.pick = pick;
+    if (write) a.n_accept[b] = mine;
   }
+  __syncthreads();
+}
+
+constexpr int kDecideWaves = 8;
+template <class E>
+__global__ __launch_bounds__(kDecideWaves * 64) void k_verify_decide(VerifyCall a) {
+  __shared__ Decision s;
+  decide<E, kDecideWaves>(a, blockIdx.x, true, s);
+  if (threadIdx.x == 0) a.picks[blockIdx.x] = s.pick;
 }
 
 // max(0, p - q) of a sequence whose token n was turned down
@@ -349,9 +369,6 @@ __global__ __launch_bounds__(kThreads) void k_verify_totals(VerifyCall a) {
 // the sums of the sampled rows, by each wave in a fixed order (NaN and an empty row end as in the statistics)
 __device__ __forceinline__ void sampled_sums(const VerifyCall& a, int b, const VerifyPick& k, int lane, double& sp,
                                              double& sq) {
-  sp = k.sp;
-  sq = k.sq;
-  if (!a.totals) return;
   double t[2] = {0.0, 0.0};
   for (int i = lane; i < a.parts; i += 64)
 #pragma unroll
@@ -364,20 +381,30 @@ __device__ __forceinline__ void sampled_sums(const VerifyCall& a, int b, const V
   if (a.draft && k.down && k.mq > -INFINITY) sq = t[1];
 }
 
-// the parts of sum p and, where a token was turned down, of sum max(0, p - q)
-template <class E>
-__global__ __launch_bounds__(kThreads) void k_verify_parts(VerifyCall a) {
+// The parts of sum p and, where a token was turned down, of sum max(0, p - q).
+// DECIDE: every workgroup decides for itself beforehand, with more waves for that.
+template <class E, bool DECIDE>
+__global__ __launch_bounds__(DECIDE ? kDecideWaves * 64 : kThreads) void k_verify_parts(VerifyCall a) {
+  constexpr int W = DECIDE ? kDecideWaves : kWaves;
   const int part = blockIdx.x % a.parts, b = blockIdx.x / a.parts;
-  const VerifyPick k = a.picks[b];
-  __shared__ double s_sum[kWaves][2], s_table[32];
+  __shared__ double s_sum[W][2], s_table[32];
+  __shared__ Decision s;
   fill_table(s_table);
-  __syncthreads();
-  double sp, sq;
-  sampled_sums(a, b, k, threadIdx.x & 63, sp, sq);
-  const Rest<E> rest(a, b, a.n_accept[b], k, sp, sq, s_table);
+  if (DECIDE) {
+    decide<E, W>(a, b, part == 0, s);
+    if (part == 0 && threadIdx.x == 0) a.picks[b] = s.pick;
+  } else {
+    if (threadIdx.x == 0) s = Decision{a.picks[b], a.n_accept[b]};
+    __syncthreads();
+  }
+  const VerifyPick k = s.pick;
+  const int n = s.n;
+  double sp = k.sp, sq = k.sq;
+  if (!DECIDE) sampled_sums(a, b, k, threadIdx.x & 63, sp, sq);
+  const Rest<E> rest(a, b, n, k, sp, sq, s_table);
   const int hi = min(a.V, (part + 1) * a.part);
   double sum[2] = {0.0, 0.0};
-  for (int i = part * a.part + 8 * threadIdx.x; i < hi; i += 8 * kThreads) {
+  for (int i = part * a.part + 8 * threadIdx.x; i < hi; i += 8 * 64 * W) {
     double p[8], w[8];
     rest.eight(i, a.V, k.down, p, w);   // (a part ends at the row's end or at a whole vector)
 #pragma unroll
@@ -395,7 +422,7 @@ __global__ __launch_bounds__(kThreads) void k_verify_parts(VerifyCall a) {
   __syncthreads();
   if (threadIdx.x < 2) {
     double t = 0.0;
-    for (int w = 0; w < kWaves; ++w) t += s_sum[w][threadIdx.x];
+    for (int w = 0; w < W; ++w) t += s_sum[w][threadIdx.x];
     a.sums[((long long)threadIdx.x * a.B + b) * a.parts + part] = t;
   }
 }
@@ -467,8 +494,8 @@ __global__ __launch_bounds__(kThreads) void k_verify_token(VerifyCall a) {
   if (part >= 0) {
     // the same inside the part, 2048 entries at a time
     const bool use_rest = s_rest;
-    double sp, sq;
-    sampled_sums(a, b, k, lane, sp, sq);
+    double sp = k.sp, sq = k.sq;
+    if (a.totals) sampled_sums(a, b, k, lane, sp, sq);
     const Rest<E> rest(a, b, n, k, sp, sq, s_table);
     const double left = s_left;
     const int hi = min(a.V, (part + 1) * a.part);
@@ -522,11 +549,14 @@ __global__ __launch_bounds__(kThreads) void k_verify_token(VerifyCall a) {
     a.out_token[(long long)b * (a.T + 1) + t] = t < n ? a.token[(long long)b * a.T + t] : t == n ? token : -1;
 }
 
-__global__ __launch_bounds__(64) void k_verify_greedy(VerifyCall a) {
-  const int b = blockIdx.x, lane = threadIdx.x, len = draft_len(a, b);
-  int n = 0, best = -1;
-  bool running = true;
-  for (int t = 0; t <= len; ++t) {
+// One workgroup a sequence, a wave a row in turn, as in decide.
+__global__ __launch_bounds__(kDecideWaves * 64) void k_verify_greedy(VerifyCall a) {
+  const int b = blockIdx.x, lane = threadIdx.x & 63, wid = threadIdx.x >> 6, len = draft_len(a, b);
+  __shared__ int s_n, s_best;
+  if (threadIdx.x == 0) s_n = len;
+  __syncthreads();
+  int mine = INT_MAX, best = -1;
+  for (int t = wid; t <= len; t += kDecideWaves) {
     float m = -INFINITY;
     int idx = INT_MAX;
     for (int i = lane; i < a.splits; i += 64) {
@@ -544,16 +574,22 @@ __global__ __launch_bounds__(64) void k_verify_greedy(VerifyCall a) {
     if (idx == INT_MAX) idx = -1;   // a row of -inf and NaN has no largest entry
     const bool same = t < len && idx >= 0 && a.token[(long long)b * a.T + t] == idx;
     if (lane == 0 && t < len) a.accept[(long long)b * a.T + t] = same ? 1.f : 0.f;
-    if (running) {
+    if (mine == INT_MAX && !same) {
+      mine = t;
       best = idx;
-      n = t;
-      running = same;
+      if (lane == 0) atomicMin(&s_n, t);
     }
   }
-  if (lane == 0) a.n_accept[b] = n;
-  for (int t = len + lane; t < a.T; t += 64) a.accept[(long long)b * a.T + t] = 0.f;
-  for (int t = lane; t <= a.T; t += 64)
-    a.out_token[(long long)b * (a.T + 1) + t] = t < n ? a.token[(long long)b * a.T + t] : t == n ? best : -1;
+  __syncthreads();
+  const int n = s_n;
+  if (lane == 0 && mine == n) {
+    s_best = best;
+    a.n_accept[b] = n;
+  }
+  __syncthreads();
+  for (int t = len + threadIdx.x; t < a.T; t += kDecideWaves * 64) a.accept[(long long)b * a.T + t] = 0.f;
+  for (int t = threadIdx.x; t <= a.T; t += kDecideWaves * 64)
+    a.out_token[(long long)b * (a.T + 1) + t] = t < n ? a.token[(long long)b * a.T + t] : t == n ? s_best : -1;
 }
 
 template <class E>
@@ -563,7 +599,7 @@ hipError_t verify(const VerifyCall& a, hipStream_t s) {
   if (a.greedy) {
     k_verify_stats<E, kGreedy><<<(unsigned)(rows * a.splits), kThreads, 0, s>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    k_verify_greedy<<<a.B, 64, 0, s>>>(a);
+    k_verify_greedy<<<a.B, kDecideWaves * 64, 0, s>>>(a);
     return hipGetLastError();
   }
   if (a.totals)
@@ -571,13 +607,15 @@ hipError_t verify(const VerifyCall& a, hipStream_t s) {
   else
     k_verify_stats<E, kDouble><<<(unsigned)(rows * a.splits), kThreads, 0, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  k_verify_decide<E><<<a.B, kDecideWaves * 64, 0, s>>>(a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (a.totals) {
+  if (!a.totals) {
+    k_verify_parts<E, true><<<(unsigned)(a.B * a.parts), kDecideWaves * 64, 0, s>>>(a);
+  } else {
+    k_verify_decide<E><<<a.B, kDecideWaves * 64, 0, s>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
     k_verify_totals<E><<<(unsigned)(a.B * a.parts), kThreads, 0, s>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
+    k_verify_parts<E, false><<<(unsigned)(a.B * a.parts), kThreads, 0, s>>>(a);
   }
-  k_verify_parts<E><<<(unsigned)(a.B * a.parts), kThreads, 0, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   k_verify_token<E><<<a.B, kThreads, 0, s>>>(a);
   return hipGetLastError();

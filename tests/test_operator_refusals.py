@@ -96,7 +96,8 @@ def _verify(**kw):
     (dict(tb=-1), 2), (dict(dr=-1), 2), (dict(dtype=3), 5), (dict(flags=2), 3), (dict(ts=math.nan), 3),
     (dict(ds=-0.5), 3), (dict(ds=math.inf), 3), (dict(target=None), 1), (dict(token=None), 1), (dict(u=None), 1),
     (dict(r=None), 1), (dict(out=None), 1), (dict(n=None), 1), (dict(accept=None), 1), (dict(target=P + 1), 5),
-    (dict(token=P + 2), 5), (dict(dtype=1, draft=P + 2), 5), (dict(B=1 << 10, T=1000, V=1 << 28), 2)])
+    (dict(token=P + 2), 5), (dict(dtype=1, draft=P + 2), 5), (dict(B=1 << 10, T=1000, V=1 << 28), 2),
+    (dict(B=1 << 20, T=0, V=100000), 2)])
 def test_verify_refusals(kw, status):
     p = _verify(**kw)
     assert rpd.lib().rpd_verify_draft(ctypes.byref(p), P, 1 << 50, None) == status

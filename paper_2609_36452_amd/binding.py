@@ -765,18 +765,14 @@ class _Distill(torch.autograd.Function):
         p = _distill_problem(logits, teacher_id, teacher_logit, teacher_lse, weight, logit_scale)
         loss, state = _distill_loss(p, logits, None)
         ctx.save_for_backward(logits, teacher_id, teacher_logit, teacher_lse, weight, state)
-        ctx.problem = p
+        ctx.logit_scale = logit_scale
         return loss
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad_loss):
-        *inputs, state = ctx.saved_tensors
-        p = ctx.problem
-        if [_ptr(t) for t in inputs] == [p.logits, p.id, p.teacher, p.teacher_lse, p.weight]:
-            p = RpdDistill.from_buffer_copy(p)
-        else:   # the saved tensors were moved meanwhile
-            p = _distill_problem(*inputs, p.logit_scale)
+        *inputs, state = ctx.saved_tensors   # perhaps not where they were (saved tensors' hooks)
+        p = _distill_problem(*inputs, ctx.logit_scale)
         logits = inputs[0]
         grad = _grad_like(logits, p)
         up = grad_loss.to(torch.float32).contiguous()   # a broadcast upstream gradient has stride 0

@@ -26,6 +26,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kHeld = 4;   // vectors that a thread holds
 constexpr int kMaxList = RPD_DISTILL_MAX_K;
+static_assert(kMaxList <= kThreads, "a thread an entry of the list");
 
 // a row's state between the loss and the gradient
 struct RowState {
@@ -51,11 +52,14 @@ __device__ __forceinline__ const typename E::t* row_of(const DistillCall& a, int
   return static_cast<const typename E::t*>(a.logits) + n * a.stride;
 }
 
+// A list in LDS is read four at a time: filled up with -1.
+__device__ __forceinline__ int4 four_of(const int* s_ids, int i) { return *reinterpret_cast<const int4*>(s_ids + i); }
+
 // the row's list into LDS; with `marks` (a bit per entry of [lo, hi)), those in it marked. Ends with a barrier.
 __device__ __forceinline__ void load_list(const DistillCall& a, int n, int* s_ids, uint32_t* s_mark, int lo, int hi) {
   if (s_mark)
     for (int i = threadIdx.x; i < (hi - lo + 31) / 32; i += blockDim.x) s_mark[i] = 0;
-  for (int j = threadIdx.x; j < a.k; j += blockDim.x) s_ids[j] = a.ids[(long long)n * a.k + j];
+  for (int j = threadIdx.x; j < (a.k + 3 & ~3); j += blockDim.x) s_ids[j] = j < a.k ? a.ids[(long long)n * a.k + j] : -1;
   __syncthreads();
   if (!s_mark) return;
   for (int j = threadIdx.x; j < a.k; j += blockDim.x) {
@@ -84,21 +88,21 @@ __global__ __launch_bounds__(kThreads) void k_distill_part(DistillCall a) {
   const int n = blockIdx.x / a.splits, split = blockIdx.x - n * a.splits;
   if (skipped(a, n)) return;
   extern __shared__ uint32_t s_mark[];   // a bit per entry of the part
-  __shared__ int s_ids[kMaxList];
+  __shared__ __align__(16) int s_ids[kMaxList];
   __shared__ float s_max[kThreads / 64], s_sum[kThreads / 64];
   const int lo = split * a.chunk, hi = min(a.V, lo + a.chunk);
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, first = lo + 8 * threadIdx.x;
   const typename E::t* p = row_of<E>(a, n);
-  // (a part is at most kHeld vectors a thread, or read in rounds of as many)
   MaxSum s{-INFINITY, 0.f};
-  bool listed = false;
-  for (int base = first; base - 8 * (int)threadIdx.x < hi; base += kHeld * 8 * kThreads) {
-    Eight<E> held[kHeld];
+  Eight<E> held[kHeld];
+  auto fetch = [&](int base) {
 #pragma unroll
     for (int j = 0; j < kHeld; ++j)
       if (base + j * 8 * kThreads < hi) load_eight<E>(p, base + j * 8 * kThreads, hi, held[j]);
-    if (!listed) load_list(a, n, s_ids, s_mark, lo, hi);
-    listed = true;
+  };
+  fetch(first);   // before the list, whose loads and barriers then cost nothing
+  load_list(a, n, s_ids, s_mark, lo, hi);
+  for (int base = first; base - 8 * (int)threadIdx.x < hi;) {
     // the list's entries out, then one maximum and one sum over all that are held
     float m = s.m;
 #pragma unroll
@@ -124,6 +128,8 @@ __global__ __launch_bounds__(kThreads) void k_distill_part(DistillCall a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) s.S += __expf(fmaf(held[j].at(e), a.scale, -ref));
     }
+    base += kHeld * 8 * kThreads;
+    fetch(base);   // a part that is longer than a thread holds
   }
   float m = s.m;
 #pragma unroll
@@ -151,35 +157,73 @@ __device__ __forceinline__ void wave_sum(double (&v)[N]) {
     for (int k = 32; k >= 1; k >>= 1) v[i] += __shfl_xor(v[i], k);
 }
 
-// The row's loss and state from the maximum and mass of its entries outside the list; one wave.
+// The row's loss and state, by one wave: from the maximum and mass of its parts' entries outside the list. Latency is
+// all of it: what needs no token is fetched at once, then the tokens' logits (1024 rows with a list of 64: 9.7 us, 12.5
+// with five waits for memory instead of two).
 template <class E>
-__device__ __forceinline__ void row_loss(const DistillCall& a, int n, MaxSum s, const int* s_ids, int lane) {
+__global__ __launch_bounds__(64) void k_distill_loss(DistillCall a) {
   constexpr int kEach = kMaxList / 64;
+  const int n = blockIdx.x, lane = threadIdx.x;
+  __shared__ __align__(16) int s_ids[kMaxList];
+  float weight = a.weight ? a.weight[n] : 1.f;
+  const float tref_given = a.lse ? a.lse[n] : 0.f;
+  float2 part = make_float2(-INFINITY, 0.f);   // (at most 64 parts a row)
+  if (lane < a.splits) part = a.partials[(long long)n * a.splits + lane];
+  float teacher[kEach];
+  int at[kEach];
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    const int j = lane + 64 * u;
+    at[u] = -1;
+    teacher[u] = 0.f;
+    if (j < a.k) {
+      at[u] = a.ids[(long long)n * a.k + j];
+      teacher[u] = teacher_at(a, (long long)n * a.k + j);
+    }
+  }
+  asm volatile("" : "+v"(weight), "+v"(part.x), "+v"(part.y), "+v"(at[0]), "+v"(teacher[0]));   // before the branch
+  if (weight == 0.f) {
+    if (lane == 0) {
+      a.loss[n] = 0.f;
+      *reinterpret_cast<RowState*>(a.state + (long long)n * RPD_DISTILL_STATE) = RowState{};
+    }
+    return;
+  }
   const typename E::t* p = row_of<E>(a, n);
   double t[kEach], z[kEach], pj[kEach];
-  int at[kEach];
   bool ok[kEach], first[kEach];
+  MaxSum s{part.x, 0.f};
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) s.m = fmaxf(s.m, __shfl_xor(s.m, k));
+  s.S = part.y * carry(part.x, ref_of(s.m, a.scale), a.scale);
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) s.S += __shfl_xor(s.S, k);
   double tmax = -INFINITY, sums[2] = {0.0, 0.0};   // teacher's, student's mass in the list
   float top = s.m;
 #pragma unroll
   for (int u = 0; u < kEach; ++u) {
-    const int j = lane + 64 * u;
-    const int v = j < a.k ? s_ids[j] : -1;
-    at[u] = v;
+    const int v = at[u];
+    s_ids[lane + 64 * u] = v;
     ok[u] = v >= 0 && v < a.V;
-    t[u] = ok[u] ? (double)teacher_at(a, (long long)n * a.k + j) * (double)a.scale : -INFINITY;
+    t[u] = ok[u] ? (double)teacher[u] * (double)a.scale : -INFINITY;
     const float zj = ok[u] ? E::one(p + v) : -INFINITY;
     z[u] = (double)zj * (double)a.scale;
     tmax = fmax(tmax, t[u]);
     top = fmaxf(top, zj);
     first[u] = ok[u];
   }
+  __syncthreads();
   // a token listed twice is in the list once
-#pragma unroll 4
-  for (int i = 0; i < a.k; ++i) {
-    const int v = s_ids[i];
 #pragma unroll
-    for (int u = 0; u < kEach; ++u) first[u] &= !(i < lane + 64 * u && v == at[u]);
+  for (int u = 0; u < kEach; ++u) {
+    const int j = lane + 64 * u;
+    if (64 * u >= a.k) continue;
+#pragma unroll 4
+    for (int i = 0; i < min(a.k, 64 * u + 64); i += 4) {
+      const int4 v = four_of(s_ids, i);
+      first[u] &= !((v.x == at[u] && i < j) || (v.y == at[u] && i + 1 < j) || (v.z == at[u] && i + 2 < j) ||
+                    (v.w == at[u] && i + 3 < j));
+    }
   }
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
@@ -192,7 +236,7 @@ __device__ __forceinline__ void row_loss(const DistillCall& a, int n, MaxSum s, 
   }
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) tmax = fmax(tmax, __shfl_xor(tmax, k));
-  const float tref = a.lse ? a.lse[n] : (float)(tmax == -INFINITY ? 0.0 : tmax);
+  const float tref = a.lse ? tref_given : (float)(tmax == -INFINITY ? 0.0 : tmax);
 #pragma unroll
   for (int u = 0; u < kEach; ++u) {
     pj[u] = 0.0;
@@ -217,7 +261,7 @@ __device__ __forceinline__ void row_loss(const DistillCall& a, int n, MaxSum s, 
   if (lane != 0) return;
   if (rest > 0.0) l[0] += rest * (log(rest) - (log((double)s.S) + drop - ln_S));
   const double P = (none ? 0.0 : sums[0] * tinv) + rest;
-  a.loss[n] = none ? 0.f : (float)((a.weight ? (double)a.weight[n] : 1.0) * l[0]);
+  a.loss[n] = none ? 0.f : (float)((double)weight * l[0]);
   RowState st;
   st.ref = ref;
   st.in = (float)(P / S);
@@ -229,48 +273,35 @@ __device__ __forceinline__ void row_loss(const DistillCall& a, int n, MaxSum s, 
   *reinterpret_cast<RowState*>(a.state + (long long)n * RPD_DISTILL_STATE) = st;
 }
 
-template <class E>
-__global__ __launch_bounds__(64) void k_distill_loss(DistillCall a) {
-  const int n = blockIdx.x, lane = threadIdx.x;
-  if (skipped(a, n)) {
-    if (lane == 0) {
-      a.loss[n] = 0.f;
-      *reinterpret_cast<RowState*>(a.state + (long long)n * RPD_DISTILL_STATE) = RowState{};
-    }
-    return;
-  }
-  __shared__ int s_ids[kMaxList];
-  load_list(a, n, s_ids, nullptr, 0, 0);
-  float m = -INFINITY, S = 0.f;
-  for (int i = lane; i < a.splits; i += 64) m = fmaxf(m, a.partials[(long long)n * a.splits + i].x);
-#pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
-  const float ref = ref_of(m, a.scale);
-  for (int i = lane; i < a.splits; i += 64) {
-    const float2 v = a.partials[(long long)n * a.splits + i];
-    S += v.y * carry(v.x, ref, a.scale);
-  }
-#pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) S += __shfl_xor(S, k);
-  row_loss<E>(a, n, MaxSum{m, S}, s_ids, lane);
-}
-
 // The part [lo, hi) of a row's gradient: the formula of the entries outside the list everywhere, then those in the
-// list over it. Streamed past the caches, which keep the logits between the loss and the gradient (1024 rows of
-// 126464 bf16, three quarters of them read: 50 us for the sums and 75 here, 64 and 77 with ordinary stores).
+// list over it. Streamed past the caches, which keep the logits between the loss and the gradient. 1024 rows of 126464
+// bf16, three quarters of them read: 42 us for the sums and 70 here (452 MB: 6.5 TB/s); with ordinary stores the sums
+// take 14 us more, this 2.
 template <class E>
-__device__ __forceinline__ void row_grad(const DistillCall& a, int n, int lo, int hi, const RowState& st,
-                                         const int* s_ids) {
+__device__ __forceinline__ void row_grad(const DistillCall& a, int n, int lo, int hi, const RowState& st) {
   typedef typename E::t T;
   const T* p = row_of<E>(a, n);
   T* g = static_cast<T*>(a.grad) + n * a.grad_stride;
   const float c = (a.weight ? a.weight[n] : 1.f) * (a.up ? a.up[n] : 1.f) * a.scale, co = c * st.out;
   const int first = lo + 8 * threadIdx.x;
-  for (int base = first; base < hi; base += kHeld * 8 * kThreads) {
-    Eight<E> held[kHeld];
+  Eight<E> held[kHeld];
+  auto fetch = [&](int base) {
 #pragma unroll
     for (int j = 0; j < kHeld; ++j)
       if (base + j * 8 * kThreads < hi) load_eight<E>(p, base + j * 8 * kThreads, hi, held[j]);
+  };
+  fetch(first);
+  // a thread's entry of the list (kMaxList is no more than the threads), and its logits
+  __shared__ __align__(16) int s_ids[kMaxList];
+  load_list(a, n, s_ids, nullptr, 0, 0);
+  const int mine = threadIdx.x, v = mine < a.k ? s_ids[mine] : -1;
+  const bool here = v >= lo && v < hi;
+  float zv = 0.f, tv = 0.f;
+  if (here) {
+    zv = E::one(p + v);
+    tv = teacher_at(a, (long long)n * a.k + mine);
+  }
+  for (int base = first; base < hi;) {
 #pragma unroll
     for (int j = 0; j < kHeld; ++j) {
       const int i = base + j * 8 * kThreads;
@@ -285,21 +316,26 @@ __device__ __forceinline__ void row_grad(const DistillCall& a, int n, int lo, in
         for (int e = 0; e < hi - i; ++e) g[i + e] = E::to(d[e]);
       }
     }
+    base += kHeld * 8 * kThreads;
+    fetch(base);
   }
   __syncthreads();
-  for (int j = threadIdx.x; j < a.k; j += kThreads) {
-    const int v = s_ids[j];
-    if (v < lo || v >= hi) continue;
-    double pv = 0.0;
-    bool first_of = true;
-    for (int i = 0; i < a.k; ++i)
-      if (s_ids[i] == v) {
-        first_of &= i >= j;
-        pv += exp((double)teacher_at(a, (long long)n * a.k + i) * (double)a.scale - (double)st.tref);
+  if (!here) return;
+  // the teacher's probability, of a token listed twice their sum, written once
+  double pv = 0.0;
+  bool first_of = true;
+#pragma unroll 4
+  for (int i = 0; i < a.k; i += 4) {
+    const int4 q = four_of(s_ids, i);
+    if (q.x != v && q.y != v && q.z != v && q.w != v) continue;
+    for (int e = i; e < i + 4; ++e)
+      if (s_ids[e] == v) {
+        first_of &= e >= mine;
+        const float t = e == mine ? tv : teacher_at(a, (long long)n * a.k + e);
+        pv += exp((double)t * (double)a.scale - (double)st.tref);
       }
-    if (first_of)
-      g[v] = E::to(c * (st.in * __expf(fmaf(E::one(p + v), a.scale, -st.ref)) - (float)(pv * (double)st.tinv)));
   }
+  if (first_of) g[v] = E::to(c * (st.in * __expf(fmaf(zv, a.scale, -st.ref)) - (float)(pv * (double)st.tinv)));
 }
 template <class E>
 __device__ __forceinline__ void row_zero(const DistillCall& a, int n, int lo, int hi) {
@@ -320,11 +356,9 @@ template <class E>
 __global__ __launch_bounds__(kThreads) void k_distill_grad(DistillCall a) {
   const int n = blockIdx.x / a.splits, split = blockIdx.x - n * a.splits;
   const int lo = split * a.chunk, hi = min(a.V, lo + a.chunk);
-  __shared__ int s_ids[kMaxList];
   const RowState st = *reinterpret_cast<const RowState*>(a.state + (long long)n * RPD_DISTILL_STATE);
   if (skipped(a, n) || st.any == 0.f) return row_zero<E>(a, n, lo, hi);   // such a row is not read
-  load_list(a, n, s_ids, nullptr, 0, 0);
-  row_grad<E>(a, n, lo, hi, st, s_ids);
+  row_grad<E>(a, n, lo, hi, st);
 }
 
 template <class E>

@@ -215,15 +215,12 @@ struct Row {
   double S;
 };
 __device__ __forceinline__ Row row_stats(const VerifyCall& a, long long row, float scale, int lane) {
-  float m = -INFINITY;
-  for (int i = lane; i < a.splits; i += 64) m = fmaxf(m, a.stats[row * a.splits + i].m);
+  RowPart v{0.0, -INFINITY, 0};   // (at most 64 parts a row)
+  if (lane < a.splits) v = a.stats[row * a.splits + lane];
+  float m = v.m;
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
-  double S = 0.0;
-  for (int i = lane; i < a.splits; i += 64) {
-    const RowPart v = a.stats[row * a.splits + i];
-    S += v.m == -INFINITY ? v.S : v.S * exp(((double)v.m - (double)m) * (double)scale);
-  }
+  double S = v.m == -INFINITY ? v.S : v.S * exp(((double)v.m - (double)m) * (double)scale);
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) S += __shfl_xor(S, k);
   return Row{m, S};
@@ -557,13 +554,10 @@ __global__ __launch_bounds__(kDecideWaves * 64) void k_verify_greedy(VerifyCall 
   __syncthreads();
   int mine = INT_MAX, best = -1;
   for (int t = wid; t <= len; t += kDecideWaves) {
-    float m = -INFINITY;
-    int idx = INT_MAX;
-    for (int i = lane; i < a.splits; i += 64) {
-      const RowPart v = a.stats[((long long)b * (a.T + 1) + t) * a.splits + i];
-      idx = v.m > m ? v.idx : v.m < m ? idx : min(idx, v.idx);
-      m = fmaxf(m, v.m);
-    }
+    RowPart v{0.0, -INFINITY, INT_MAX};
+    if (lane < a.splits) v = a.stats[((long long)b * (a.T + 1) + t) * a.splits + lane];
+    float m = v.m;
+    int idx = v.idx;
 #pragma unroll
     for (int k = 32; k >= 1; k >>= 1) {
       const float om = __shfl_xor(m, k);

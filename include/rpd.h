@@ -408,7 +408,7 @@ size_t rpd_quant_workspace_size(const rpd_quant_head* h, int32_t M, int32_t stat
  * M rows through the head: logits y = W x, or the softmax statistics of
  * logit_scale * y as rpd_gate_commit takes them (the logits then never reach
  * memory). Exactly one of `logits` and the three statistics is given. Codes
- * are exact operands and sums are float32; x is exact up to 2^-28 of the
+ * are exact operands and sums are float32; x is exact up to 2^-39 of the
  * row's largest finite magnitude. Equal rows of the head give equal logits;
  * of equal logits the lowest index is the argmax.
  *   M          0 <= M <= 2^20 (0: nothing is done)
@@ -416,7 +416,8 @@ size_t rpd_quant_workspace_size(const rpd_quant_head* h, int32_t M, int32_t stat
  *   logits     device [M][V], rows logits_stride >= V apart, of type
  *              logits_dtype: dtype or RPD_DTYPE_F32; or NULL
  *   argmax, confidence, entropy   device [M] int32 / float / float (top
- *              probability, nats); all given or all NULL
+ *              probability, nats); all given or all NULL. A row of NaN has
+ *              argmax -1 and the others NaN
  *   logit_scale  finite and > 0, or 0 for 1; the statistics only
  *   workspace  rpd_quant_workspace_size bytes, 256-byte aligned (may be NULL
  *              where that is 0); its prior contents do not matter
@@ -461,8 +462,9 @@ rpd_status rpd_quant_project(const rpd_quant_head* h, const void* packed, int32_
  *   n_accept   device [B] int32
  *   accept     device [B][T] float32 (greedy: 1 or 0); 0 for t >= len; NaN
  *              where p_t or q_t has no distribution or both are 0 at x_t
- * Acceptance probabilities carry float32 sums; the drawn token's sums are
- * float64.
+ * Acceptance probabilities carry sums of float32 accuracy, or of float64 where
+ * the rows are few; the drawn token's sums are float64. Outputs must not
+ * overlap the inputs.
  */
 typedef struct rpd_verify {
   int32_t B, T, V, dtype;
@@ -499,7 +501,7 @@ rpd_status rpd_verify_draft(const rpd_verify* p, void* workspace, size_t workspa
  *   loss[n] = weight[n] * (sum_j p_j ln(p_j / q_j) + p_T ln(p_T / q_T))
  *   grad[n] = weight[n] * grad_loss[n] * d loss_n / d logits[n]
  * Rows are independent (the masked positions of a canvas, say).
- *   N, V, k    0 <= N <= 2^24 (0: nothing is done), 1 <= V <= 2^20,
+ *   N, V, k    0 <= N < 2^24 (0: nothing is done), 1 <= V <= 2^20,
  *              1 <= k <= RPD_DISTILL_MAX_K; together bounded by what one launch
  *              holds (logits of 100 GB are far below that)
  *   dtype      of logits and grad: RPD_DTYPE_BF16, _F16 or _F32
@@ -517,7 +519,8 @@ rpd_status rpd_verify_draft(const rpd_verify* p, void* workspace, size_t workspa
  *   loss       device [N] float32
  *   state      device [N][RPD_DISTILL_STATE] float32: what the gradient needs
  *              of the loss
- *   grad       device [N][V], rows grad_stride >= V apart
+ *   grad       device [N][V], rows grad_stride >= V apart; not the logits'
+ *              memory
  * A list without entries (or of probability 0 without teacher_lse) has loss
  * and gradient 0. A list token of student probability 0 makes the loss inf.
  */

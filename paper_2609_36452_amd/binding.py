@@ -583,8 +583,9 @@ class QuantHead:
 
     codes uint8 [V][d/2] (column 2j in the low nibble of byte j, 2j+1 in the high one), scales [V][ceil(d/group)]
     bfloat16 or float16, optional zeros uint8 of the same shape (values 0..15; 8 everywhere without). Packs them once
-    into ``packed`` on the current stream; the inputs are not kept. Calls on another stream than that one wait for it
-    as for any tensor of the caller's (``stream.wait_stream``)."""
+    into ``packed`` on the current stream; the inputs are not kept. Outputs and workspaces of the calls are made on
+    the current stream as well: another one that is given as ``stream`` has to wait for it beforehand
+    (``stream.wait_stream``), as for any tensor of the caller's."""
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor | None = None,
                  group: int = 128):
@@ -716,7 +717,8 @@ def verify_draft(target_logits: torch.Tensor, draft_token: torch.Tensor, u: torc
                  draft_len: torch.Tensor | None = None, target_scale: float = 1.0, draft_scale: float = 1.0,
                  greedy: bool = False, stream=None) -> dict:
     """``rpd_verify_draft``: drafted tokens against a target's logits, from given random numbers (see
-    ``VerifyDraft``). Returns token, n_accept and accept, valid once the stream has run."""
+    ``VerifyDraft``). Returns token, n_accept and accept, valid once the stream has run; a ``stream`` other than the
+    current one, on which they are made, has to wait for it beforehand."""
     call = VerifyDraft(target_logits, draft_token, u, r, draft_logits, draft_len, target_scale, draft_scale, greedy)
     if stream is not None:
         call.workspace.record_stream(stream)
@@ -789,7 +791,8 @@ def distill(logits: torch.Tensor, teacher_id: torch.Tensor, teacher_logit: torch
 
     logits [..., V] (bfloat16, float16 or float32), teacher_id int32 [..., k] (entries outside 0..V-1 are no part of
     the list), teacher_logit [..., k], optional teacher_lse and weight float32 [...]. Returns float32 [...],
-    differentiable once in ``logits`` (the teacher and the weights are constants)."""
+    differentiable once in ``logits`` (the teacher and the weights are constants). A backward pass that is captured into
+    a graph must not meet leaves that an earlier backward pass outside it still refers to (as for any torch function)."""
     return _Distill.apply(logits, teacher_id, teacher_logit, teacher_lse, weight, float(logit_scale))
 
 
@@ -798,7 +801,8 @@ def distill_grad(logits: torch.Tensor, teacher_id: torch.Tensor, teacher_logit: 
                  grad_loss: torch.Tensor | None = None, logit_scale: float = 1.0,
                  stream=None) -> tuple[torch.Tensor, torch.Tensor]:
     """Loss and gradient in one call, for a training step that knows the upstream gradient ``grad_loss`` (float32
-    [...], 1 if None) beforehand: (loss [...], gradient [..., V] of ``logits``'s type). Not recorded by autograd."""
+    [...], 1 if None) beforehand: (loss [...], gradient [..., V] of ``logits``'s type). Not recorded by autograd.
+    ``stream`` as in ``verify_draft``."""
     logits = logits.detach()
     p = _distill_problem(logits, teacher_id, teacher_logit, teacher_lse, weight, logit_scale)
     if grad_loss is not None:

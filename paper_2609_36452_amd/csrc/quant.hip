@@ -18,10 +18,11 @@
 // masking and setting the exponent being one.
 // bf16 rows become fp16 by a power of two per row (the largest finite |x| comes
 // to 2^14..2^15): their 8 bits fit, and an element so small that it falls among
-// fp16's subnormals is off by at most 2^-40 of the row's largest, far below
+// fp16's subnormals is off by at most 2^-39 of the row's largest, far below
 // what fp32 accumulation keeps. Sums are fp32: within a group on the matrix
 // cores, then scaled, then over groups, then over waves, in a fixed order that
 // is the same for every vocabulary row (equal rows give equal logits).
+#include <climits>
 #include <cstdint>
 
 #include "reduce_device.h"
@@ -500,7 +501,7 @@ __global__ __launch_bounds__(64) void k_quant_stats(QuantCall a) {
   float4 keep[8];
   const Soft st = wave_merge_row(a.partials + (long long)m * a.slots, a.slots, lane, keep);
   if (lane == 0) {
-    a.argmax[m] = st.idx;
+    a.argmax[m] = st.idx == INT_MAX ? -1 : st.idx;   // a row of NaN has none
     a.confidence[m] = 1.f / st.S;
     a.entropy[m] = logf(st.S) - st.T / st.S;
   }

@@ -124,8 +124,9 @@ VerifyPlan verify_plan(const rpd_verify* p) {
   // statistics, as long as the launch fills the GPU's workgroups twice over, longer ones of up to 8192, which a
   // thread holds in registers (a workgroup's start and merges cost about as much as 2048 entries).
   v.part = (int)up_div(up_div(p->V, 64), 2048) * 2048;
-  v.parts = (int)up_div(p->V, v.part);
   v.chunk = v.part;
+  while (p->B * up_div(p->V, v.part) > kMaxBlocks) v.part *= 2;   // so many sequences that a launch holds no more
+  v.parts = (int)up_div(p->V, v.part);
   while (v.chunk < 8192 && v.rows * up_div(p->V, 2 * v.chunk) >= kFill) v.chunk *= 2;
   v.splits = (int)up_div(p->V, v.chunk);
   v.picks = round256((size_t)v.rows * v.splits * sizeof(rpd::RowPart));
@@ -140,7 +141,7 @@ VerifyPlan verify_plan(const rpd_verify* p) {
 // ---------------------------------------------------------------- distill --
 
 bool distill_shape_ok(const rpd_distill* p) {
-  return p->N >= 0 && p->N <= 1 << 24 && p->V >= 1 && p->V <= 1 << 20 && p->k >= 1 && p->k <= RPD_DISTILL_MAX_K;
+  return p->N >= 0 && p->N < 1 << 24 && p->V >= 1 && p->V <= 1 << 20 && p->k >= 1 && p->k <= RPD_DISTILL_MAX_K;
 }
 
 struct DistillPlan {
@@ -161,7 +162,7 @@ DistillPlan distill_plan(const rpd_distill* p) {
 rpd_status check_distill(const rpd_distill* p, bool grad) {
   if (!p) return fail(RPD_ERR_NULL_POINTER, "problem is NULL");
   if (!distill_shape_ok(p))
-    return fail(RPD_ERR_BAD_SHAPE, "need 0<=N<=2^24, 1<=V<=2^20, 1<=k<=%d (got N=%d V=%d k=%d)", RPD_DISTILL_MAX_K, p->N,
+    return fail(RPD_ERR_BAD_SHAPE, "need 0<=N<2^24, 1<=V<=2^20, 1<=k<=%d (got N=%d V=%d k=%d)", RPD_DISTILL_MAX_K, p->N,
                 p->V, p->k);
   if (!is_float_dtype(p->dtype) || !is_float_dtype(p->teacher_dtype))
     return fail(RPD_ERR_UNSUPPORTED, "dtype %d / teacher_dtype %d is not supported", p->dtype, p->teacher_dtype);
@@ -174,6 +175,7 @@ rpd_status check_distill(const rpd_distill* p, bool grad) {
   if (p->N == 0) return RPD_OK;
   if (!p->logits || !p->id || !p->teacher || !p->state || (grad && !p->grad))
     return fail(RPD_ERR_NULL_POINTER, "logits, id, teacher, state%s are required", grad ? " and grad" : "");
+  if (grad && p->grad == p->logits) return fail(RPD_ERR_BAD_PARAM, "grad must not be the logits' memory");
   const unsigned e = elem_align(p->dtype);
   if (misaligned(p->logits, e) || misaligned(p->grad, e) || misaligned(p->teacher, elem_align(p->teacher_dtype)) ||
       misaligned(p->id, 3) || misaligned(p->teacher_lse, 3) || misaligned(p->weight, 3) ||
@@ -334,8 +336,7 @@ rpd_status rpd_verify_draft(const rpd_verify* p, void* workspace, size_t workspa
       misaligned(p->accept, 3))
     return fail(RPD_ERR_UNSUPPORTED, "a pointer is not aligned to its element");
   const VerifyPlan v = verify_plan(p);
-  if (v.rows * v.splits > kMaxBlocks || (!greedy && (long long)p->B * v.parts > kMaxBlocks))
-    return fail(RPD_ERR_BAD_SHAPE, "B * T * V is too large");
+  if (v.rows * v.splits > kMaxBlocks) return fail(RPD_ERR_BAD_SHAPE, "B * T * V is too large");
   rpd_status st = check_workspace(workspace, workspace_bytes, v.bytes);
   if (st != RPD_OK) return st;
   rpd::VerifyCall a{};

@@ -107,6 +107,22 @@ def test_quant_rows_keep_to_themselves():
     assert torch.equal(y[6], plain[6] * 2.0 ** 100) and torch.equal(y[7], plain[7] * 2.0 ** -100)
 
 
+@pytest.mark.parametrize("M", [9, 24])
+def test_quant_statistics_of_broken_rows(M):
+    codes, scales, _ = R.make_head(700, 264, 64, BF, False, 7, DEV)
+    head = rpd.QuantHead(codes, scales, group=64)
+    x = _x(M, 264, BF, 10)
+    plain = head.stats(x)
+    x[2, 5] = math.nan
+    x[4, 7] = math.inf
+    got = head.stats(x)
+    assert int(got["argmax"][2]) == -1
+    assert all(bool(got[k][m].isnan()) for k, m in (("confidence", 2), ("entropy", 2), ("entropy", 4)))
+    keep = [m for m in range(M) if m not in (2, 4)]
+    for k in plain:
+        assert torch.equal(got[k][keep], plain[k][keep])
+
+
 def test_quant_out_of_wider_rows_and_nothing_beside_them():
     codes, scales, _ = R.make_head(333, 128, 32, HF, False, 8, DEV)
     head = rpd.QuantHead(codes, scales, group=32)
@@ -500,3 +516,141 @@ def test_operators_together():
     loss.sum().backward()
     ref = R.distill(q[0].cpu(), ids[0].int().cpu(), top[0].cpu(), lse[0].cpu(), mask[0, :T].float().cpu())
     _check_distill(loss[0], x.grad[0], ref, V)
+
+
+# ------------------------------------------------------------ long rows, far apart --
+
+def test_verify_parts_longer_than_a_workgroup_holds():
+    V = 1200007
+    c = _verify_case(1, 1, V, F32, True, False, 61)
+    d = [t.to(DEV) for t in c[:5]]
+    o = rpd.verify_draft(*d[:4], draft_logits=d[4])
+    _check_verify(o, R.verify(*c[:4], draft=c[4]), V)
+    o = rpd.verify_draft(*d[:2], greedy=True)
+    _check_verify(o, R.verify(*c[:2], None, None, greedy=True), V)
+
+
+def test_verify_many_short_sequences():
+    c = _verify_case(5000, 1, 7, HF, True, True, 62)
+    d = [t.to(DEV) for t in c]
+    o = rpd.verify_draft(*d[:4], draft_logits=d[4], draft_len=d[5])
+    _check_verify(o, R.verify(*c[:4], draft=c[4], lens=c[5]), 7)
+
+
+@pytest.mark.parametrize("V,dtype", [(1 << 20, BF), (700001, F32)])
+def test_distill_parts_longer_than_a_workgroup_holds(V, dtype):
+    c = _distill_case(2, V, 256, dtype, True, 63)
+    ref = R.distill(*c)
+    logits, ids, top, lse, weight, up = [t.to(DEV) for t in c]
+    loss, grad = rpd.distill_grad(logits, ids, top, teacher_lse=lse, weight=weight, grad_loss=up)
+    _check_distill(loss, grad, ref, V)
+
+
+def _apart(rows):
+    """The same rows more than 2^31 elements apart."""
+    n, step = rows.shape[-1], (1 << 31) + 8
+    far = torch.empty(((rows.shape[0] - 1) * step + n,), dtype=rows.dtype, device=DEV)
+    view = far.as_strided(rows.shape, (step, 1))
+    view.copy_(rows)
+    return view
+
+
+def test_rows_further_apart_than_32_bits():
+    codes, scales, _ = R.make_head(1003, 256, 64, BF, False, 64, DEV)
+    head = rpd.QuantHead(codes, scales, group=64)
+    x = _x(3, 256, BF, 65)
+    near = head.logits(x)
+    out = _apart(torch.zeros_like(near))
+    head.logits(_apart(x), out=out)
+    assert torch.equal(out, near)
+    del out
+    c = _verify_case(1, 2, 1003, BF, True, False, 66)
+    target, token, u, r, q = [t.to(DEV) for t in c[:5]]
+    want = rpd.verify_draft(target, token, u, r, draft_logits=q)
+    got = rpd.verify_draft(_apart(target[0])[None], token, u, r, draft_logits=_apart(q[0])[None])
+    for k in want:
+        assert torch.equal(got[k], want[k])
+    logits, ids, top, lse, weight, up = [t.to(DEV) for t in _distill_case(3, 1003, 16, BF, True, 67)]
+    a = (ids, top, lse, None, up)
+    for got, want in zip(rpd.distill_grad(_apart(logits), *a), rpd.distill_grad(logits, *a)):
+        assert torch.equal(got, want)
+
+
+# ---------------------------------------------------------------- calls of no rows --
+
+def test_no_rows():
+    codes, scales, _ = R.make_head(100, 64, 32, HF, False, 68, DEV)
+    head = rpd.QuantHead(codes, scales, group=32)
+    x = torch.empty((2, 0, 64), dtype=HF, device=DEV)
+    assert head.logits(x).shape == (2, 0, 100)
+    assert all(v.shape == (2, 0) for v in head.stats(x).values())
+    logits = torch.empty((0, 50), dtype=F32, device=DEV, requires_grad=True)
+    loss = rpd.distill(logits, torch.empty((0, 4), dtype=torch.int32, device=DEV), torch.empty((0, 4), device=DEV))
+    grad, = torch.autograd.grad(loss.sum(), logits)
+    assert loss.shape == (0,) and grad.shape == (0, 50)
+
+
+# ------------------------------------------------------------------------ autograd --
+
+def test_distill_backward_from_saved_tensors_that_moved():
+    """A strided view saved on the host comes back dense, at another address."""
+    wide = _rows(torch.Generator().manual_seed(69), (6,), 1500, BF).to(DEV)
+    _, ids, top, lse, weight, up = [t.to(DEV) for t in _distill_case(6, 999, 10, BF, True, 70)]
+    _, want = rpd.distill_grad(wide[:, :999], ids, top, lse, weight, up)
+    x = wide[:, :999].detach().requires_grad_(True)
+    with torch.autograd.graph.save_on_cpu():
+        loss = rpd.distill(x, ids, top, lse, weight)
+    grad, = torch.autograd.grad(loss, x, up)
+    assert torch.equal(grad, want)
+
+
+def test_distill_forward_and_backward_in_a_graph():
+    """Captured with gradients by autograd; every replay on new logits equals the eager call, which runs between."""
+    _, ids, top, lse, weight, up = [t.to(DEV) for t in _distill_case(7, 2500, 12, F32, True, 71)]
+    x = torch.zeros((7, 2500), device=DEV, requires_grad=True)
+
+    def step():
+        loss = rpd.distill(x, ids, top, teacher_lse=lse, weight=weight)
+        return loss.detach(), torch.autograd.grad(loss, x, up)[0]
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):   # what the first backward pass sets up is not captured
+        step()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for seed in range(4):
+        with torch.no_grad():
+            x.copy_(_rows(torch.Generator().manual_seed(seed), (7,), 2500, F32))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held]
+        for a, b in zip(got, rpd.distill_grad(x, ids, top, lse, weight, up)):
+            assert torch.equal(a, b)
+
+
+def test_two_streams_at_once():
+    """Calls that overlap on two streams, each with objects or workspaces of its own, over one packed head."""
+    codes, scales, _ = R.make_head(30011, 1024, 128, BF, False, 72, DEV)
+    head = rpd.QuantHead(codes, scales)
+    xs = [_x(24, 1024, BF, 73 + i) for i in range(2)]
+    cases = [[t.to(DEV) for t in _verify_case(6, 3, 30011, BF, True, False, 75 + i)[:5]] for i in range(2)]
+    calls = [rpd.VerifyDraft(*c[:4], draft_logits=c[4]) for c in cases]
+
+    def work(i):
+        o = calls[i]()
+        return [head.logits(xs[i]), *head.stats(xs[i]).values(), *[t.clone() for t in o.values()]]
+
+    want = [work(i) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(work(i))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for run in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(run, want[i]))

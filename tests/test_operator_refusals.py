@@ -96,8 +96,7 @@ def _verify(**kw):
     (dict(tb=-1), 2), (dict(dr=-1), 2), (dict(dtype=3), 5), (dict(flags=2), 3), (dict(ts=math.nan), 3),
     (dict(ds=-0.5), 3), (dict(ds=math.inf), 3), (dict(target=None), 1), (dict(token=None), 1), (dict(u=None), 1),
     (dict(r=None), 1), (dict(out=None), 1), (dict(n=None), 1), (dict(accept=None), 1), (dict(target=P + 1), 5),
-    (dict(token=P + 2), 5), (dict(dtype=1, draft=P + 2), 5), (dict(B=1 << 10, T=1000, V=1 << 28), 2),
-    (dict(B=1 << 20, T=0, V=100000), 2)])
+    (dict(token=P + 2), 5), (dict(dtype=1, draft=P + 2), 5), (dict(B=1 << 10, T=1000, V=1 << 28), 2)])
 def test_verify_refusals(kw, status):
     p = _verify(**kw)
     assert rpd.lib().rpd_verify_draft(ctypes.byref(p), P, 1 << 50, None) == status
@@ -115,9 +114,22 @@ def test_verify_workspace_refusals():
     assert L.rpd_verify_draft(None, P, n, None) == 1
 
 
+def test_verify_workspace_of_many_sequences():
+    """A launch holds fewer than 2^24 workgroups: the parts of a row grow with the sequences."""
+    L = rpd.lib()
+
+    def size(B):
+        return L.rpd_verify_workspace_size(ctypes.byref(_verify(B=B, T=0, V=32000, draft=None)))
+
+    # per sequence: 4 parts' statistics of 16 bytes, a pick of 32, and float64 sums of 2 rows and their totals in 16
+    # parts, or 8 where 16 of them are too many
+    assert size(1 << 19) == (1 << 19) * (4 * 16 + 32 + 2 * 16 * 16)
+    assert size(1 << 20) == (1 << 20) * (4 * 16 + 32 + 2 * 8 * 16)
+
+
 def _distill(**kw):
     a = dict(N=4, V=100, k=8, dtype=0, teacher_dtype=1, logits=P, logits_stride=100, id=P, teacher=P, teacher_lse=P,
-             weight=P, grad_loss=P, logit_scale=1.0, loss=P, state=P, grad=P, grad_stride=100)
+             weight=P, grad_loss=P, logit_scale=1.0, loss=P, state=P, grad=2 * P, grad_stride=100)
     a.update(kw)
     return rpd.RpdDistill(*a.values())
 
@@ -127,7 +139,8 @@ def _distill(**kw):
     (dict(k=257), 2), (dict(dtype=4), 5), (dict(teacher_dtype=-1), 5), (dict(logit_scale=math.nan), 3),
     (dict(logit_scale=-2.0), 3), (dict(logits_stride=99), 2), (dict(grad_stride=99), 2), (dict(logits=None), 1),
     (dict(id=None), 1), (dict(teacher=None), 1), (dict(state=None), 1), (dict(id=P + 2), 5), (dict(logits=P + 1), 5),
-    (dict(weight=P + 1), 5), (dict(N=1 << 24, V=1 << 20, logits_stride=1 << 20, grad_stride=1 << 20), 2)])
+    (dict(weight=P + 1), 5), (dict(grad=P), 3), (dict(N=1 << 24), 2),
+    (dict(N=(1 << 24) - 1, V=1 << 20, logits_stride=1 << 20, grad_stride=1 << 20), 2)])
 def test_distill_refusals(kw, status):
     L = rpd.lib()
     p = _distill(**kw)

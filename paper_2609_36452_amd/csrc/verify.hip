@@ -367,9 +367,9 @@ __global__ __launch_bounds__(kThreads) void k_verify_totals(VerifyCall a) {
 __device__ __forceinline__ void sampled_sums(const VerifyCall& a, int b, const VerifyPick& k, int lane, double& sp,
                                              double& sq) {
   double t[2] = {0.0, 0.0};
-  for (int i = lane; i < a.parts; i += 64)
 #pragma unroll
-    for (int c = 0; c < 2; ++c) t[c] += a.totals[((long long)c * a.B + b) * a.parts + i];
+  for (int c = 0; c < 2; ++c)
+    if (lane < a.parts) t[c] = a.totals[((long long)c * a.B + b) * a.parts + lane];   // (at most 64 parts)
 #pragma unroll
   for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -435,66 +435,46 @@ __device__ __forceinline__ double wave_scan(double v, int lane) {   // inclusive
 
 template <class E>
 __global__ __launch_bounds__(kThreads) void k_verify_token(VerifyCall a) {
-  const int b = blockIdx.x, n = a.n_accept[b], lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  const int b = blockIdx.x, lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  // everything that does not depend on the part, at once (at most 64 parts, a lane each)
+  const int n = a.n_accept[b];
   const VerifyPick k = a.picks[b];
-  __shared__ double s_table[32], s_wave[kWaves], s_left;
-  __shared__ int s_part, s_rest, s_token, s_last;
+  const float r = a.r[b];
+  double weight[2] = {0.0, 0.0};   // of p, of the draft's rest
+  if (lane < a.parts) {
+    weight[0] = a.sums[(long long)b * a.parts + lane];
+    weight[1] = a.sums[((long long)a.B + b) * a.parts + lane];
+  }
+  double sp = k.sp, sq = k.sq;
+  if (a.totals) sampled_sums(a, b, k, lane, sp, sq);
+  __shared__ double s_table[32], s_wave[kWaves];
+  __shared__ int s_token, s_last;
   fill_table(s_table);
-  if (wid == 0) {
-    // the part in which the running sum passes r of the whole (by rounding alone, the last that holds anything), a
-    // lane having `per` neighbouring parts; of the draft's rest, or where there is none of the target's row
-    const int per = (a.parts + 63) / 64, i0 = min(lane * per, a.parts), i1 = min(i0 + per, a.parts);
-    auto weight = [&](int i, bool rest) { return a.sums[((long long)rest * a.B + b) * a.parts + i]; };
-    bool rest = k.down;
-    double mine = 0.0, all = 0.0;
-    for (int attempt = 0; attempt < 2; ++attempt) {
-      mine = 0.0;
-      for (int i = i0; i < i1; ++i) mine += weight(i, rest);
-      mine = wave_scan(mine, lane);
-      all = __shfl(mine, 63);
-      if (!rest || all > 0.0) break;
-      rest = false;
-    }
-    const double at = (double)a.r[b] * all;
-    double before = __shfl_up(mine, 1);
-    if (lane == 0) before = 0.0;
-    int pick = INT_MAX, last = -1;
-    double pick_before = 0.0, last_before = 0.0;
-    if (all > 0.0 && all <= 1.7976931348623157e308)
-      for (int i = i0; i < i1; ++i) {
-        const double w = weight(i, rest);
-        if (w > 0.0) {
-          last = i;
-          last_before = before;
-          if (pick == INT_MAX && before + w > at) {
-            pick = i;
-            pick_before = before;
-          }
-        }
-        before += w;
-      }
-    // the first lane that has one, else the last part that holds anything
-    const unsigned long long hit = __ballot(pick != INT_MAX), any = __ballot(last >= 0);
-    const int from = hit ? __builtin_ctzll(hit) : any ? 63 - __builtin_clzll(any) : 0;
-    const int part = __shfl(hit ? pick : last, from);
-    const double pb = __shfl(hit ? pick_before : last_before, from);
-    if (lane == 0) {
-      s_part = part;
-      s_rest = rest;
-      s_left = at - pb;
-      s_token = INT_MAX;
-      s_last = -1;
-    }
+  if (threadIdx.x == 0) {
+    s_token = INT_MAX;
+    s_last = -1;
   }
   __syncthreads();
-  const int part = s_part;
+  // the part in which the running sum passes r of the whole (by rounding alone, the last that holds anything), by each
+  // wave; of the draft's rest, or where there is none of the target's row
+  bool use_rest = k.down;
+  double w_part = use_rest ? weight[1] : weight[0], scan = wave_scan(w_part, lane), all = __shfl(scan, 63);
+  if (use_rest && !(all > 0.0)) {
+    use_rest = false;
+    w_part = weight[0];
+    scan = wave_scan(w_part, lane);
+    all = __shfl(scan, 63);
+  }
+  const double at = (double)r * all;
+  double before_part = __shfl_up(scan, 1);
+  if (lane == 0) before_part = 0.0;
+  const bool some = all > 0.0 && all <= 1.7976931348623157e308 && w_part > 0.0;
+  const unsigned long long passed = __ballot(some && before_part + w_part > at), any = __ballot(some);
+  const int part = passed ? __builtin_ctzll(passed) : any ? 63 - __builtin_clzll(any) : -1;
+  const double left = at - __shfl(before_part, max(part, 0));
   if (part >= 0) {
     // the same inside the part, 2048 entries at a time
-    const bool use_rest = s_rest;
-    double sp = k.sp, sq = k.sq;
-    if (a.totals) sampled_sums(a, b, k, lane, sp, sq);
     const Rest<E> rest(a, b, n, k, sp, sq, s_table);
-    const double left = s_left;
     const int hi = min(a.V, (part + 1) * a.part);
     double done = 0.0;
     int last = -1;
@@ -514,10 +494,10 @@ __global__ __launch_bounds__(kThreads) void k_verify_token(VerifyCall a) {
         last = w[e] > 0.0 ? i + e : last;
         mine += w[e];
       }
-      const double scan = wave_scan(mine, lane);
-      if (lane == 63) s_wave[wid] = scan;
+      const double upto = wave_scan(mine, lane);
+      if (lane == 63) s_wave[wid] = upto;
       __syncthreads();
-      double before = done + (scan - mine);
+      double before = done + (upto - mine);
       for (int v = 0; v < kWaves; ++v) {
         before += v < wid ? s_wave[v] : 0.0;
         done += s_wave[v];

@@ -16,11 +16,11 @@
 //   k_verify_totals  float64 sums of that row (after float32 statistics)
 //   k_verify_parts   sums of max(0, p - q), and of p, over parts of that row
 //   k_verify_token   the part that r falls in, then the token in it
-// A launch that waits for the one before it takes 4 us however little it does.
-// 5 target and 4 draft rows of 126464 bf16: 16.9 us in three launches, 19.3
-// with the decision as a fourth. (A draw by the last workgroup to finish its
-// part needs no launch either, but the release and acquire cost 62 parts as
-// much as it, and 32 x 38 parts 14 us more.)
+// A launch that waits for the one before it takes 4 us however little it does:
+// 5 target and 4 draft rows of 126464 bf16 take 15.6 us in three launches, and
+// the decision as a fourth 2.4 us more. (A draw by the last workgroup to finish
+// its part needs no launch either, but the release and acquire cost 62 parts
+// as much as it, and 32 x 38 parts 14 us more.)
 // The draw is float64, exponentials included: the token's border lies among up
 // to V cumulative sums a few 1e-6 apart, and in float32 a draw in a hundred of
 // a flat row would fall on the neighbour of the right token. Few rows take
@@ -96,6 +96,18 @@ template <class E>
 __device__ __forceinline__ const typename E::t* draft_row(const VerifyCall& a, int b, int t) {
   return static_cast<const typename E::t*>(a.draft) + b * a.d_batch + t * a.d_row;
 }
+// 8 entries of a row from i on, -inf past `hi`
+template <class E>
+__device__ __forceinline__ void load_eight(const typename E::t* p, int i, int hi, Eight<E>& v) {
+  if (i + 8 <= hi) {
+    v.load(p + i);
+  } else {
+    float z[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = i + e < hi ? E::one(p + i + e) : -INFINITY;
+    v.set(z);
+  }
+}
 __device__ __forceinline__ int draft_len(const VerifyCall& a, int b) {
   return a.len ? min(max(a.len[b], 0), a.T) : a.T;
 }
@@ -118,16 +130,7 @@ __global__ __launch_bounds__(kThreads) void k_verify_stats(VerifyCall a) {
   // the part's first vectors are held, a longer part's others read again
   constexpr int kHeld = 4;
   Eight<E> held[kHeld];
-  auto get = [&](int i, Eight<E>& v) {
-    if (i + 8 <= hi) {
-      v.load(p + i);
-    } else {
-      float z[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = i + e < hi ? E::one(p + i + e) : -INFINITY;
-      v.set(z);
-    }
-  };
+  auto get = [&](int i, Eight<E>& v) { load_eight<E>(p, i, hi, v); };
   const int first = lo + 8 * threadIdx.x;
 #pragma unroll
   for (int j = 0; j < kHeld; ++j)
@@ -295,28 +298,30 @@ struct Rest {
                                   const double* table)
       : p(target_row<E>(a, b, n)), q(a.draft ? draft_row<E>(a, b, n) : nullptr), ep(k.mp, a.target_scale, table),
         eq(k.mq, a.draft_scale, table), ip(1.0 / sp), iq(1.0 / sq), x(k.x) {}
+  __device__ __forceinline__ void fetch(int i, int V, bool down, Eight<E>& vp, Eight<E>& vq) const {
+    load_eight<E>(p, i, V, vp);
+    if (down && q) load_eight<E>(q, i, V, vq);
+  }
   // p of the 8 entries from i on (0 past the row's end) and, of a token turned down, the rest
-  __device__ __forceinline__ void eight(int i, int V, bool down, double (&p8)[8], double (&w)[8]) const {
-    Eight<E> vp, vq;
-    const bool whole = i + 8 <= V;
-    if (whole) {
-      vp.load(p + i);
-      if (down && q) vq.load(q + i);
-    }
+  __device__ __forceinline__ void eight(int i, bool down, const Eight<E>& vp, const Eight<E>& vq, double (&p8)[8],
+                                        double (&w)[8]) const {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      p8[e] = w[e] = 0.0;
-      if (!whole && i + e >= V) continue;
-      p8[e] = ep(whole ? vp.at(e) : E::one(p + i + e)) * ip;
+      p8[e] = ep(vp.at(e)) * ip;
+      w[e] = 0.0;
       if (!down) continue;
       if (q)
-        w[e] = p8[e] - eq(whole ? vq.at(e) : E::one(q + i + e)) * iq;
+        w[e] = p8[e] - eq(vq.at(e)) * iq;
       else
         w[e] = i + e == x ? 0.0 : p8[e];
       w[e] = w[e] > 0.0 ? w[e] : 0.0;
     }
   }
 };
+
+// Vectors of a part that a thread has in flight: a part of 4096 entries is one round (rows of up to 262144; one vector
+// at a time, two in turn, takes 2 us more over three passes of 32 pairs of rows of 152064).
+constexpr int kFlight = 2;
 
 // Float64 sums over parts of the sampled rows, where the statistics are float32.
 template <class E>
@@ -331,21 +336,23 @@ __global__ __launch_bounds__(kThreads) void k_verify_totals(VerifyCall a) {
   const typename E::t* q = a.draft && k.down ? draft_row<E>(a, b, n) : nullptr;
   const int hi = min(a.V, (part + 1) * a.part);
   double sum[2] = {0.0, 0.0};
-  for (int i = part * a.part + 8 * threadIdx.x; i < hi; i += 8 * kThreads) {
-    if (i + 8 <= hi) {
-      Eight<E> vp, vq;
-      vp.load(p + i);
-      if (q) vq.load(q + i);
+  for (int i = part * a.part + 8 * threadIdx.x; i < hi; i += kFlight * 8 * kThreads) {
+    Eight<E> vp[kFlight], vq[kFlight];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[0] += ep.about(vp.at(e));
+    for (int u = 0; u < kFlight; ++u) {
+      const int at = i + u * 8 * kThreads;
+      if (at >= hi) continue;
+      load_eight<E>(p, at, hi, vp[u]);
+      if (q) load_eight<E>(q, at, hi, vq[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kFlight; ++u) {
+      if (i + u * 8 * kThreads >= hi) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[0] += ep.about(vp[u].at(e));
       if (q) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[1] += eq.about(vq.at(e));
-      }
-    } else {
-      for (int v = i; v < hi; ++v) {
-        sum[0] += ep.about(E::one(p + v));
-        if (q) sum[1] += eq.about(E::one(q + v));
+        for (int e = 0; e < 8; ++e) sum[1] += eq.about(vq[u].at(e));
       }
     }
   }
@@ -401,13 +408,21 @@ __global__ __launch_bounds__(DECIDE ? kDecideWaves * 64 : kThreads) void k_verif
   const Rest<E> rest(a, b, n, k, sp, sq, s_table);
   const int hi = min(a.V, (part + 1) * a.part);
   double sum[2] = {0.0, 0.0};
-  for (int i = part * a.part + 8 * threadIdx.x; i < hi; i += 8 * 64 * W) {
-    double p[8], w[8];
-    rest.eight(i, a.V, k.down, p, w);   // (a part ends at the row's end or at a whole vector)
+  for (int i = part * a.part + 8 * threadIdx.x; i < hi; i += kFlight * 8 * 64 * W) {
+    Eight<E> vp[kFlight], vq[kFlight];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      sum[0] += p[e];
-      sum[1] += w[e];
+    for (int u = 0; u < kFlight; ++u)   // (a part ends at the row's end or at a whole vector)
+      if (i + u * 8 * 64 * W < hi) rest.fetch(i + u * 8 * 64 * W, a.V, k.down, vp[u], vq[u]);
+#pragma unroll
+    for (int u = 0; u < kFlight; ++u) {
+      if (i + u * 8 * 64 * W >= hi) continue;
+      double p[8], w[8];
+      rest.eight(i + u * 8 * 64 * W, k.down, vp[u], vq[u], p, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        sum[0] += p[e];
+        sum[1] += w[e];
+      }
     }
   }
 #pragma unroll
@@ -478,13 +493,17 @@ __global__ __launch_bounds__(kThreads) void k_verify_token(VerifyCall a) {
     const int hi = min(a.V, (part + 1) * a.part);
     double done = 0.0;
     int last = -1;
+    Eight<E> vp, vq, next_p, next_q;
+    const int first = part * a.part + 8 * threadIdx.x;
+    if (first < hi) rest.fetch(first, a.V, use_rest, vp, vq);
     for (int i0 = part * a.part; i0 < hi; i0 += 8 * kThreads) {
       const int i = i0 + 8 * threadIdx.x;
       double p8[8], w[8], mine = 0.0;
       int hit = -1;
 #pragma unroll
       for (int e = 0; e < 8; ++e) p8[e] = w[e] = 0.0;
-      if (i < hi) rest.eight(i, a.V, use_rest, p8, w);
+      if (i + 8 * kThreads < hi) rest.fetch(i + 8 * kThreads, a.V, use_rest, next_p, next_q);
+      if (i < hi) rest.eight(i, use_rest, vp, vq, p8, w);
       if (!use_rest) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = p8[e];
@@ -513,6 +532,8 @@ __global__ __launch_bounds__(kThreads) void k_verify_token(VerifyCall a) {
       __syncthreads();
       if (s_token != INT_MAX) break;
       __syncthreads();
+      vp = next_p;
+      vq = next_q;
     }
     if (s_token == INT_MAX) {   // by rounding alone
 #pragma unroll

@@ -69,19 +69,6 @@ __device__ __forceinline__ void load_list(const DistillCall& a, int n, int* s_id
   __syncthreads();
 }
 
-// 8 entries of a row from i on, -inf past `hi`
-template <class E>
-__device__ __forceinline__ void load_eight(const typename E::t* p, int i, int hi, Eight<E>& v) {
-  if (i + 8 <= hi) {
-    v.load(p + i);
-  } else {
-    float z[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) z[e] = i + e < hi ? E::one(p + i + e) : -INFINITY;
-    v.set(z);
-  }
-}
-
 // maximum and mass of the entries of a part of a row outside the list
 template <class E>
 __global__ __launch_bounds__(kThreads) void k_distill_part(DistillCall a) {

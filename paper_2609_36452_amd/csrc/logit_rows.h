@@ -85,6 +85,19 @@ struct Eight<F32> {
   }
 };
 
+// 8 entries of a row from i on, -inf past `hi`
+template <class E>
+__device__ __forceinline__ void load_eight(const typename E::t* p, int i, int hi, Eight<E>& v) {
+  if (i + 8 <= hi) {
+    v.load(p + i);
+  } else {
+    float z[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = i + e < hi ? E::one(p + i + e) : -INFINITY;
+    v.set(z);
+  }
+}
+
 // Maximum m of the raw logits and S = sum e^(scale z - r) with r the rounded
 // product scale m: one fused rounding an exponent, so that any scale is as
 // exact as 1. Nothing seen: m = -inf, S = 0; a row that is -inf throughout

@@ -96,18 +96,6 @@ template <class E>
 __device__ __forceinline__ const typename E::t* draft_row(const VerifyCall& a, int b, int t) {
   return static_cast<const typename E::t*>(a.draft) + b * a.d_batch + t * a.d_row;
 }
-// 8 entries of a row from i on, -inf past `hi`
-template <class E>
-__device__ __forceinline__ void load_eight(const typename E::t* p, int i, int hi, Eight<E>& v) {
-  if (i + 8 <= hi) {
-    v.load(p + i);
-  } else {
-    float z[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) z[e] = i + e < hi ? E::one(p + i + e) : -INFINITY;
-    v.set(z);
-  }
-}
 __device__ __forceinline__ int draft_len(const VerifyCall& a, int b) {
   return a.len ? min(max(a.len[b], 0), a.T) : a.T;
 }

@@ -616,12 +616,14 @@ class QuantHead:
             raise ValueError(f"x has {x.shape[-1]} columns, the head {self.d}")
         return _rows("x", x)
 
-    def _workspace(self, M: int, statistics: int, stream) -> torch.Tensor:
-        ws = torch.empty(int(lib().rpd_quant_workspace_size(ctypes.byref(self.head), M, statistics)),
-                         dtype=torch.uint8, device=self.device)
+    def _workspace(self, M: int, statistics: int, stream) -> tuple[torch.Tensor | None, int]:
+        nbytes = int(lib().rpd_quant_workspace_size(ctypes.byref(self.head), M, statistics))
+        if nbytes == 0:
+            return None, 0
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         if stream is not None:
             ws.record_stream(stream)
-        return ws
+        return ws, nbytes
 
     def logits(self, x: torch.Tensor, out_dtype: torch.dtype | None = None, out: torch.Tensor | None = None,
                stream=None) -> torch.Tensor:
@@ -629,15 +631,17 @@ class QuantHead:
         r = self._x(x)
         if out is None:
             out = torch.empty((*x.shape[:-1], self.V), dtype=out_dtype or x.dtype, device=x.device)
-        elif tuple(out.shape) != (*x.shape[:-1], self.V) or (out_dtype and out.dtype != out_dtype):
-            raise ValueError(f"out has shape {tuple(out.shape)} and dtype {out.dtype}")
-        _one_device("out", out, x=x)
-        o = _rows("out", out)
+            out_stride = self.V
+        else:
+            if tuple(out.shape) != (*x.shape[:-1], self.V) or (out_dtype and out.dtype != out_dtype):
+                raise ValueError(f"out has shape {tuple(out.shape)} and dtype {out.dtype}")
+            _one_device("out", out, x=x)
+            out_stride = _row_stride(_rows("out", out))
         code = _float_code("out", out)
-        ws = self._workspace(r.shape[0], 0, stream)
+        ws, nbytes = self._workspace(r.shape[0], 0, stream)
         _enqueue(x.device, stream, lib().rpd_quant_project, ctypes.byref(self.head), self.packed.data_ptr(),
-                 r.shape[0], r.data_ptr(), _row_stride(r), o.data_ptr(), _row_stride(o), code, None, None, None, 1.0,
-                 ws.data_ptr(), ws.numel())
+                 r.shape[0], r.data_ptr(), _row_stride(r), out.data_ptr(), out_stride, code, None, None, None, 1.0,
+                 _ptr(ws), nbytes)
         return out
 
     def stats(self, x: torch.Tensor, logit_scale: float = 1.0, stream=None) -> dict:
@@ -648,10 +652,10 @@ class QuantHead:
         o = {"argmax": torch.empty(x.shape[:-1], dtype=torch.int32, **e),
              "confidence": torch.empty(x.shape[:-1], dtype=torch.float32, **e),
              "entropy": torch.empty(x.shape[:-1], dtype=torch.float32, **e)}
-        ws = self._workspace(r.shape[0], 1, stream)
+        ws, nbytes = self._workspace(r.shape[0], 1, stream)
         _enqueue(x.device, stream, lib().rpd_quant_project, ctypes.byref(self.head), self.packed.data_ptr(),
                  r.shape[0], r.data_ptr(), _row_stride(r), None, 0, 0, o["argmax"].data_ptr(),
-                 o["confidence"].data_ptr(), o["entropy"].data_ptr(), float(logit_scale), ws.data_ptr(), ws.numel())
+                 o["confidence"].data_ptr(), o["entropy"].data_ptr(), float(logit_scale), _ptr(ws), nbytes)
         return o
 
 

@@ -514,9 +514,11 @@ hipError_t project_z(const QuantDims& q, const QuantCall& a, hipStream_t s) {
                                   : k_quant_project<NC, MT, GPC, true, LONG, PRE, false>)
                         : (a.bf16 ? k_quant_project<NC, MT, GPC, false, LONG, PRE, true>
                                   : k_quant_project<NC, MT, GPC, false, LONG, PRE, false>);
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                     (int)lds);
-  if (e != hipSuccess) return e;
+  if (lds > 64 * 1024) {   // what a launch may have without asking
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
   kernel<<<a.slots * a.row_groups, a.waves * 64, lds, s>>>(q, a);
   return hipGetLastError();
 }

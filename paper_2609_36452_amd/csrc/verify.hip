@@ -205,13 +205,14 @@ struct Row {
   float m;
   double S;
 };
-__device__ __forceinline__ Row row_stats(const VerifyCall& a, long long row, float scale, int lane) {
+__device__ __forceinline__ Row row_stats(const VerifyCall& a, long long row, float scale, int lane,
+                                         const double* table) {
   RowPart v{0.0, -INFINITY, 0};   // (at most 64 parts a row)
   if (lane < a.splits) v = a.stats[row * a.splits + lane];
   float m = v.m;
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
-  double S = v.m == -INFINITY ? v.S : v.S * exp(((double)v.m - (double)m) * (double)scale);
+  double S = v.m == -INFINITY ? v.S : v.S * Exp64(m, scale, table)(v.m);
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) S += __shfl_xor(S, k);
   return Row{m, S};
@@ -226,10 +227,11 @@ struct Decision {
   int n;
 };
 template <class E, int WAVES>
-__device__ __forceinline__ void decide(const VerifyCall& a, int b, bool write, Decision& s) {
+__device__ __forceinline__ void decide(const VerifyCall& a, int b, bool write, Decision& s, double* table) {
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
   const int len = draft_len(a, b);
   if (threadIdx.x == 0) s.n = len;
+  fill_table(table);
   __syncthreads();
   const long long t0 = (long long)b * (a.T + 1), d0 = (long long)a.B * (a.T + 1) + (long long)b * a.T;
   int mine = INT_MAX;
@@ -241,14 +243,16 @@ __device__ __forceinline__ void decide(const VerifyCall& a, int b, bool write, D
     const bool valid = x >= 0 && x < a.V;
     const float zp = valid ? E::one(target_row<E>(a, b, t) + x) : -INFINITY;
     const float zq = valid && a.draft ? E::one(draft_row<E>(a, b, t) + x) : 0.f;
-    const Row p = row_stats(a, t0 + t, a.target_scale, lane);
+    const Row p = row_stats(a, t0 + t, a.target_scale, lane, table);
     Row q{0.f, 1.0};
-    if (a.draft && drafted) q = row_stats(a, d0 + t, a.draft_scale, lane);
+    if (a.draft && drafted) q = row_stats(a, d0 + t, a.draft_scale, lane, table);
     float acc = 0.f;
     if (drafted) {
-      double l = ((double)zp - (double)p.m) * (double)a.target_scale - log(p.S);
-      if (a.draft) l -= ((double)zq - (double)q.m) * (double)a.draft_scale - log(q.S);
-      acc = !valid ? 0.f : l > 0.0 ? 1.f : (float)exp(l);
+      // one exponential of both distances: the quotient overflows only where it is far above 1
+      double l = ((double)zp - (double)p.m) * (double)a.target_scale;
+      if (a.draft) l -= ((double)zq - (double)q.m) * (double)a.draft_scale;
+      const double quotient = exp(l) * (q.S / p.S);
+      acc = !valid ? 0.f : quotient > 1.0 ? 1.f : (float)quotient;
       if (write && lane == 0) a.accept[(long long)b * a.T + t] = acc;
     }
     if (mine == INT_MAX && !(drafted && u < acc)) {
@@ -271,7 +275,8 @@ constexpr int kDecideWaves = 8;
 template <class E>
 __global__ __launch_bounds__(kDecideWaves * 64) void k_verify_decide(VerifyCall a) {
   __shared__ Decision s;
-  decide<E, kDecideWaves>(a, blockIdx.x, true, s);
+  __shared__ double s_table[32];
+  decide<E, kDecideWaves>(a, blockIdx.x, true, s, s_table);
   if (threadIdx.x == 0) a.picks[blockIdx.x] = s.pick;
 }
 
@@ -381,12 +386,12 @@ __global__ __launch_bounds__(DECIDE ? kDecideWaves * 64 : kThreads) void k_verif
   const int part = blockIdx.x % a.parts, b = blockIdx.x / a.parts;
   __shared__ double s_sum[W][2], s_table[32];
   __shared__ Decision s;
-  fill_table(s_table);
   if (DECIDE) {
-    decide<E, W>(a, b, part == 0, s);
+    decide<E, W>(a, b, part == 0, s, s_table);
     if (part == 0 && threadIdx.x == 0) a.picks[b] = s.pick;
   } else {
     if (threadIdx.x == 0) s = Decision{a.picks[b], a.n_accept[b]};
+    fill_table(s_table);
     __syncthreads();
   }
   const VerifyPick k = s.pick;

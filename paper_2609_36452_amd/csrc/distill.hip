@@ -238,22 +238,24 @@ __global__ __launch_bounds__(64) void k_distill_loss(DistillCall a) {
   const double tinv = a.lse ? 1.0 : none ? 0.0 : 1.0 / sums[0];
   const double rest = a.lse ? fmax(0.0, 1.0 - sums[0]) : 0.0;   // NaN in the list shows in its own terms
   const double drop = s.S == 0.f ? 0.0 : (double)tail - (double)ref;   // S_T's exponent in units of S's
-  const double S = (double)s.S * exp(drop) + sums[1], ln_S = log(S);
+  const double e_drop = exp(drop), S = (double)s.S * e_drop + sums[1];
+  // four logarithms for the time of one
+  const double logs = log(lane == 0 ? S : lane == 1 ? tinv : lane == 2 ? rest : (double)s.S);
+  const double ln_S = __shfl(logs, 0), ln_tinv = __shfl(logs, 1), ln_rest = __shfl(logs, 2), ln_tail = __shfl(logs, 3);
   double l[1] = {0.0};
-  const double ln_tinv = a.lse ? 0.0 : log(tinv);
 #pragma unroll
   for (int u = 0; u < kEach; ++u)
     if (pj[u] != 0.0) l[0] += pj[u] * tinv * ((t[u] + ln_tinv) - (z[u] - ln_S));
   wave_sum(l);
   if (lane != 0) return;
-  if (rest > 0.0) l[0] += rest * (log(rest) - (log((double)s.S) + drop - ln_S));
+  if (rest > 0.0) l[0] += rest * (ln_rest - (ln_tail + drop - ln_S));
   const double P = (none ? 0.0 : sums[0] * tinv) + rest;
   a.loss[n] = none ? 0.f : (float)((double)weight * l[0]);
   RowState st;
   st.ref = ref;
   st.in = (float)(P / S);
   st.tail = tail;
-  st.out = (float)(P * exp(drop) / S - (rest > 0.0 ? rest / (double)s.S : 0.0));
+  st.out = (float)(P * e_drop / S - (rest > 0.0 ? rest / (double)s.S : 0.0));
   st.tref = tref;
   st.tinv = (float)tinv;
   st.any = none ? 0.f : 1.f;

@@ -17,7 +17,7 @@
 //   k_verify_parts   sums of max(0, p - q), and of p, over parts of that row
 //   k_verify_token   the part that r falls in, then the token in it
 // A launch that waits for the one before it takes 4 us however little it does:
-// 5 target and 4 draft rows of 126464 bf16 take 15.6 us in three launches, and
+// 5 target and 4 draft rows of 126464 bf16 take 15.2 us in three launches, and
 // the decision as a fourth 2.4 us more. (A draw by the last workgroup to finish
 // its part needs no launch either, but the release and acquire cost 62 parts
 // as much as it, and 32 x 38 parts 14 us more.)

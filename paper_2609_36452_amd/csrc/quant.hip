@@ -4,6 +4,9 @@
 //
 // Bound: one stream of the packed codes from HBM (half a byte a weight). What
 // has to keep up with it is turning codes into matrix operands and feeding x.
+// 4096 columns, V = 126464 (267 MB): 44 us for one row (6.1 TB/s); 54-59 for 32
+// rows, where converting the codes and the products take as long as the stream;
+// 96-100 for 64 rows, which convert them twice.
 //
 // x stays: the waves of a workgroup divide the columns among them, each keeps
 // the fp16 fragments of its columns of all rows in registers, and only the
@@ -126,11 +129,11 @@ __device__ __forceinline__ typename Raw<N>::t load_bits(char* base, int range, u
 // 1024 + 16 q: one mask-and-or each, one subtraction or multiply-add for a
 // pair, one shift for the other two pairs. masks: 0x000f000f and 0x00f000f0,
 // one: 1024 in both halves, in registers (as literals they do not fit into one
-// instruction: 107.6 us instead of 96.2 at 32 rows). As subnormals, q 2^-24,
+// instruction: 107.6 us instead of 96.2 at 64 rows). As subnormals, q 2^-24,
 // the codes would need no subtraction, 5 instructions, and the zero points a
 // correction by the sums of x; but the matrix cores keep fewer bits of such
 // products: logits were off by 4e-6 of their size, 1e-7 so, for 4% of the time
-// at 32 rows.
+// at 64 rows.
 __device__ __forceinline__ f16x8 decode(uint32_t w, f16x2 zl, f16x2 zh, uint32_t mask_low, uint32_t mask_high,
                                         uint32_t one) {
   const f16x2 sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};

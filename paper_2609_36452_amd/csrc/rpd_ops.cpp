@@ -57,7 +57,13 @@ rpd::QuantDims quant_dims(const rpd_quant_head* h) {
 }
 
 // Workgroups of up to 16 waves, each wave keeping the x of 1, 2 or 4 chunks of
-// 128 columns in registers; longer rows take several rounds and reload x.
+// 128 columns in registers; longer rows take several rounds and reload x. Rows
+// of V = 126464 bf16, us: 4096 columns with 16 waves 43.4 (1 row) and 51.0 (16
+// rows), with 8 waves of twice the chunks 44.3 and 54.2 (2048 columns: 26.8 and
+// 31.1, 25.9 and 30.0). More than 16 rows share converted codes between two
+// tiles of 16 as long as their x fits the registers: 32 rows of 4096 columns
+// 63.4, of 2048 41.0, and 77.1 and 49.4 as row groups of 16; 64 rows 102.8 and
+// 132.7.
 void quant_plan(const rpd::QuantDims& q, rpd::QuantCall& a) {
   a.nc_wave = q.nc <= 16 ? 1 : q.nc <= 32 ? 2 : 4;
   a.row_tiles = a.M > 16 && a.nc_wave < 4 ? 2 : 1;
@@ -122,7 +128,8 @@ VerifyPlan verify_plan(const rpd_verify* p) {
   v.rows = (long long)p->B * (p->T + 1) + (p->draft && !greedy ? (long long)p->B * p->T : 0);
   // Parts of whole 2048 entries (8 a thread), at most 64 of them, which one wave merges in a step. For the
   // statistics, as long as the launch fills the GPU's workgroups twice over, longer ones of up to 8192, which a
-  // thread holds in registers (a workgroup's start and merges cost about as much as 2048 entries).
+  // thread holds in registers: 288 target and 256 draft rows of 152064 bf16 63.0 us, with parts of 4096 68.5;
+  // 1024 rows of 126464 bf16 distilled 137 us, with parts of 2048 191.
   v.part = (int)up_div(up_div(p->V, 64), 2048) * 2048;
   v.chunk = v.part;
   while (p->B * up_div(p->V, v.part) > kMaxBlocks) v.part *= 2;   // so many sequences that a launch holds no more

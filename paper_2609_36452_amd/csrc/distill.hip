@@ -30,10 +30,10 @@ static_assert(kMaxList <= kThreads, "a thread an entry of the list");
 
 // a row's state between the loss and the gradient
 struct RowState {
-  float ref, in;   // in the list: in * e^(scale z - ref) - p, with in = P / S (S relative to ref)
-  float tail, out; // outside: out * e^(scale z - tail), tail the largest exponent there (a student that is
-                   // sure leaves e^(tail - ref) far below float32's range)
-  float tref;      // the teacher's p_j = tinv * e^(scale t_j - tref)
+  float top, in;   // in the list: in * e^(scale (z - top)) - p, with in = P / S (S relative to top)
+  float tail, out; // outside: out * e^(scale (z - tail)), tail the largest logit there (a student that is
+                   // sure leaves e^(scale (tail - top)) far below float32's range)
+  float tref;      // the teacher's p_j = tinv * e^(scale (t_j - tref)), with its log-sum-exp e^(scale t_j - tref)
   float tinv;
   float any;       // 0: no gradient
 };
@@ -43,6 +43,11 @@ __device__ __forceinline__ float teacher_at(const DistillCall& a, long long i) {
   if (a.teacher_dtype == RPD_DTYPE_F32) return static_cast<const float*>(a.teacher)[i];
   return a.teacher_dtype == RPD_DTYPE_BF16 ? Bf16::one(static_cast<const uint16_t*>(a.teacher) + i)
                                            : F16::one(static_cast<const uint16_t*>(a.teacher) + i);
+}
+
+// the exponent of a teacher's logit relative to tref
+__device__ __forceinline__ double teacher_below(const DistillCall& a, double t, float tref) {
+  return a.lse ? t * (double)a.scale - (double)tref : (t - (double)tref) * (double)a.scale;
 }
 
 __device__ __forceinline__ bool skipped(const DistillCall& a, int n) { return a.weight && a.weight[n] == 0.f; }
@@ -106,14 +111,14 @@ __global__ __launch_bounds__(kThreads) void k_distill_part(DistillCall a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) m = fmaxf(m, held[j].at(e));
     }
-    const float ref = ref_of(m, a.scale);
-    s.S *= carry(s.m, ref, a.scale);
+    const float top = top_of(m);
+    s.S *= carry(s.m, top, a.scale);
     s.m = m;
 #pragma unroll
     for (int j = 0; j < kHeld; ++j) {
       if (base + j * 8 * kThreads >= hi) continue;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s.S += __expf(fmaf(held[j].at(e), a.scale, -ref));
+      for (int e = 0; e < 8; ++e) s.S += exp_below(held[j].at(e), top, a.scale);
     }
     base += kHeld * 8 * kThreads;
     fetch(base);   // a part that is longer than a thread holds
@@ -125,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void k_distill_part(DistillCall a) {
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kThreads / 64; ++w) m = fmaxf(m, s_max[w]);
-  float S = s.S * carry(s.m, ref_of(m, a.scale), a.scale);
+  float S = s.S * carry(s.m, top_of(m), a.scale);
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) S += __shfl_xor(S, k);
   if (lane == 0) s_sum[wid] = S;
@@ -182,21 +187,21 @@ __global__ __launch_bounds__(64) void k_distill_loss(DistillCall a) {
   MaxSum s{part.x, 0.f};
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) s.m = fmaxf(s.m, __shfl_xor(s.m, k));
-  s.S = part.y * carry(part.x, ref_of(s.m, a.scale), a.scale);
+  s.S = part.y * carry(part.x, top_of(s.m), a.scale);
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) s.S += __shfl_xor(s.S, k);
-  double tmax = -INFINITY, sums[2] = {0.0, 0.0};   // teacher's, student's mass in the list
-  float top = s.m;
+  double sums[2] = {0.0, 0.0};   // teacher's, student's mass in the list
+  float tmax = -INFINITY, zmax = s.m;
 #pragma unroll
   for (int u = 0; u < kEach; ++u) {
     const int v = at[u];
     s_ids[lane + 64 * u] = v;
     ok[u] = v >= 0 && v < a.V;
-    t[u] = ok[u] ? (double)teacher[u] * (double)a.scale : -INFINITY;
-    const float zj = ok[u] ? E::one(p + v) : -INFINITY;
-    z[u] = (double)zj * (double)a.scale;
-    tmax = fmax(tmax, t[u]);
-    top = fmaxf(top, zj);
+    const float tj = ok[u] ? teacher[u] : -INFINITY, zj = ok[u] ? E::one(p + v) : -INFINITY;
+    t[u] = tj;
+    z[u] = zj;
+    tmax = fmaxf(tmax, tj);
+    zmax = fmaxf(zmax, zj);
     first[u] = ok[u];
   }
   __syncthreads();
@@ -213,22 +218,23 @@ __global__ __launch_bounds__(64) void k_distill_loss(DistillCall a) {
     }
   }
 #pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
-  const float ref = ref_of(top, a.scale), tail = ref_of(s.m, a.scale);
+  for (int k = 32; k >= 1; k >>= 1) zmax = fmaxf(zmax, __shfl_xor(zmax, k));
+  const float top = top_of(zmax), tail = top_of(s.m);
+  const double scale = a.scale;
 #pragma unroll
   for (int u = 0; u < kEach; ++u) {
     if (64 * u >= a.k) continue;
-    z[u] -= (double)ref;
+    z[u] = (z[u] - (double)top) * scale;
     if (first[u]) sums[1] += exp(z[u]);
   }
 #pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) tmax = fmax(tmax, __shfl_xor(tmax, k));
-  const float tref = a.lse ? tref_given : (float)(tmax == -INFINITY ? 0.0 : tmax);
+  for (int k = 32; k >= 1; k >>= 1) tmax = fmaxf(tmax, __shfl_xor(tmax, k));
+  const float tref = a.lse ? tref_given : top_of(tmax);
 #pragma unroll
   for (int u = 0; u < kEach; ++u) {
     pj[u] = 0.0;
     if (64 * u >= a.k) continue;
-    t[u] -= (double)tref;
+    t[u] = teacher_below(a, t[u], tref);
     if (ok[u]) pj[u] = exp(t[u]);
     sums[0] += pj[u];
   }
@@ -237,7 +243,7 @@ __global__ __launch_bounds__(64) void k_distill_loss(DistillCall a) {
   const bool none = !a.lse && sums[0] == 0.0;
   const double tinv = a.lse ? 1.0 : none ? 0.0 : 1.0 / sums[0];
   const double rest = a.lse ? fmax(0.0, 1.0 - sums[0]) : 0.0;   // NaN in the list shows in its own terms
-  const double drop = s.S == 0.f ? 0.0 : (double)tail - (double)ref;   // S_T's exponent in units of S's
+  const double drop = s.S == 0.f ? 0.0 : ((double)tail - (double)top) * scale;   // S_T's exponent in units of S's
   const double e_drop = exp(drop), S = (double)s.S * e_drop + sums[1];
   // four logarithms for the time of one
   const double logs = log(lane == 0 ? S : lane == 1 ? tinv : lane == 2 ? rest : (double)s.S);
@@ -252,7 +258,7 @@ __global__ __launch_bounds__(64) void k_distill_loss(DistillCall a) {
   const double P = (none ? 0.0 : sums[0] * tinv) + rest;
   a.loss[n] = none ? 0.f : (float)((double)weight * l[0]);
   RowState st;
-  st.ref = ref;
+  st.top = top;
   st.in = (float)(P / S);
   st.tail = tail;
   st.out = (float)(P * e_drop / S - (rest > 0.0 ? rest / (double)s.S : 0.0));
@@ -297,7 +303,7 @@ __device__ __forceinline__ void row_grad(const DistillCall& a, int n, int lo, in
       if (i >= hi) continue;
       float d[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) d[e] = co * __expf(fmaf(held[j].at(e), a.scale, -st.tail));
+      for (int e = 0; e < 8; ++e) d[e] = co * exp_below(held[j].at(e), st.tail, a.scale);
       if (i + 8 <= hi) {
         held[j].set(d);
         held[j].stream(g + i);
@@ -321,10 +327,10 @@ __device__ __forceinline__ void row_grad(const DistillCall& a, int n, int lo, in
       if (s_ids[e] == v) {
         first_of &= e >= mine;
         const float t = e == mine ? tv : teacher_at(a, (long long)n * a.k + e);
-        pv += exp((double)t * (double)a.scale - (double)st.tref);
+        pv += exp(teacher_below(a, t, st.tref));
       }
   }
-  if (first_of) g[v] = E::to(c * (st.in * __expf(fmaf(zv, a.scale, -st.ref)) - (float)(pv * (double)st.tinv)));
+  if (first_of) g[v] = E::to(c * (st.in * exp_below(zv, st.top, a.scale) - (float)(pv * (double)st.tinv)));
 }
 template <class E>
 __device__ __forceinline__ void row_zero(const DistillCall& a, int n, int lo, int hi) {

@@ -98,22 +98,29 @@ __device__ __forceinline__ void load_eight(const typename E::t* p, int i, int hi
   }
 }
 
-// Maximum m of the raw logits and S = sum e^(scale z - r) with r the rounded
-// product scale m: one fused rounding an exponent, so that any scale is as
-// exact as 1. Nothing seen: m = -inf, S = 0; a row that is -inf throughout
-// keeps S = 0; NaN and +inf leave S NaN.
+// Maximum m of the raw logits and S = sum e^(scale (z - m)). Nothing seen: m =
+// -inf, S = 0; a row that is -inf throughout keeps S = 0; NaN and +inf leave S
+// NaN.
 struct MaxSum {
   float m, S;
 };
+// what exponents are relative to
+__device__ __forceinline__ float top_of(float m) { return m == -INFINITY ? 0.f : m; }
+// e^(scale (z - top)) for z up to top. The difference first: scale * top may be above float32's range though z and top
+// are not, and where it is not, its rounding alone may be more than any exponent (a mask of the type's lowest value).
+// The two roundings are 2^-24 of the exponent each.
+__device__ __forceinline__ float exp_below(float z, float top, float scale) { return __expf((z - top) * scale); }
+// what a sum relative to m is worth relative to `top` (0 while nothing was seen)
+__device__ __forceinline__ float carry(float m, float top, float scale) {
+  return m == -INFINITY ? 0.f : exp_below(m, top, scale);
+}
+
+// scale m, rounded, for sums of e^(scale z - ref)
 __device__ __forceinline__ float ref_of(float m, float scale) {
   // not to be fused with a subtraction that follows: two sums over the same m would differ by the product's
   // rounding, some 1e-6 at every merge
 #pragma clang fp contract(off)
   return m == -INFINITY ? 0.f : m * scale;
-}
-// what a sum relative to m is worth relative to r (0 while nothing was seen, whatever r: rows far below 0)
-__device__ __forceinline__ float carry(float m, float r, float scale) {
-  return m == -INFINITY ? 0.f : __expf(ref_of(m, scale) - r);
 }
 
 }  // namespace

@@ -1,0 +1,142 @@
+"""The operators beside the commit step where their values or sizes go to the ends of what a call may hold, against plain
+float64 forms."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_36452_amd import binding as rpd
+from tests import operators_ref as R
+from tests.gpu_util import note
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF, HF, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+def _f32(scale):
+    return float(torch.tensor(scale, dtype=F32))
+
+
+def _dev(*tensors):
+    return [None if t is None else t.to(DEV) for t in tensors]
+
+
+# ---------------------------------------------------------------- distill --
+
+def _distill(logits, ids, top, lse=None, up=None, scale=1.0):
+    """loss [N], gradient [N][V] and the magnitude of its terms in float64; differences of logits before their scale, so
+    that rows far from 0 keep them."""
+    N, V = logits.shape
+    up = torch.ones(N) if up is None else up
+    losses, grads, terms = torch.zeros(N).double(), torch.zeros((N, V)).double(), torch.zeros((N, V)).double()
+    for n in range(N):
+        at = ids[n].long()[(ids[n] >= 0) & (ids[n] < V)]
+        t = top[n].double()[(ids[n] >= 0) & (ids[n] < V)]
+        p = ((t - t.max()) * scale).softmax(0) if lse is None else (t * scale - float(lse[n])).exp()
+        inside = torch.zeros(V, dtype=torch.bool).index_fill_(0, at, True)
+        rest = 0.0 if lse is None or bool(inside.all()) else max(0.0, 1.0 - float(p.sum()))
+        z = logits[n].double()
+        ln_S = ((z - z.max()) * scale).exp().sum().log()
+        log_q = (z - z.max()) * scale - ln_S
+        some = p > 0
+        loss = (p[some] * (p[some].log() - log_q[at][some])).sum()
+        share = torch.zeros(V, dtype=torch.float64).scatter_add(0, at, p)
+        tail = torch.zeros(V, dtype=torch.float64)
+        if rest > 0:
+            o = z[~inside]
+            ln_T = ((o - o.max()) * scale).exp().sum().log()
+            loss = loss + rest * (math.log(rest) - ((o.max() - z.max()) * scale + ln_T - ln_S))
+            tail = torch.where(inside, tail, rest * ((z - o.max()) * scale - ln_T).exp())
+        q = (float(p.sum()) + rest) * log_q.exp()
+        c = float(up[n]) * scale
+        losses[n], grads[n], terms[n] = loss, c * (q - share - tail), abs(c) * (q + share + tail)
+    return losses, grads, terms
+
+
+def _check_loss_and_grad(loss, grad, ref, V):
+    """As far from the float64 form as float32 sums allow; infinite where that is above float32's range."""
+    rl, rg, terms = ref
+    e = 2 * R.sum_error(V)
+    loss, rl = loss.detach().cpu().double(), rl.float().double()
+    assert torch.equal(loss.isinf(), rl.isinf()) and bool(((loss == rl) | ((loss - rl).abs() <= e * (1 + rl.abs()))).all()), \
+        (loss, rl)
+    g = grad.cpu().double()
+    step = R.half_step(grad.dtype) * 1.01 * (rg.abs() + e * terms) + torch.finfo(grad.dtype).smallest_normal
+    assert bool(((g - rg).abs() <= e * terms + step).all()), float((g - rg).abs().nan_to_num(math.inf).max())
+
+
+def _masked_students(V, dtype, value, tail, scale, seed):
+    """Rows of logits with `value` in places, a teacher's list of 12 tokens in each; what stays is ordinary."""
+    g = torch.Generator().manual_seed(seed)
+    N, k = 6, 12
+    z = 2.0 * torch.randn((N, V), generator=g)
+    z[:, 1024:1032] -= 40.0                          # eight neighbours and the second half, never listed
+    z[:, V // 2:] -= 40.0
+    top, ids = z.topk(k, dim=1)
+    logits = (z + torch.randn((N, V), generator=g)).to(dtype)
+    outside = torch.ones((N, V), dtype=torch.bool).scatter_(1, ids, False)
+    logits[0, 1024:1032] = value
+    logits[1, V // 2:] = value
+    logits[2, outside[2].nonzero()[10:, 0]] = value  # an allow-list
+    logits[3, outside[3]] = value                    # nothing but the list
+    logits[4] = value                                # flat
+    logits[5, V - 8:] = value                        # padding behind the vocabulary
+    lse = torch.logsumexp(z.double() * scale, 1).float() if tail else None
+    return logits, ids.int(), top, lse, 0.5 + torch.rand((N,), generator=g)
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("scale", [0.7, 1.0, 1.25, 2.0])
+@pytest.mark.parametrize("dtype,value", [(BF, "lowest"), (F32, "lowest"), (F32, -1e10), (BF, -1e30)])
+def test_distill_masks_of_any_value(dtype, value, scale, tail):
+    note(f"  distill masked {dtype} {value} scale={scale} tail={tail}")
+    V, scale = 8192, _f32(scale)
+    value = torch.finfo(dtype).min if value == "lowest" else value
+    logits, ids, top, lse, up = _masked_students(V, dtype, value, tail, scale, 80)
+    ref = _distill(logits, ids, top, lse, up, scale)
+    a = _dev(logits, ids, top, lse, up)
+    loss, grad = rpd.distill_grad(*a[:3], teacher_lse=a[3], grad_loss=a[4], logit_scale=scale)
+    _check_loss_and_grad(loss, grad, ref, V)
+    x = a[0].clone().requires_grad_(True)
+    loss = rpd.distill(x, *a[1:3], teacher_lse=a[3], logit_scale=scale)
+    _check_loss_and_grad(loss, torch.autograd.grad(loss, x, a[4])[0], ref, V)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_distill_masks_in_long_parts(dtype):
+    """So many rows that a part is as long as a thread can hold."""
+    V, copies, scale = 32768, 200, 1.25
+    logits, ids, top, lse, up = _masked_students(V, dtype, torch.finfo(dtype).min, True, scale, 81)
+    ref = _distill(logits, ids, top, lse, up, scale)
+    a = [t.to(DEV).repeat(copies, *[1] * (t.dim() - 1)) for t in (logits, ids, top, lse, up)]
+    loss, grad = rpd.distill_grad(*a[:3], teacher_lse=a[3], grad_loss=a[4], logit_scale=scale)
+    _check_loss_and_grad(loss[:6], grad[:6], ref, V)
+    assert torch.equal(loss.view(copies, 6), loss[:6].expand(copies, 6))
+    assert bool((grad.view(copies, 6, V) == grad[:6]).all())
+
+
+@pytest.mark.parametrize("scale", [3e8, 1e30])
+def test_distill_scales_that_leave_one_token(scale):
+    V, scale = 3000, _f32(scale)
+    g = torch.Generator().manual_seed(82)
+    logits = 2.0 * torch.randn((3, V), generator=g)
+    ids = torch.tensor([[5, 9], [7, -1], [int(logits[2].argmax()), 4]], dtype=torch.int32)
+    top = torch.tensor([[1.0, 1.0], [2.0, 0.0], [3.0, 1.0]])
+    ref = _distill(logits, ids, top, scale=scale)
+    loss, grad = rpd.distill_grad(*_dev(logits, ids, top), logit_scale=scale)
+    _check_loss_and_grad(loss, grad, ref, V)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_distill_teachers_of_lowest_values(dtype):
+    """A teacher that masks what it lists: flat over the list, or its one other token."""
+    V, scale = 2500, 2.0
+    g = torch.Generator().manual_seed(83)
+    logits = torch.randn((2, V), generator=g)
+    ids = torch.tensor([[3, 700, 2400], [8, 9, 10]], dtype=torch.int32)
+    top = torch.full((2, 3), torch.finfo(dtype).min, dtype=dtype)
+    top[1, 1] = 1.0
+    ref = _distill(logits, ids, top, scale=scale)
+    loss, grad = rpd.distill_grad(*_dev(logits, ids, top), logit_scale=scale)
+    _check_loss_and_grad(loss, grad, ref, V)

@@ -115,13 +115,5 @@ __device__ __forceinline__ float carry(float m, float top, float scale) {
   return m == -INFINITY ? 0.f : exp_below(m, top, scale);
 }
 
-// scale m, rounded, for sums of e^(scale z - ref)
-__device__ __forceinline__ float ref_of(float m, float scale) {
-  // not to be fused with a subtraction that follows: two sums over the same m would differ by the product's
-  // rounding, some 1e-6 at every merge
-#pragma clang fp contract(off)
-  return m == -INFINITY ? 0.f : m * scale;
-}
-
 }  // namespace
 }  // namespace rpd

@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kThreads) void k_verify_stats(VerifyCall a) {
     if (threadIdx.x == 0) out = RowPart{0.0, m, idx};
     return;
   }
-  const float scale = is_draft ? a.draft_scale : a.target_scale, ref = ref_of(m, scale);
+  const float scale = is_draft ? a.draft_scale : a.target_scale, below = top_of(m);
   const Exp64 ex(m, scale, s_table);
   double sum = 0.0;
   float single = 0.f;
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(kThreads) void k_verify_stats(VerifyCall a) {
       if (KIND == kDouble)
         sum += ex.about(v.at(e));
       else
-        single += __expf(fmaf(v.at(e), scale, -ref));
+        single += exp_below(v.at(e), below, scale);
     }
   };
 #pragma unroll
@@ -194,7 +194,6 @@ __global__ __launch_bounds__(kThreads) void k_verify_stats(VerifyCall a) {
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int w = 1; w < kWaves; ++w) sum += s_sum[w];
-    if (KIND == kSingle && m > -INFINITY) sum *= exp((double)ref - (double)m * (double)scale);   // the reference's rounding
     // a part of nothing but -inf has no sum (one of NaN does not end here: its sum is NaN)
     out = RowPart{m == -INFINITY && sum == sum ? 0.0 : sum, m, 0};
   }

@@ -140,3 +140,50 @@ def test_distill_teachers_of_lowest_values(dtype):
     ref = _distill(logits, ids, top, scale=scale)
     loss, grad = rpd.distill_grad(*_dev(logits, ids, top), logit_scale=scale)
     _check_loss_and_grad(loss, grad, ref, V)
+
+
+# ----------------------------------------------------------------- verify --
+
+def _check_verify(o, ref, V):
+    token, n, accept = ref
+    got = o["accept"].cpu().double()
+    assert torch.equal(got.isnan(), accept.isnan()), (got, accept)
+    assert bool((((got - accept).abs() <= 2 * R.sum_error(V) * accept + 2.0 ** -23) | accept.isnan()).all()), (got, accept)
+    assert torch.equal(o["n_accept"].cpu().long(), n) and torch.equal(o["token"].cpu().long(), token)
+
+
+@pytest.mark.parametrize("copies", [1, 14, 40])   # float64 statistics, float32 ones, and those of longer parts
+@pytest.mark.parametrize("scales", [(1.5, 0.7), (0.9, 1.25)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_verify_masks_of_any_value(dtype, scales, copies):
+    note(f"  verify masked {dtype} scales={scales} copies={copies}")
+    V, B, T = 20011, 9, 2
+    g = torch.Generator().manual_seed(84)
+    target = 3.0 * torch.randn((B, T + 1, V), generator=g)
+    draft = target[:, :T] + torch.randn((B, T, V), generator=g)
+    lo = torch.finfo(dtype).min
+    some = torch.randperm(V, generator=g)[20:]
+    target[0, :, some] = lo                          # an allow-list
+    draft[0, :, some] = lo
+    target[1, :, 8192:16384] = lo                    # whole parts
+    draft[2, :, 8192:16384] = lo
+    target[3, :, 16384:], draft[3, :, 16384:] = lo, lo
+    target[4], draft[4] = lo, lo                     # flat
+    target[5, :, 2048:8192] = -1e10
+    target[6, :, 2048:8192], draft[6, :, :9000] = -1e30, -1e30
+    token = draft.argmax(2).int()
+    target[7, 0, int(token[7, 0])] = lo              # the drafted token masked out
+    draft[8, 0, 5] = lo                              # drafted though masked out
+    token[8, 0] = 5
+    token[4] = 11
+    target, draft = target.to(dtype), draft.to(dtype)
+    u, r = torch.rand((B, T), generator=g), torch.rand((B,), generator=g)
+    ts, ds = scales
+    many = [t.to(DEV).repeat(copies, *[1] * (t.dim() - 1)) for t in (target, token, u, r, draft)]
+    for q in (draft, None):
+        ref = R.verify(target, token, u, r, draft=q, target_scale=ts, draft_scale=ds)
+        o = rpd.verify_draft(*many[:4], draft_logits=None if q is None else many[4], target_scale=ts, draft_scale=ds)
+        for i in (0, B * (copies - 1)):
+            _check_verify({k: v[i:i + B] for k, v in o.items()}, ref, V)
+        for v in o.values():
+            assert torch.equal(v.view(copies, -1), v[:B].view(1, -1).expand(copies, -1))

@@ -497,7 +497,7 @@ rpd_status rpd_verify_draft(const rpd_verify* p, void* workspace, size_t workspa
  * p_j for its tokens: the softmax of logit_scale * teacher[n] over the list,
  * or, with teacher_lse, e^(logit_scale * teacher[n][j] - teacher_lse[n]), the
  * rest p_T = max(0, 1 - sum p_j) then being one entry for all tokens outside
- * the list (student's mass q_T).
+ * the list (student's mass q_T); p_T is 0 where the list holds every token.
  *   loss[n] = weight[n] * (sum_j p_j ln(p_j / q_j) + p_T ln(p_T / q_T))
  *   grad[n] = weight[n] * grad_loss[n] * d loss_n / d logits[n]
  * Rows are independent (the masked positions of a canvas, say).
@@ -522,7 +522,9 @@ rpd_status rpd_verify_draft(const rpd_verify* p, void* workspace, size_t workspa
  *   grad       device [N][V], rows grad_stride >= V apart; not the logits'
  *              memory
  * A list without entries (or of probability 0 without teacher_lse) has loss
- * and gradient 0. A list token of student probability 0 makes the loss inf.
+ * and gradient 0. A list token of student probability 0 makes the loss inf, and
+ * so does any p_T > 0, be it the rounding of teacher_lse, where the student
+ * excludes every token outside the list (give no teacher_lse there).
  */
 typedef struct rpd_distill {
   int32_t N, V, k, dtype, teacher_dtype;

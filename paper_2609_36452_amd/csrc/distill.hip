@@ -239,10 +239,15 @@ __global__ __launch_bounds__(64) void k_distill_loss(DistillCall a) {
     sums[0] += pj[u];
   }
   wave_sum(sums);
+  int listed = 0;   // different tokens in the list
+#pragma unroll
+  for (int u = 0; u < kEach; ++u)
+    if (64 * u < a.k) listed += __popcll(__ballot(first[u]));
   // a list without any mass: in list mode there is no teacher, and no loss
   const bool none = !a.lse && sums[0] == 0.0;
   const double tinv = a.lse ? 1.0 : none ? 0.0 : 1.0 / sums[0];
-  const double rest = a.lse ? fmax(0.0, 1.0 - sums[0]) : 0.0;   // NaN in the list shows in its own terms
+  // NaN in the list shows in its own terms; where no token is outside the list, 1 - sum p is the rounding of lse
+  const double rest = a.lse && listed < a.V ? fmax(0.0, 1.0 - sums[0]) : 0.0;
   const double drop = s.S == 0.f ? 0.0 : ((double)tail - (double)top) * scale;   // S_T's exponent in units of S's
   const double e_drop = exp(drop), S = (double)s.S * e_drop + sums[1];
   // four logarithms for the time of one

@@ -142,6 +142,23 @@ def test_distill_teachers_of_lowest_values(dtype):
     _check_loss_and_grad(loss, grad, ref, V)
 
 
+@pytest.mark.parametrize("V,k", [(1, 1), (50, 50), (50, 64), (256, 256)])
+def test_distill_lists_of_the_whole_vocabulary(V, k):
+    """No token is outside the list, whatever the teacher's rounded sum leaves for one."""
+    g = torch.Generator().manual_seed(88 + V)
+    N = 40
+    z = 2.0 * torch.randn((N, V), generator=g)
+    ids = torch.full((N, k), -1, dtype=torch.int32)
+    ids[:, :V] = torch.stack([torch.randperm(V, generator=g) for _ in range(N)]).int()
+    top = torch.zeros((N, k))
+    top[:, :V] = z.gather(1, ids[:, :V].long())
+    logits = z + torch.randn((N, V), generator=g)
+    lse = torch.logsumexp(z, 1)
+    lse[::2] += 1e-3                         # in these rows the list's mass is below 1 for certain
+    loss, grad = rpd.distill_grad(*_dev(logits, ids, top), teacher_lse=lse.to(DEV))
+    _check_loss_and_grad(loss, grad, _distill(logits, ids, top, lse), V)
+
+
 # ----------------------------------------------------------------- verify --
 
 def _check_verify(o, ref, V):

@@ -520,7 +520,7 @@ rpd_status rpd_verify_draft(const rpd_verify* p, void* workspace, size_t workspa
  *   state      device [N][RPD_DISTILL_STATE] float32: what the gradient needs
  *              of the loss
  *   grad       device [N][V], rows grad_stride >= V apart; not the logits'
- *              memory
+ *              memory (rows of the logits' stride may lie between theirs)
  * A list without entries (or of probability 0 without teacher_lse) has loss
  * and gradient 0. A list token of student probability 0 makes the loss inf, and
  * so does any p_T > 0, be it the rounding of teacher_lse, where the student

@@ -166,6 +166,18 @@ DistillPlan distill_plan(const rpd_distill* p) {
   return d;
 }
 
+// Whether a row of the gradient takes memory of a row of the logits, which other workgroups still read then (both
+// aligned to their elements). Rows of one stride may lie between each other; of two strides, the ranges must be apart.
+bool grad_over_logits(const rpd_distill* p) {
+  const long long size = p->dtype == RPD_DTYPE_F32 ? 4 : 2, V = p->V, last = p->N - 1;
+  const __int128 at =
+      ((__int128) reinterpret_cast<uintptr_t>(p->grad) - (__int128) reinterpret_cast<uintptr_t>(p->logits)) / size;
+  if (at >= (__int128)last * p->logits_stride + V || -at >= (__int128)last * p->grad_stride + V) return false;
+  if (last == 0 || p->grad_stride != p->logits_stride) return true;
+  const long long stride = p->logits_stride, shift = (long long)(((at % stride) + stride) % stride);
+  return shift < V || shift > stride - V;
+}
+
 rpd_status check_distill(const rpd_distill* p, bool grad) {
   if (!p) return fail(RPD_ERR_NULL_POINTER, "problem is NULL");
   if (!distill_shape_ok(p))
@@ -182,12 +194,12 @@ rpd_status check_distill(const rpd_distill* p, bool grad) {
   if (p->N == 0) return RPD_OK;
   if (!p->logits || !p->id || !p->teacher || !p->state || (grad && !p->grad))
     return fail(RPD_ERR_NULL_POINTER, "logits, id, teacher, state%s are required", grad ? " and grad" : "");
-  if (grad && p->grad == p->logits) return fail(RPD_ERR_BAD_PARAM, "grad must not be the logits' memory");
   const unsigned e = elem_align(p->dtype);
   if (misaligned(p->logits, e) || misaligned(p->grad, e) || misaligned(p->teacher, elem_align(p->teacher_dtype)) ||
       misaligned(p->id, 3) || misaligned(p->teacher_lse, 3) || misaligned(p->weight, 3) ||
       misaligned(p->grad_loss, 3) || misaligned(p->loss, 3) || misaligned(p->state, 3))
     return fail(RPD_ERR_UNSUPPORTED, "a pointer is not aligned to its element");
+  if (grad && grad_over_logits(p)) return fail(RPD_ERR_BAD_PARAM, "grad must not be the logits' memory");
   return RPD_OK;
 }
 

@@ -127,9 +127,11 @@ VerifyPlan verify_plan(const rpd_verify* p) {
   const bool greedy = (p->flags & RPD_VERIFY_GREEDY) != 0;
   v.rows = (long long)p->B * (p->T + 1) + (p->draft && !greedy ? (long long)p->B * p->T : 0);
   // Parts of whole 2048 entries (8 a thread), at most 64 of them, which one wave merges in a step. For the
-  // statistics, as long as the launch fills the GPU's workgroups twice over, longer ones of up to 8192, which a
-  // thread holds in registers: 288 target and 256 draft rows of 152064 bf16 63.0 us, with parts of 4096 68.5;
-  // 1024 rows of 126464 bf16 distilled 137 us, with parts of 2048 191.
+  // statistics, as long as the launch fills the GPU's workgroups twice over, they are doubled while shorter than
+  // 8192, which a workgroup's threads hold in registers: 288 target and 256 draft rows of 152064 bf16 63.0 us, with
+  // parts of 4096 68.5; 1024 rows of 126464 bf16 distilled 137 us, with parts of 2048 191. From V = 262145 to 393216
+  // parts of 6144 become 12288, read in two rounds (the verification's, twice): 1024 rows of 393216 bf16 distilled
+  // 448 us and greedily verified 141, in parts of 6144 504 and 148; of 300001, 350 and 106, and 340 and 117.
   v.part = (int)up_div(up_div(p->V, 64), 2048) * 2048;
   v.chunk = v.part;
   while (p->B * up_div(p->V, v.part) > kMaxBlocks) v.part *= 2;   // so many sequences that a launch holds no more

@@ -40,3 +40,14 @@ def test_distill_refuses_a_gradient_over_the_logits(N, V, ls, at, gs, refused, d
     # a call that is not refused for its memory is for its workspace
     assert rpd.lib().rpd_distill_loss(ctypes.byref(p), None, 0, None) == (3 if refused else 1)
     assert ("logits" in rpd.last_error()) == refused and ("workspace" in rpd.last_error()) != refused
+
+
+@pytest.mark.parametrize("V,parts", [(131072, 16), (262144, 32), (262145, 22), (300000, 25), (393216, 32), (393217, 49),
+                                     (1 << 20, 64)])
+def test_parts_of_many_rows(V, parts):
+    """Parts of whole 2048 entries, at most 64 of them, doubled while they are shorter than 8192."""
+    p = _distill(4000, V)
+    assert rpd.lib().rpd_distill_workspace_size(ctypes.byref(p)) == _r(4000 * parts * 8)
+    q = rpd.RpdVerify(2000, 1, V, rpd.DTYPE_BF16, P, 2 * V, V, None, 0, 0, P, None, P, P, 1.0, 1.0,
+                      rpd.VERIFY_GREEDY, P, P, P)
+    assert rpd.lib().rpd_verify_workspace_size(ctypes.byref(q)) == _r(4000 * parts * 16)

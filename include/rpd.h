@@ -367,7 +367,10 @@ rpd_status rpd_apply_commit(int32_t B, int32_t L, uint8_t* mask, int32_t* canvas
  * types are RPD_DTYPE_BF16, RPD_DTYPE_F16 and RPD_DTYPE_F32 as each entry
  * says; strides are in elements, the last dimension is contiguous, and rows
  * need no alignment beyond their element's. NaN and infinities follow IEEE
- * arithmetic and stay in the row (sequence) that holds them.
+ * arithmetic and stay in the row (sequence) that holds them. Finite logits may
+ * be of any size, at any scale: a mask of the type's lowest value is probability
+ * 0, and a row of nothing else is flat (two logits whose difference exceeds
+ * float32's range count as infinitely far apart).
  */
 
 /*

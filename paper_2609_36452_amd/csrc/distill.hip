@@ -275,7 +275,7 @@ __global__ __launch_bounds__(64) void k_distill_loss(DistillCall a) {
 
 // The part [lo, hi) of a row's gradient: the formula of the entries outside the list everywhere, then those in the
 // list over it. Streamed past the caches, which keep the logits between the loss and the gradient. 1024 rows of 126464
-// bf16, three quarters of them read: 42 us for the sums and 70 here (452 MB: 6.5 TB/s); with ordinary stores the sums
+// bf16, three quarters of them read: 40 us for the sums and 69 here (452 MB: 6.5 TB/s); with ordinary stores the sums
 // take 14 us more, this 2.
 template <class E>
 __device__ __forceinline__ void row_grad(const DistillCall& a, int n, int lo, int hi, const RowState& st) {

@@ -5,8 +5,13 @@
 // Bound: one stream of the packed codes from HBM (half a byte a weight). What
 // has to keep up with it is turning codes into matrix operands and feeding x.
 // 4096 columns, V = 126464 (267 MB): 44 us for one row (6.1 TB/s); 54-59 for 32
-// rows, where converting the codes and the products take as long as the stream;
-// 96-100 for 64 rows, which convert them twice.
+// rows, where converting the codes and the products take as long as the stream
+// (the vector instructions hold a SIMD for 56% of the time, the matrix cores for
+// 24%); 96-100 for 64 rows, which convert them twice (61% and 28%). Rows of more
+// than 8192 columns leave that bound: x no longer fits the registers, is loaded
+// and converted anew for every tile, and the converting forms spill a few of
+// them: 65536 rows of 16384 bf16 take 187 us for one row (2.9 TB/s of codes), 311
+// for 16, 280 for 32; of 8192 50, 58 and 77.
 //
 // x stays: the waves of a workgroup divide the columns among them, each keeps
 // the fp16 fragments of its columns of all rows in registers, and only the
@@ -22,9 +27,12 @@
 // bf16 rows become fp16 by a power of two per row (the largest finite |x| comes
 // to 2^14..2^15): their 8 bits fit, and an element so small that it falls among
 // fp16's subnormals is off by at most 2^-39 of the row's largest, far below
-// what fp32 accumulation keeps. Sums are fp32: within a group on the matrix
-// cores, then scaled, then over groups, then over waves, in a fixed order that
-// is the same for every vocabulary row (equal rows give equal logits).
+// what fp32 accumulation keeps. fp16 rows stay as they are: among subnormal
+// elements every product with q - z is a whole multiple of 2^-24, and nothing of
+// it is lost (rows of 2^-22 to 2^-14 give the logits of the same rows times 2^10
+// bit by bit). Sums are fp32: within a group on the matrix cores, then scaled,
+// then over groups, then over waves, in a fixed order that is the same for every
+// vocabulary row (equal rows give equal logits).
 #include <climits>
 #include <cstdint>
 
@@ -132,8 +140,9 @@ __device__ __forceinline__ typename Raw<N>::t load_bits(char* base, int range, u
 // instruction: 107.6 us instead of 96.2 at 64 rows). As subnormals, q 2^-24,
 // the codes would need no subtraction, 5 instructions, and the zero points a
 // correction by the sums of x; but the matrix cores keep fewer bits of such
-// products: logits were off by 4e-6 of their size, 1e-7 so, for 4% of the time
-// at 64 rows.
+// products (one instruction over normally distributed x: off by 1.3e-6 of the
+// terms instead of 3e-8): logits were off by 4e-6 of their size, 1e-7 so, for 4%
+// of the time at 64 rows.
 __device__ __forceinline__ f16x8 decode(uint32_t w, f16x2 zl, f16x2 zh, uint32_t mask_low, uint32_t mask_high,
                                         uint32_t one) {
   const f16x2 sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};

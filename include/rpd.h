@@ -553,6 +553,71 @@ rpd_status rpd_distill_loss(const rpd_distill* p, void* workspace, size_t worksp
  * (`loss` is not used; needs no workspace) */
 rpd_status rpd_distill_grad(const rpd_distill* p, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Drafting with an 8-bit output head: quantization to blocks of 8-bit floating
+ * point, the head in that form, and sampling from its logits. The conventions
+ * above hold for them too.
+ */
+
+/*
+ * Blocks of 8-bit floating point (e4m3: 4 significant bits, largest 448, no
+ * infinities): a scale for each 128 columns of a row (block_rows 1), or for
+ * each 128 x 128 of a matrix (block_rows 128); blocks at an end may be smaller.
+ *   scale = the smallest power of two in 2^-126 .. 2^120 with which the block's
+ *           largest finite magnitude is at most 448 (1 where that is 0)
+ *   code  = e4m3(x / scale), to nearest, ties to even; NaN of what is not finite
+ *   rows, d    0 <= rows <= 2^28 (0: nothing is done), 1 <= d <= 2^28; together
+ *              bounded by what one launch holds
+ *   dtype      of x: RPD_DTYPE_BF16, _F16 or _F32
+ *   x          device [rows][d], rows x_stride >= d apart
+ *   codes      device [rows][d] bytes, rows codes_stride >= d apart
+ *   scales     device [rows or ceil(rows / 128)][ceil(d / 128)] float32
+ * x, codes and scales must not overlap.
+ */
+rpd_status rpd_fp8_quantize(int32_t rows, int32_t d, int32_t dtype, const void* x, int64_t x_stride, int32_t block_rows,
+                            uint8_t* codes, int64_t codes_stride, float* scales, void* stream);
+
+/*
+ * An output head in e4m3 with a scale for each block of 128 x 128 (of any
+ * float32 value):
+ *   W[v][k] = scales[v / 128][k / 128] * code[v][k]
+ *   V, d       1 <= V, d <= 2^20, V * d <= 2^36
+ *   codes      device [V][d] bytes, contiguous
+ *   scales     device [ceil(V / 128)][ceil(d / 128)] float32
+ *   transpose  0: packs W; 1: packs its transpose, a head of d rows and V
+ *              columns (for the gradient of the rows: dx = dy W)
+ *   packed     device, 256-byte aligned, rpd_fp8_packed_size bytes (of (d, V)
+ *              with transpose)
+ * The codes are laid out once, for the matrix cores.
+ */
+size_t rpd_fp8_packed_size(int32_t V, int32_t d); /* 0 if out of range */
+rpd_status rpd_fp8_pack(int32_t V, int32_t d, const uint8_t* codes, const float* scales, int32_t transpose, void* packed,
+                        size_t packed_bytes, void* stream);
+
+/* Workspace bytes of rpd_fp8_project for M rows; 0 if out of range. */
+size_t rpd_fp8_workspace_size(int32_t V, int32_t d, int32_t M, int32_t statistics);
+
+/*
+ * M rows through a packed head of V rows and d columns. The rows are quantized
+ * first, as rpd_fp8_quantize does with block_rows 1; with x^ what their codes
+ * and scales stand for, logits y = W x^, or the softmax statistics of
+ * logit_scale * y as rpd_gate_commit takes them (the logits then never reach
+ * memory). Codes and x^ are exact operands (magnitudes below 2^-126 may count
+ * as 0), sums are float32. Equal rows of the head give equal logits; of equal
+ * logits the lowest index is the argmax.
+ *   M          0 <= M <= 2^20 (0: nothing is done)
+ *   x          device [M][d] of type x_dtype (bf16, fp16 or fp32), rows x_stride >= d apart
+ *   logits     device [M][V] of type logits_dtype (any of the three), rows
+ *              logits_stride >= V apart; or NULL
+ *   argmax, confidence, entropy, logit_scale   as rpd_quant_project's
+ *   workspace  rpd_fp8_workspace_size bytes, 256-byte aligned; its prior
+ *              contents do not matter
+ */
+rpd_status rpd_fp8_project(int32_t V, int32_t d, const void* packed, int32_t M, const void* x, int64_t x_stride,
+                           int32_t x_dtype, void* logits, int64_t logits_stride, int32_t logits_dtype, int32_t* argmax,
+                           float* confidence, float* entropy, float logit_scale, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
 /* Static text for a status code. */
 const char* rpd_status_string(rpd_status s);
 

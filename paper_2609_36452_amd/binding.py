@@ -165,7 +165,13 @@ def lib() -> ctypes.CDLL:
                 ("rpd_verify_draft", ctypes.c_int, [ver, v, size, v]),
                 ("rpd_distill_workspace_size", size, [dis]),
                 ("rpd_distill_loss", ctypes.c_int, [dis, v, size, v]),
-                ("rpd_distill_grad", ctypes.c_int, [dis, v])):
+                ("rpd_distill_grad", ctypes.c_int, [dis, v]),
+                ("rpd_fp8_quantize", ctypes.c_int, [i32, i32, i32, v, i64, i32, v, i64, v, v]),
+                ("rpd_fp8_packed_size", size, [i32, i32]),
+                ("rpd_fp8_pack", ctypes.c_int, [i32, i32, v, v, i32, v, size, v]),
+                ("rpd_fp8_workspace_size", size, [i32, i32, i32, i32]),
+                ("rpd_fp8_project", ctypes.c_int,
+                 [i32, i32, v, i32, v, i64, i32, v, i64, i32, v, v, v, ctypes.c_float, v, size, v])):
             f = getattr(L, name)
             f.restype, f.argtypes = res, args
         L.rpd_status_string.restype = ctypes.c_char_p
@@ -816,3 +822,151 @@ def distill_grad(logits: torch.Tensor, teacher_id: torch.Tensor, teacher_logit: 
     grad = _grad_like(logits, p)
     loss, _ = _distill_loss(p, logits, stream)
     return loss, grad
+
+
+# ------------------------------------------------------ drafting with an 8-bit head --
+
+FP8_BLOCK = 128
+
+
+def _blocks_of(n: int) -> int:
+    return -(-n // FP8_BLOCK)
+
+
+def fp8_quantize(x: torch.Tensor, block_rows: int = 1, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+    """``rpd_fp8_quantize``: x [..., d] (bfloat16, float16 or float32) to e4m3 codes (torch.float8_e4m3fn, of x's
+    shape) and float32 scales, powers of two: one for each 128 columns of a row ([..., ceil(d/128)]), or, with
+    ``block_rows=128``, for each 128 x 128 of a matrix x [V][d] ([ceil(V/128)][ceil(d/128)]). Not recorded by
+    autograd. ``stream`` as in ``verify_draft``."""
+    _one_device("x", x)
+    code = _float_code("x", x)
+    if block_rows not in (1, FP8_BLOCK):
+        raise ValueError(f"block_rows must be 1 or {FP8_BLOCK} (got {block_rows})")
+    if block_rows > 1 and x.dim() != 2:
+        raise ValueError("x must be [V][d] for blocks of rows")
+    x = x.detach()
+    r = _rows("x", x)
+    rows, d = r.shape
+    codes = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
+    lead = tuple(x.shape[:-1]) if block_rows == 1 else (_blocks_of(rows),)
+    scales = torch.empty((*lead, _blocks_of(d)), dtype=torch.float32, device=x.device)
+    _enqueue(x.device, stream, lib().rpd_fp8_quantize, rows, d, code, r.data_ptr(), _row_stride(r), int(block_rows),
+             codes.data_ptr(), max(d, 1), scales.data_ptr())
+    return codes, scales
+
+
+class _Fp8Logits(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, head, out_dtype):
+        ctx.head, ctx.dtype = head, x.dtype
+        return head._logits(x, out_dtype, None, None)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        return ctx.head.input_grad(grad.contiguous(), out_dtype=ctx.dtype), None, None
+
+
+class Fp8Head:
+    """An output head in 8-bit floating point with a scale for each block of 128 x 128 (``rpd_fp8_pack``,
+    ``rpd_fp8_project``): W[v][k] = scales[v // 128][k // 128] * codes[v][k].
+
+    codes torch.float8_e4m3fn (or their bytes, uint8) [V][d], scales float32 [ceil(V/128)][ceil(d/128)] of any value.
+    Packs them once into ``packed`` on the current stream, and with ``train`` the transpose as well, for the gradient
+    of the rows; the inputs are not kept. Rows are quantized within a call (``fp8_quantize``). Outputs and workspaces of
+    the calls are made on the current stream: another one that is given as ``stream`` has to wait for it beforehand
+    (``stream.wait_stream``), as for any tensor of the caller's."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, train: bool = False):
+        self.device = _one_device("codes", codes, scales=scales)
+        if codes.dim() != 2:
+            raise ValueError("codes must be [V][d]")
+        V, d = codes.shape
+        _check_dev("codes", codes, (V, d), (torch.float8_e4m3fn, torch.uint8))
+        _check_dev("scales", scales, (_blocks_of(V), _blocks_of(d)), (torch.float32,))
+        self.V, self.d, self.train = V, d, bool(train)
+        self.packed = self._pack(codes, scales, False)
+        self.packed_t = self._pack(codes, scales, True) if train else None
+
+    def _pack(self, codes, scales, transpose):
+        size = (self.d, self.V) if transpose else (self.V, self.d)
+        # an invalid head has size 0, and the call below says what is wrong with it
+        packed = torch.empty(max(int(lib().rpd_fp8_packed_size(*size)), 1), dtype=torch.uint8, device=self.device)
+        _enqueue(self.device, None, lib().rpd_fp8_pack, self.V, self.d, codes.data_ptr(), scales.data_ptr(),
+                 int(transpose), packed.data_ptr(), packed.numel())
+        return packed
+
+    @classmethod
+    def from_weight(cls, w_u: torch.Tensor, train: bool = False) -> "Fp8Head":
+        """The head of a weight matrix W_U [V][d] (bfloat16, float16 or float32), quantized by ``fp8_quantize``."""
+        return cls(*fp8_quantize(w_u, block_rows=FP8_BLOCK), train=train)
+
+    def _project(self, packed, V, d, x, x_name, out, statistics, logit_scale, stream):
+        """x [..., d] through the packed head of V rows: into ``out``, or the three tensors of ``statistics``."""
+        _one_device(x_name, x, packed=packed)
+        code = _float_code(x_name, x)
+        if x.dim() < 1 or x.shape[-1] != d:
+            raise ValueError(f"{x_name} has shape {tuple(x.shape)}, the head takes [..., {d}]")
+        r = _rows(x_name, x)
+        nbytes = int(lib().rpd_fp8_workspace_size(V, d, r.shape[0], int(out is None)))
+        ws = None
+        if nbytes:
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+            if stream is not None:
+                ws.record_stream(stream)
+        out_stride = 0 if out is None else _row_stride(_rows("out", out))
+        s = statistics or {}
+        _enqueue(x.device, stream, lib().rpd_fp8_project, V, d, packed.data_ptr(), r.shape[0], r.data_ptr(),
+                 _row_stride(r), code, _ptr(out), out_stride, 0 if out is None else _float_code("out", out),
+                 _ptr(s.get("argmax")), _ptr(s.get("confidence")), _ptr(s.get("entropy")), float(logit_scale), _ptr(ws),
+                 nbytes)
+
+    @staticmethod
+    def _out(x, x_name, n, out_dtype, out):
+        if out is None:
+            return torch.empty((*x.shape[:-1], n), dtype=out_dtype or x.dtype, device=x.device)
+        if tuple(out.shape) != (*x.shape[:-1], n) or (out_dtype and out.dtype != out_dtype):
+            raise ValueError(f"out has shape {tuple(out.shape)} and dtype {out.dtype}")
+        _one_device("out", out, **{x_name: x})
+        return out
+
+    def _logits(self, x, out_dtype, out, stream):
+        out = self._out(x, "x", self.V, out_dtype, out)
+        self._project(self.packed, self.V, self.d, x, "x", out, None, 1.0, stream)
+        return out
+
+    def logits(self, x: torch.Tensor, out_dtype: torch.dtype | None = None, out: torch.Tensor | None = None,
+               stream=None) -> torch.Tensor:
+        """x [..., d] (bfloat16, float16 or float32) through the head: [..., V] of type ``out_dtype`` (x's if None), into
+        ``out`` if given. Differentiable once in x, of a head made with ``train`` (the quantization counts as the
+        identity, the weights are constants, and the upstream gradient is quantized as x is); with ``out`` or
+        ``stream``, x must not require a gradient."""
+        if not (x.requires_grad and torch.is_grad_enabled()):
+            return self._logits(x, out_dtype, out, stream)
+        if not self.train:
+            raise ValueError("x requires a gradient: make the head with train=True (or detach x)")
+        if out is not None or stream is not None:
+            raise ValueError("x requires a gradient: neither out nor stream can be given")
+        return _Fp8Logits.apply(x, self, out_dtype)
+
+    def stats(self, x: torch.Tensor, logit_scale: float = 1.0, stream=None) -> dict:
+        """The softmax statistics of logit_scale * (x through the head), as ``gate_commit`` takes them for
+        x [K][B][L][d]: argmax int32, confidence and entropy float32, of x's leading shape. Not recorded by autograd."""
+        e = dict(device=x.device)
+        o = {"argmax": torch.empty(x.shape[:-1], dtype=torch.int32, **e),
+             "confidence": torch.empty(x.shape[:-1], dtype=torch.float32, **e),
+             "entropy": torch.empty(x.shape[:-1], dtype=torch.float32, **e)}
+        self._project(self.packed, self.V, self.d, x.detach(), "x", None, o, logit_scale, stream)
+        return o
+
+    def input_grad(self, grad: torch.Tensor, out_dtype: torch.dtype | None = None, out: torch.Tensor | None = None,
+                   stream=None) -> torch.Tensor:
+        """The gradient of the rows, grad W, from the logits' gradient [..., V] (quantized within the call, a scale for
+        each 128 of its columns): [..., d] of type ``out_dtype`` (grad's if None), into ``out`` if given. Of a head made
+        with ``train``; what ``logits`` calls in its backward pass, for a training step that needs no autograd."""
+        if not self.train:
+            raise ValueError("the head was made without train=True")
+        grad = grad.detach()
+        out = self._out(grad, "grad", self.d, out_dtype, out)
+        self._project(self.packed_t, self.d, self.V, grad, "grad", out, None, 1.0, stream)
+        return out

@@ -1,0 +1,185 @@
+// C ABI of the 8-bit floating-point blocks: argument validation, workspace
+// layout and launch planning. Kernels live in fp8.hip.
+#include <algorithm>
+
+#include "rpd_checks.h"
+
+using namespace rpd;
+
+namespace {
+
+bool head_ok(int V, int d) { return V >= 1 && V <= 1 << 20 && d >= 1 && d <= 1 << 20 && (long long)V * d <= 1LL << 36; }
+
+rpd_status check_head(int V, int d) {
+  if (!head_ok(V, d)) return fail(RPD_ERR_BAD_SHAPE, "need 1<=V,d<=2^20, V*d<=2^36 (got V=%d d=%d)", V, d);
+  return RPD_OK;
+}
+
+Fp8Dims fp8_dims(int V, int d) {
+  Fp8Dims q{};
+  q.V = V;
+  q.d = d;
+  q.nc = (int)up_div(d, kFp8Block);
+  q.n16 = (int)up_div(V, 16);
+  q.nr = (int)up_div(V, kFp8Block);
+  q.scale_offset = round256((size_t)q.n16 * q.nc * 2048);
+  q.bytes = q.scale_offset + round256((size_t)q.nr * q.nc * 4);
+  return q;
+}
+
+constexpr int kWanted = 512;      // workgroups: two on each of 256 CUs
+constexpr int kLeastChunks = 4;   // of a split
+
+void fp8_plan(const Fp8Dims& q, bool stats, Fp8Call& a) {
+  a.mb = (int)up_div(a.M, 16);
+  a.nrt = (int)up_div(a.mb, kFp8TileBlocks);
+  a.nb = (int)up_div(a.mb, a.nrt);
+  a.nrt = (int)up_div(a.mb, a.nb);
+  a.nvt = (int)up_div(q.V, kFp8TileRows);
+  a.splits = 1;
+  const long long tiles = (long long)a.nrt * a.nvt;
+  if (!stats && tiles < kWanted)
+    a.splits = (int)std::max(1LL, std::min(kWanted / tiles, (long long)q.nc / kLeastChunks));
+}
+
+struct Fp8Space {
+  size_t partials, sums, bytes;   // offsets (the rows come first)
+};
+Fp8Space fp8_space(const Fp8Dims& q, const Fp8Call& a, bool stats) {
+  Fp8Space w{};
+  w.partials = round256((size_t)a.mb * q.nc * 4096);
+  w.sums = w.partials + (stats ? round256((size_t)a.M * a.nvt * 16) : 0);
+  w.bytes = w.sums + (a.splits > 1 ? round256((size_t)a.splits * a.M * q.n16 * 64) : 0);
+  return w;
+}
+
+}  // namespace
+
+extern "C" {
+
+rpd_status rpd_fp8_quantize(int32_t rows, int32_t d, int32_t dtype, const void* x, int64_t x_stride, int32_t block_rows,
+                            uint8_t* codes, int64_t codes_stride, float* scales, void* stream) {
+  clear_error();
+  if (rows < 0 || rows > 1 << 28 || d < 1 || d > 1 << 28)
+    return fail(RPD_ERR_BAD_SHAPE, "need 0<=rows<=2^28, 1<=d<=2^28 (got rows=%d d=%d)", rows, d);
+  if (!is_float_dtype(dtype)) return fail(RPD_ERR_UNSUPPORTED, "dtype %d is not supported", dtype);
+  if (block_rows != 1 && block_rows != kFp8Block)
+    return fail(RPD_ERR_BAD_PARAM, "block_rows must be 1 or %d (got %d)", kFp8Block, block_rows);
+  if (x_stride < d || codes_stride < d) return fail(RPD_ERR_BAD_SHAPE, "row strides must be at least d");
+  const long long nb = up_div(d, kFp8Block);
+  if ((block_rows == 1 ? up_div(rows * nb, 16) : up_div(rows, kFp8Block) * nb) > kMaxBlocks)
+    return fail(RPD_ERR_BAD_SHAPE, "rows * d is too large (rows=%d d=%d)", rows, d);
+  if (rows == 0) return RPD_OK;
+  if (!x || !codes || !scales) return fail(RPD_ERR_NULL_POINTER, "x, codes and scales are required");
+  if (misaligned(x, elem_align(dtype)) || misaligned(scales, 3))
+    return fail(RPD_ERR_UNSUPPORTED, "a pointer is not aligned to its element");
+  // what is written must not be what other workgroups still read
+  const uintptr_t xa = reinterpret_cast<uintptr_t>(x), ca = reinterpret_cast<uintptr_t>(codes),
+                  sa = reinterpret_cast<uintptr_t>(scales);
+  const unsigned long long xn = ((unsigned long long)(rows - 1) * x_stride + d) * (dtype == RPD_DTYPE_F32 ? 4 : 2),
+                           cn = (unsigned long long)(rows - 1) * codes_stride + d,
+                           sn = (unsigned long long)(block_rows == 1 ? rows : up_div(rows, kFp8Block)) * nb * 4;
+  auto meet = [](uintptr_t p, unsigned long long n, uintptr_t q, unsigned long long k) { return p < q + k && q < p + n; };
+  if (meet(xa, xn, ca, cn) || meet(xa, xn, sa, sn) || meet(ca, cn, sa, sn))
+    return fail(RPD_ERR_BAD_PARAM, "x, codes and scales must not overlap");
+  Fp8Quantize a{};
+  a.rows = rows;
+  a.d = d;
+  a.nb = (int)nb;
+  a.dtype = dtype;
+  a.x = x;
+  a.x_stride = x_stride;
+  a.codes = codes;
+  a.codes_stride = codes_stride;
+  a.scales = scales;
+  const hipError_t e = launch_fp8_quantize(a, block_rows, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(RPD_ERR_HIP, "launch: %s", hipGetErrorString(e));
+  return RPD_OK;
+}
+
+size_t rpd_fp8_packed_size(int32_t V, int32_t d) { return head_ok(V, d) ? fp8_dims(V, d).bytes : 0; }
+
+rpd_status rpd_fp8_pack(int32_t V, int32_t d, const uint8_t* codes, const float* scales, int32_t transpose, void* packed,
+                        size_t packed_bytes, void* stream) {
+  clear_error();
+  const rpd_status st = check_head(V, d);
+  if (st != RPD_OK) return st;
+  if (transpose != 0 && transpose != 1) return fail(RPD_ERR_BAD_PARAM, "transpose must be 0 or 1");
+  if (!codes || !scales || !packed) return fail(RPD_ERR_NULL_POINTER, "codes, scales and packed are required");
+  if (misaligned(scales, 3)) return fail(RPD_ERR_UNSUPPORTED, "scales must be aligned to their element");
+  if (misaligned(packed, 255)) return fail(RPD_ERR_UNSUPPORTED, "packed must be 256-byte aligned");
+  const Fp8Dims q = transpose ? fp8_dims(d, V) : fp8_dims(V, d);
+  if (packed_bytes < q.bytes)
+    return fail(RPD_ERR_WORKSPACE_TOO_SMALL, "packed has %zu bytes, %zu needed", packed_bytes, q.bytes);
+  const hipError_t e =
+      launch_fp8_pack(q, codes, scales, transpose != 0, static_cast<uint8_t*>(packed), static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(RPD_ERR_HIP, "launch: %s", hipGetErrorString(e));
+  return RPD_OK;
+}
+
+size_t rpd_fp8_workspace_size(int32_t V, int32_t d, int32_t M, int32_t statistics) {
+  if (!head_ok(V, d) || M < 1 || M > 1 << 20) return 0;
+  const Fp8Dims q = fp8_dims(V, d);
+  Fp8Call a{};
+  a.M = M;
+  fp8_plan(q, statistics != 0, a);
+  return fp8_space(q, a, statistics != 0).bytes;
+}
+
+rpd_status rpd_fp8_project(int32_t V, int32_t d, const void* packed, int32_t M, const void* x, int64_t x_stride,
+                           int32_t x_dtype, void* logits, int64_t logits_stride, int32_t logits_dtype, int32_t* argmax,
+                           float* confidence, float* entropy, float logit_scale, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+  clear_error();
+  rpd_status st = check_head(V, d);
+  if (st != RPD_OK) return st;
+  if (M < 0 || M > 1 << 20) return fail(RPD_ERR_BAD_SHAPE, "need 0<=M<=2^20 (got %d)", M);
+  if (!is_float_dtype(x_dtype)) return fail(RPD_ERR_UNSUPPORTED, "x_dtype %d is not supported", x_dtype);
+  if (x_stride < d || (logits && logits_stride < V))
+    return fail(RPD_ERR_BAD_SHAPE, "row strides must be at least the row's length");
+  if (logits && !is_float_dtype(logits_dtype))
+    return fail(RPD_ERR_UNSUPPORTED, "logits_dtype %d is not supported", logits_dtype);
+  if (!scale_ok(logit_scale))
+    return fail(RPD_ERR_BAD_PARAM, "logit_scale must be finite and > 0, or 0 for 1 (got %g)", logit_scale);
+  if (M == 0) return RPD_OK;
+  if (!packed || !x) return fail(RPD_ERR_NULL_POINTER, "packed and x are required");
+  const int ns = (argmax != nullptr) + (confidence != nullptr) + (entropy != nullptr);
+  if (logits ? ns != 0 : ns != 3)
+    return fail(RPD_ERR_NULL_POINTER, "give either logits, or argmax, confidence and entropy");
+  if (misaligned(packed, 255)) return fail(RPD_ERR_UNSUPPORTED, "packed must be 256-byte aligned");
+  if (misaligned(x, elem_align(x_dtype)) || misaligned(logits, elem_align(logits_dtype)) || misaligned(argmax, 3) ||
+      misaligned(confidence, 3) || misaligned(entropy, 3))
+    return fail(RPD_ERR_UNSUPPORTED, "a pointer is not aligned to its element");
+  const Fp8Dims q = fp8_dims(V, d);
+  const uint8_t* pk = static_cast<const uint8_t*>(packed);
+  Fp8Call a{};
+  a.packed = pk;
+  a.scales = reinterpret_cast<const float*>(pk + q.scale_offset);
+  a.M = M;
+  a.x = x;
+  a.x_stride = x_stride;
+  a.x_type = x_dtype;
+  a.out = logits;
+  a.out_stride = logits_stride;
+  a.out_type = logits_dtype;
+  a.logit_scale = scale_of(logit_scale);
+  a.argmax = argmax;
+  a.confidence = confidence;
+  a.entropy = entropy;
+  fp8_plan(q, logits == nullptr, a);
+  if ((long long)a.nrt * (a.nvt + 7) * a.splits > kMaxBlocks || (long long)a.mb * q.nc > kMaxBlocks ||
+      (long long)M * up_div(V, 4) / 256 > kMaxBlocks)
+    return fail(RPD_ERR_BAD_SHAPE, "M * V or M * d is too large (M=%d V=%d d=%d)", M, V, d);
+  const Fp8Space w = fp8_space(q, a, logits == nullptr);
+  st = check_workspace(workspace, workspace_bytes, w.bytes);
+  if (st != RPD_OK) return st;
+  char* ws = static_cast<char*>(workspace);
+  a.xrows = reinterpret_cast<uint8_t*>(ws);
+  a.partials = reinterpret_cast<float4*>(ws + w.partials);
+  a.sums = reinterpret_cast<float*>(ws + w.sums);
+  const hipError_t e = launch_fp8_project(q, a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(RPD_ERR_HIP, "launch: %s", hipGetErrorString(e));
+  return RPD_OK;
+}
+
+}  // extern "C"

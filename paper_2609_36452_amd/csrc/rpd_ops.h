@@ -1,5 +1,6 @@
 // Internal interface between the C ABI of the operators around the commit step
-// (rpd_ops.cpp) and their gfx950 kernels (quant.hip, verify.hip, distill.hip).
+// (rpd_ops.cpp, rpd_fp8.cpp) and their gfx950 kernels (quant.hip, verify.hip,
+// distill.hip, fp8.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -131,5 +132,55 @@ struct DistillCall {
 
 hipError_t launch_distill_loss(const DistillCall& a, hipStream_t s);   // with a.grad the gradient as well
 hipError_t launch_distill_grad(const DistillCall& a, hipStream_t s);
+
+// --------------------------------------------------------------- fp8.hip --
+
+constexpr int kFp8Block = 128;       // columns, and rows of a matrix, that share a scale
+constexpr int kFp8TileRows = 256;    // rows of the head a workgroup
+constexpr int kFp8TileBlocks = 4;    // blocks of 16 rows of x a workgroup, at most
+
+struct Fp8Quantize {
+  int rows, d, nb, dtype;   // nb: blocks of columns
+  const void* x;            // [rows][d], rows x_stride elements apart
+  long long x_stride;
+  uint8_t* codes;           // [rows][d], rows codes_stride apart
+  long long codes_stride;
+  float* scales;            // [rows or blocks of rows][nb]
+};
+
+// a head as it is packed: V rows of d columns (of a transposed one, the other way round)
+struct Fp8Dims {
+  int V, d;
+  int nc, n16, nr;          // chunks of 128 columns, tiles of 16 rows, blocks of 128 rows
+  size_t scale_offset, bytes;
+};
+
+struct Fp8Call {
+  const uint8_t* packed;
+  const float* scales;      // [nr][nc]
+  int M;
+  const void* x;            // [M][d], rows x_stride elements apart
+  long long x_stride;
+  int x_type;
+  void* out;                // [M][V], rows out_stride elements apart; NULL: statistics
+  long long out_stride;
+  int out_type;
+  float logit_scale;
+  int32_t* argmax;          // NULL: logits
+  float* confidence;
+  float* entropy;
+  // workspace
+  uint8_t* xrows;           // [mb][nc][4096]: bf16 operands
+  float4* partials;         // [M][nvt]
+  float* sums;              // [splits][M][16 n16], of more than one split
+  // plan
+  int mb, nb;               // blocks of 16 rows of x: all of them, and of a workgroup
+  int nrt, nvt, splits;     // workgroups = nrt x nvt x splits
+};
+
+hipError_t launch_fp8_quantize(const Fp8Quantize& a, int block_rows, hipStream_t s);
+hipError_t launch_fp8_pack(const Fp8Dims& q, const uint8_t* codes, const float* scales, bool transpose, uint8_t* packed,
+                           hipStream_t s);
+hipError_t launch_fp8_project(const Fp8Dims& q, const Fp8Call& a, hipStream_t s);
 
 }  // namespace rpd

@@ -618,6 +618,61 @@ rpd_status rpd_fp8_project(int32_t V, int32_t d, const void* packed, int32_t M, 
                            float* confidence, float* entropy, float logit_scale, void* workspace, size_t workspace_bytes,
                            void* stream);
 
+/*
+ * Sampling from rows of logits, from given random numbers. The tokens of a row
+ * are taken in order of their logits, the largest first, equal ones by index;
+ * with e_j = e^(scale (z_j - z_0)) of the j-th, those are kept that pass every
+ * filter:
+ *   top_k   j < top_k (0: off)
+ *   top_p   e_0 + .. + e_(j-1) < top_p * (the sum over what top_k leaves), or
+ *           j = 0 (1 and more: off)
+ *   min_p   e_j >= min_p (0: off)
+ * The token is the first in that order with e_0 + .. + e_j > r * (the sum over
+ * the kept). A logit of -inf is never kept. A row with NaN or +inf, or of
+ * nothing but -inf, has no distribution: token -1, probability NaN, none kept.
+ *   N, V       0 <= N < 2^22 (0: nothing is done), 1 <= V <= 2^20
+ *   dtype      of the logits: RPD_DTYPE_BF16, _F16 or _F32
+ *   logits     device [N][V], rows logits_stride >= V apart
+ *   r          device [N] float32 in [0, 1)
+ *   logit_scale, top_k, top_p, min_p   for all rows: an inverse temperature,
+ *              finite and > 0, or 0 for 1; >= 0; > 0; in 0 .. 1
+ *   scales, top_ks, top_ps, min_ps   device [N] float32 (top_ks int32), one for
+ *              each row, in place of the number, or NULL. Values out of range:
+ *              a scale of 0 is 1, one below 0 or not finite leaves the row no
+ *              distribution; top_k below 0 is off; top_p of 0 and less keeps
+ *              one token, NaN is off; min_p below 0 or NaN is off, above 1 is 1
+ *   token      device [N] int32
+ *   prob       device [N] float32 or NULL: the token's probability among the kept
+ *   kept       device [N] int32 or NULL: how many were kept
+ *   filtered   device [N][V] of the logits' type or NULL, rows filtered_stride
+ *              >= V apart: the logits of the kept tokens, -inf elsewhere (as
+ *              rpd_verify_draft takes them); must not overlap the logits
+ * Sums are of 64 bits; equal inputs give equal outputs.
+ */
+typedef struct rpd_sample {
+  int32_t N, V, dtype;
+  const void* logits;
+  int64_t logits_stride;
+  const float* r;
+  float logit_scale;
+  int32_t top_k;
+  float top_p, min_p;
+  const float* scales;
+  const int32_t* top_ks;
+  const float* top_ps;
+  const float* min_ps;
+  int32_t* token;
+  float* prob;
+  int32_t* kept;
+  void* filtered;
+  int64_t filtered_stride;
+} rpd_sample;
+
+/* Workspace bytes of rpd_sample_tokens (pointers only tested for NULL); 0 if
+ * the shape is out of range or none is needed. */
+size_t rpd_sample_workspace_size(const rpd_sample* p);
+rpd_status rpd_sample_tokens(const rpd_sample* p, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Static text for a status code. */
 const char* rpd_status_string(rpd_status s);
 

@@ -73,6 +73,16 @@ class RpdDistill(ctypes.Structure):
                 ("state", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("grad_stride", ctypes.c_int64)]
 
 
+class RpdSample(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("logits", ctypes.c_void_p), ("logits_stride", ctypes.c_int64), ("r", ctypes.c_void_p),
+                ("logit_scale", ctypes.c_float), ("top_k", ctypes.c_int32), ("top_p", ctypes.c_float),
+                ("min_p", ctypes.c_float), ("scales", ctypes.c_void_p), ("top_ks", ctypes.c_void_p),
+                ("top_ps", ctypes.c_void_p), ("min_ps", ctypes.c_void_p), ("token", ctypes.c_void_p),
+                ("prob", ctypes.c_void_p), ("kept", ctypes.c_void_p), ("filtered", ctypes.c_void_p),
+                ("filtered_stride", ctypes.c_int64)]
+
+
 _OUT_FIELDS = ["commit", "token", "entropy", "confidence", "persistence", "drop", "stability", "flags",
                "upstream_entropy", "n_commit", "layer_argmax", "layer_conf", "layer_entropy", "status"]
 
@@ -155,6 +165,7 @@ def lib() -> ctypes.CDLL:
                                        ctypes.c_void_p, ctypes.c_void_p]
         v, i32, i64, size = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
         head, ver, dis = ctypes.POINTER(RpdQuantHead), ctypes.POINTER(RpdVerify), ctypes.POINTER(RpdDistill)
+        sam = ctypes.POINTER(RpdSample)
         for name, res, args in (
                 ("rpd_quant_packed_size", size, [head]),
                 ("rpd_quant_pack", ctypes.c_int, [head, v, v, v, v, size, v]),
@@ -171,7 +182,9 @@ def lib() -> ctypes.CDLL:
                 ("rpd_fp8_pack", ctypes.c_int, [i32, i32, v, v, i32, v, size, v]),
                 ("rpd_fp8_workspace_size", size, [i32, i32, i32, i32]),
                 ("rpd_fp8_project", ctypes.c_int,
-                 [i32, i32, v, i32, v, i64, i32, v, i64, i32, v, v, v, ctypes.c_float, v, size, v])):
+                 [i32, i32, v, i32, v, i64, i32, v, i64, i32, v, v, v, ctypes.c_float, v, size, v]),
+                ("rpd_sample_workspace_size", size, [sam]),
+                ("rpd_sample_tokens", ctypes.c_int, [sam, v, size, v])):
             f = getattr(L, name)
             f.restype, f.argtypes = res, args
         L.rpd_status_string.restype = ctypes.c_char_p
@@ -970,3 +983,50 @@ class Fp8Head:
         out = self._out(grad, "grad", self.d, out_dtype, out)
         self._project(self.packed_t, self.d, self.V, grad, "grad", out, None, 1.0, stream)
         return out
+
+
+def _of_rows(name: str, value, default, lead: tuple, dtype: torch.dtype):
+    """A parameter of ``sample``: (the number for all rows, the address of a tensor of one for each)."""
+    if not torch.is_tensor(value):
+        return value, None
+    _check_dev(name, value, lead, (dtype,))
+    return default, value.data_ptr()
+
+
+def sample(logits: torch.Tensor, r: torch.Tensor, logit_scale: float | torch.Tensor = 1.0,
+           top_k: int | torch.Tensor = 0, top_p: float | torch.Tensor = 1.0, min_p: float | torch.Tensor = 0.0,
+           filtered: bool = False, stream=None) -> dict:
+    """``rpd_sample_tokens``: a token of every row of logits [..., V] (bfloat16, float16 or float32), from given random
+    numbers r float32 [...] in [0, 1), after temperature (``logit_scale`` is its inverse), top-k, top-p and min-p in
+    that order (0, 1 and 0: off; top_k=1 is greedy). Each is a number, or a device tensor [...] with one for each row
+    (float32, top_k int32). Returns token int32, prob float32 (the token's probability among the kept) and kept int32
+    (how many were kept) of r's shape, and with ``filtered`` the logits with -inf for what was not kept, as
+    ``verify_draft`` takes them. Not recorded by autograd. ``stream`` as in ``verify_draft``."""
+    extra = {k: v for k, v in dict(logit_scale=logit_scale, top_k=top_k, top_p=top_p, min_p=min_p).items()
+             if torch.is_tensor(v)}
+    dev = _one_device("logits", logits, r=r, **extra)
+    code = _float_code("logits", logits)
+    logits = logits.detach()
+    rows = _rows("logits", logits)
+    lead = tuple(logits.shape[:-1])
+    _check_dev("r", r, lead, (torch.float32,))
+    scale, scales = _of_rows("logit_scale", logit_scale, 1.0, lead, torch.float32)
+    k, ks = _of_rows("top_k", top_k, 0, lead, torch.int32)
+    p, ps = _of_rows("top_p", top_p, 1.0, lead, torch.float32)
+    least, leasts = _of_rows("min_p", min_p, 0.0, lead, torch.float32)
+    o = {"token": torch.empty(lead, dtype=torch.int32, device=dev),
+         "prob": torch.empty(lead, dtype=torch.float32, device=dev),
+         "kept": torch.empty(lead, dtype=torch.int32, device=dev)}
+    if filtered:
+        o["logits"] = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    problem = RpdSample(rows.shape[0], rows.shape[1], code, rows.data_ptr(), _row_stride(rows), r.data_ptr(),
+                        float(scale), int(k), float(p), float(least), scales, ks, ps, leasts, o["token"].data_ptr(),
+                        o["prob"].data_ptr(), o["kept"].data_ptr(), _ptr(o.get("logits")), max(rows.shape[1], 1))
+    nbytes = int(lib().rpd_sample_workspace_size(ctypes.byref(problem)))
+    ws = None
+    if nbytes:
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        if stream is not None:
+            ws.record_stream(stream)
+    _enqueue(dev, stream, lib().rpd_sample_tokens, ctypes.byref(problem), _ptr(ws), nbytes)
+    return o

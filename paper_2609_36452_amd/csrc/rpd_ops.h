@@ -1,6 +1,6 @@
 // Internal interface between the C ABI of the operators around the commit step
-// (rpd_ops.cpp, rpd_fp8.cpp) and their gfx950 kernels (quant.hip, verify.hip,
-// distill.hip, fp8.hip).
+// (rpd_ops.cpp, rpd_fp8.cpp, rpd_sample.cpp) and their gfx950 kernels (quant.hip,
+// verify.hip, distill.hip, fp8.hip, sample.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -182,5 +182,28 @@ hipError_t launch_fp8_quantize(const Fp8Quantize& a, int block_rows, hipStream_t
 hipError_t launch_fp8_pack(const Fp8Dims& q, const uint8_t* codes, const float* scales, bool transpose, uint8_t* packed,
                            hipStream_t s);
 hipError_t launch_fp8_project(const Fp8Dims& q, const Fp8Call& a, hipStream_t s);
+
+// ------------------------------------------------------------ sample.hip --
+
+struct SampleCall {
+  int N, V, dtype;
+  const void* logits;       // [N][V], rows stride elements apart
+  long long stride;
+  const float* r;           // [N]
+  float scale;
+  int top_k;
+  float top_p, min_p;
+  const float* scales;      // [N] in place of the numbers, or NULL
+  const int32_t* top_ks;
+  const float* top_ps;
+  const float* min_ps;
+  int32_t* token;           // [N]
+  float* prob;              // [N] or NULL
+  int32_t* kept;            // [N] or NULL
+  void* filtered;           // [N][V] or NULL
+  long long filtered_stride;
+};
+
+hipError_t launch_sample(const SampleCall& a, hipStream_t s);
 
 }  // namespace rpd

@@ -69,3 +69,59 @@ def product_bound(w, x):
     additions of the blocks (parts of the sum among them)."""
     terms = torch.matmul(x.abs(), w.abs().t().contiguous())
     return (BLOCK + -(-w.shape[1] // BLOCK) + 4) * U32 * terms
+
+
+# --------------------------------------------------------------- sampling --
+
+def in_order(z):
+    """(logits in order, float64, their indexes): the largest first, equal ones by index; -inf left out."""
+    order = torch.argsort(-z.double(), stable=True)
+    t = z.double()[order]
+    n = int((t > -math.inf).sum())
+    return t[:n], order[:n]
+
+
+def f32(v):
+    return float(torch.tensor(v, dtype=torch.float32))
+
+
+def check_sample(z, r, scale, top_k, top_p, min_p, token, prob, kept, filtered=None, slack=1e-9):
+    """One row's outputs against the definition in float64. Where a border lies within `slack` of the whole mass of a
+    token's edge, either side of it is right."""
+    scale, top_p, min_p = f32(scale), f32(top_p), f32(min_p)
+    scale = 1.0 if scale == 0 else scale
+    zz = z.double()
+    if bool(zz.isnan().any()) or not bool(zz.isfinite().any()) or bool((zz == math.inf).any()) or not 0 < scale < math.inf:
+        assert token == -1 and kept == 0 and math.isnan(prob)
+        if filtered is not None:
+            assert bool((filtered == -math.inf).all())
+        return
+    t, order = in_order(z)
+    x = (t - t[0]) * scale
+    e = x.exp()
+    n = len(t)
+    if top_k > 0:
+        n = min(n, top_k)
+    c = e.cumsum(0)
+    before = c - e
+    least, most = n, n
+    if top_p < 1:
+        T = top_p * float(c[n - 1])
+        s = slack * float(c[n - 1])
+        least = max(1, int((before[:n] < T - s).sum()))
+        most = max(1, int((before[:n] < T + s).sum()))
+    if min_p > 0:
+        m = int((x >= math.log(min(min_p, 1.0)) - 0.0).sum())
+        least, most = min(least, m), min(most, m)
+    assert least <= kept <= most, (kept, least, most, n)
+    S = float(c[kept - 1])
+    at = (order[:kept] == token).nonzero()
+    assert at.numel() == 1, "a token that was not kept"
+    j = int(at[0, 0])
+    s = slack * S
+    assert float(before[j]) <= r * S + s and (float(c[j]) >= r * S - s or j == kept - 1), (j, r * S, float(before[j]), float(c[j]))
+    assert abs(prob - float(e[j]) / S) <= 2.0 ** -24 * prob + 1e-9
+    if filtered is not None:
+        want = torch.full_like(z, -math.inf)
+        want[order[:kept]] = z[order[:kept]]
+        assert torch.equal(filtered, want)

@@ -1,5 +1,6 @@
 """What 8-bit blocks, the head in them and sampling refuse, on the host, before anything is enqueued; and the float64
 forms that their GPU tests compare with."""
+import ctypes
 import math
 
 import pytest
@@ -97,3 +98,46 @@ def test_reference_codes_are_torch_casts():
         # with half the scale the largest would not fit
         top = torch.nn.functional.pad(x.abs(), (0, 84, 0, -130 % per)).double().view(-(-130 // per), per, 3, 128).amax((1, 3))
         assert bool((top <= 448 * scales).all()) and bool((top > 224 * scales).all())
+
+
+# --------------------------------------------------------------- sampling --
+
+def _sample(**kw):
+    a = dict(N=4, V=1000, dtype=rpd.DTYPE_BF16, logits=P, ls=1000, r=2 * P, scale=1.0, k=0, p=1.0, least=0.0, scales=None,
+             ks=None, ps=None, leasts=None, token=3 * P, prob=3 * P, kept=3 * P, filtered=None, fs=0)
+    a.update(kw)
+    return rpd.RpdSample(*a.values())
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(N=-1), 2), (dict(N=1 << 22), 2), (dict(V=0), 2), (dict(V=(1 << 20) + 1, ls=1 << 21), 2), (dict(dtype=4), 5),
+    (dict(ls=999), 2), (dict(filtered=4 * P, fs=999), 2), (dict(scale=-1.0), 3), (dict(scale=math.nan), 3),
+    (dict(scale=math.inf), 3), (dict(k=-1), 3), (dict(p=0.0), 3), (dict(p=-0.5), 3), (dict(p=math.nan), 3),
+    (dict(least=-0.1), 3), (dict(least=1.1), 3), (dict(least=math.nan), 3), (dict(logits=None), 1), (dict(r=None), 1),
+    (dict(token=None), 1), (dict(logits=P + 1), 5), (dict(dtype=rpd.DTYPE_F32, logits=P + 2), 5), (dict(r=P + 2), 5),
+    (dict(token=P + 1), 5), (dict(prob=P + 2), 5), (dict(kept=P + 2), 5), (dict(scales=P + 2), 5), (dict(ks=P + 2), 5),
+    (dict(ps=P + 2), 5), (dict(leasts=P + 2), 5), (dict(filtered=4 * P + 1, fs=1000), 5), (dict(filtered=P, fs=1000), 3),
+    (dict(filtered=P + 7998, fs=1000), 3), (dict(filtered=P - 7998, fs=1000), 3)])
+def test_sample_refusals(kw, status):
+    assert rpd.lib().rpd_sample_tokens(ctypes.byref(_sample(**kw)), P, 1 << 40, None) == status
+    assert rpd.last_error()
+
+
+def test_sample_nothing():
+    assert rpd.lib().rpd_sample_tokens(ctypes.byref(_sample(N=0, logits=None)), None, 0, None) == 0
+    assert rpd.lib().rpd_sample_tokens(None, None, 0, None) == 1
+
+
+def test_reference_sample():
+    """The definition on a row that is known by hand: masses 4, 2, 1, 1 by halves."""
+    z = torch.log(torch.tensor([1.0, 4.0, 1.0, 2.0], dtype=torch.float64))
+    ok = dict(scale=1.0, top_k=0, top_p=1.0, min_p=0.0)
+    R.check_sample(z, 0.49, **ok, token=1, prob=0.5, kept=4)
+    R.check_sample(z, 0.51, **ok, token=3, prob=0.25, kept=4)
+    R.check_sample(z, 0.76, **ok, token=0, prob=0.125, kept=4)
+    R.check_sample(z, 0.9, **{**ok, "top_k": 2}, token=3, prob=1 / 3, kept=2)
+    R.check_sample(z, 0.2, **{**ok, "top_p": 0.4}, token=1, prob=1.0, kept=1)
+    R.check_sample(z, 0.9, **{**ok, "min_p": 0.4}, token=3, prob=1 / 3, kept=2)
+    for wrong in (dict(token=3, prob=0.25, kept=4), dict(token=1, prob=0.4, kept=4), dict(token=1, prob=0.5, kept=3)):
+        with pytest.raises(AssertionError):
+            R.check_sample(z, 0.49, **ok, **wrong)

@@ -67,8 +67,14 @@ struct Bins {
   double m_upto[kBins];
 };
 
+constexpr int kListed = 4096;   // tokens of a bin that are taken out of the row
+
 struct Shared {
   Bins all, part;
+  uint32_t list_key[kListed];
+  int list_index[kListed];
+  uint32_t listed;
+  int list_bin;                    // whose tokens the list holds, or -1
   uint32_t wave_n[kWaves];
   double wave_m[kWaves];
   float wave_top[kWaves];
@@ -156,6 +162,7 @@ struct Bound {
 // The token found: the `at`-th (by index) of `eq` tokens of the logit `key`, before which lie n tokens of mass m; each has mass w.
 struct Place {
   uint32_t key, n, eq, at;
+  int bin;
   double m, w;
   __device__ __forceinline__ uint32_t rank() const { return n + at; }
   __device__ __forceinline__ double upto() const { return m + (double)(at + 1) * w; }
@@ -225,20 +232,41 @@ __device__ Place find(const typename E::t* row, int V, const Weigh& w, uint32_t 
     __syncthreads();
   }
   uint32_t lo = s.lo, hi = s.hi;
+  const bool listed = count <= kListed;
+  if (listed && s.list_bin != b) {
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      s.listed = 0;
+      s.list_bin = b;
+    }
+    __syncthreads();
+    each<E>(row, V, [&](float z, int i) {
+      const uint32_t k = key_of(z);
+      if (k >= lo && k <= hi) {
+        const uint32_t at = atomicAdd(&s.listed, 1u);
+        s.list_key[at] = k;
+        s.list_index[at] = i;
+      }
+    });
+  }
   while (lo < hi) {
     const uint32_t span = hi - lo;
     const int bits = 32 - __builtin_clz(span), shift = max(0, bits - 11);   // span >> shift < 2048
     __syncthreads();
     clear(s.part);
     __syncthreads();
-    each<E>(row, V, [&](float z, int) {
-      const uint32_t k = key_of(z);
+    auto add = [&](uint32_t k) {
       if (k >= lo && k <= hi) {
         const int i = (int)((hi - k) >> shift);
         atomicAdd(&s.part.n[i], 1u);
-        atomicAdd(&s.part.mass[i], Weigh::mass(w.bins_below(z), b));
+        atomicAdd(&s.part.mass[i], Weigh::mass(w.bins_below(value_of(k)), b));
       }
-    });
+    };
+    if (listed) {
+      for (uint32_t i = threadIdx.x; i < s.listed; i += kThreads) add(s.list_key[i]);
+    } else {
+      each<E>(row, V, [&](float z, int) { add(key_of(z)); });
+    }
     __syncthreads();
     scan<false>(s.part, unit, s);
     const uint32_t i = (uint32_t)choose(s.part, q, n, m, s);
@@ -247,10 +275,12 @@ __device__ Place find(const typename E::t* row, int V, const Weigh& w, uint32_t 
     const uint32_t width = (1u << shift) - 1;
     lo = hi - lo > width ? hi - width : lo;
   }
+  __syncthreads();
   Place p;
   p.key = hi;
   p.n = n;
   p.eq = count;
+  p.bin = b;
   p.m = m;
   const float z = value_of(hi);
   p.w = (double)Weigh::mass(w.bins_below(z), b) * unit;
@@ -276,6 +306,17 @@ __device__ int index_of(const typename E::t* row, int V, const Place& p, Shared&
   if (t < 64) s.slab[t] = 0;
   if (t == 0) s.token = -1;
   __syncthreads();
+  if (s.list_bin == p.bin && p.eq <= 64) {
+    for (uint32_t i = t; i < s.listed; i += kThreads) {
+      if (s.list_key[i] != p.key) continue;
+      uint32_t before = 0;
+      for (uint32_t j = 0; p.eq > 1 && j < s.listed; ++j)
+        before += s.list_key[j] == p.key && s.list_index[j] < s.list_index[i];
+      if (before == p.at) s.token = s.list_index[i];
+    }
+    __syncthreads();
+    return s.token;
+  }
   // 64 slabs of whole vectors
   const int slab = ((V + 63) / 64 + 7) / 8 * 8;
   each<E>(row, V, [&](float z, int i) {
@@ -309,10 +350,10 @@ __device__ int index_of(const typename E::t* row, int V, const Place& p, Shared&
   return s.token;
 }
 
+// a row of any type and length, read from memory in each pass
 template <class E>
-__global__ __launch_bounds__(kThreads) void k_sample(SampleCall a) {
-  __shared__ Shared s;
-  const int n = blockIdx.x, t = threadIdx.x, lane = t & 63, wid = t >> 6, V = a.V;
+__device__ __noinline__ void sample_row(const SampleCall a, int n, Shared& s) {
+  const int t = threadIdx.x, lane = t & 63, wid = t >> 6, V = a.V;
   const typename E::t* row = static_cast<const typename E::t*>(a.logits) + n * a.stride;
   typename E::t* out = a.filtered ? static_cast<typename E::t*>(a.filtered) + n * a.filtered_stride : nullptr;
   const float scale = a.scales ? a.scales[n] : a.scale;
@@ -328,9 +369,12 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleCall a) {
   });
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
-  if (lane == 0) s.wave_top[wid] = top;
-  if (lane == 0) s.wave_bad[wid] = 0;
-  if (__any(bad) && lane == 0) s.wave_bad[wid] = 1;
+  const bool any_bad = __any(bad);
+  if (lane == 0) {
+    s.wave_top[wid] = top;
+    s.wave_bad[wid] = any_bad;
+  }
+  if (t == 0) s.list_bin = -1;
   clear(s.all);
   __syncthreads();
   for (int w = 0; w < kWaves; ++w) {
@@ -417,12 +461,480 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleCall a) {
   });
 }
 
+template <class E>
+__global__ __launch_bounds__(kThreads) void k_sample(SampleCall a) {
+  __shared__ Shared s;
+  sample_row<E>(a, blockIdx.x, s);
+}
+
+// ------------------------------------------------- 16-bit logits, held in registers --
+//
+// A row of up to 163840 logits of 16 bits fits a workgroup's registers, and a
+// table with a 16-bit count for each of the 65536 values fits its LDS. So the
+// row is read once and counted by value, one LDS addition a token; masses are
+// then counts times the exponential of a value, and no token needs one of its
+// own. A thread sums the 64 values of its block of the table (equally spaced:
+// they share an exponent, so their exponentials are a geometric series, one
+// multiply-add each); bounds are found by the first wave alone, in the blocks'
+// running sums and then in a block, a value a lane.
+//
+// Values are slots, falling as they rise: 0 .. 0x7fff the positive ones from
+// the largest down, 0x8000 .. the negative ones. What is 64 nats and more below
+// the maximum has no mass (e^-64 of it) and is not counted.
+
+template <class E>
+struct Slots;
+template <>
+struct Slots<Bf16> {
+  static constexpr uint32_t low = 0xff80;   // of -inf
+};
+template <>
+struct Slots<F16> {
+  static constexpr uint32_t low = 0xfc00;
+};
+constexpr uint32_t kZero = 0x7fff, kMinusZero = 0x8000;
+
+template <class E>
+__device__ __forceinline__ float slot_value(uint32_t s) {
+  const uint16_t b = (uint16_t)(s & 0x8000 ? s : s ^ 0x7fff);
+  return E::one(&b);
+}
+template <class E>
+__device__ __forceinline__ uint32_t slot_of(float z) {
+  const uint32_t b = E::to(z);
+  return b & 0x8000 ? b : b ^ 0x7fff;
+}
+// both halves
+__device__ __forceinline__ uint32_t slots_of(uint32_t w) {
+  const uint32_t sign = (w >> 15) & 0x10001u;
+  return w ^ (0x7fff7fffu - sign * 0x7fffu);
+}
+
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+struct KeyBound {
+  bool by_rank, reach;
+  uint32_t rank;
+  double mass;
+};
+struct KeyPlace {   // as Place, with a slot in place of the key
+  uint32_t slot, n, eq, at;
+  double m, w;
+  __device__ __forceinline__ uint32_t rank() const { return n + at; }
+  __device__ __forceinline__ double upto() const { return m + (double)(at + 1) * w; }
+};
+
+struct Keys {
+  uint32_t count[32768];   // two values a word
+  uint32_t n_upto[kThreads];
+  double m_upto[kThreads];
+  uint32_t wave_n[kWaves];
+  double wave_m[kWaves];
+  uint32_t wave_lo[kWaves], wave_hi[kWaves];
+  KeyPlace cut, pick;
+  int is_cut, give_up, token;
+  uint32_t kept;
+  double mass;
+  uint32_t slab[64];
+};
+
+// By the first wave: the token at which a bound is passed.
+template <class E>
+__device__ __forceinline__ KeyPlace find_key(const Keys& s, const Weigh& w, const KeyBound& q) {
+  const int lane = threadIdx.x & 63;
+  // the block: each lane looks at 16 in a row
+  int first = kThreads, last = -1;
+#pragma unroll 4
+  for (int j = 15; j >= 0; --j) {
+    const int b = lane * 16 + j;
+    const uint32_t upto = s.n_upto[b], n = upto - (b ? s.n_upto[b - 1] : 0);
+    const double m = s.m_upto[b];
+    const bool past = q.by_rank ? upto > q.rank : q.reach ? m >= q.mass : m > q.mass;
+    if (n > 0 && past) first = b;
+    if (n > 0) last = max(last, b);
+  }
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) {
+    first = min(first, __shfl_xor(first, k));
+    last = max(last, __shfl_xor(last, k));
+  }
+  const int b = first < kThreads ? first : last;   // by rounding alone: the last that holds anything
+  const uint32_t n0 = b ? s.n_upto[b - 1] : 0;
+  const double m0 = b ? s.m_upto[b - 1] : 0.0;
+  // the value, a lane each
+  const uint32_t slot = b * 64 + lane, word = s.count[slot >> 1], c = slot & 1 ? word >> 16 : word & 0xffff;
+  const double e = c ? exp(w.bins_below(slot_value<E>(slot)) * (-1.0 / kPerNat)) : 0.0;
+  uint32_t n = c;
+  double m = c * e;
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) {
+    const uint32_t on = __shfl_up(n, k);
+    const double om = __shfl_up(m, k);
+    n += lane >= k ? on : 0;
+    m += lane >= k ? om : 0.0;
+  }
+  const bool past = c > 0 && (q.by_rank ? n0 + n > q.rank : q.reach ? m0 + m >= q.mass : m0 + m > q.mass);
+  const unsigned long long hits = __ballot(past), some = __ballot(c > 0);
+  const int at = hits ? __builtin_ctzll(hits) : 63 - __builtin_clzll(some);
+  const uint32_t before = __shfl_up(n, 1);
+  const double m_before = __shfl_up(m, 1);
+  KeyPlace p;
+  p.slot = b * 64 + at;
+  p.eq = __shfl(c, at);
+  p.n = n0 + (at ? __shfl(before, at) : 0);
+  p.m = m0 + (at ? __shfl(m_before, at) : 0.0);
+  p.w = __shfl(e, at);
+  if (q.by_rank) {
+    p.at = min(q.rank - p.n, p.eq - 1);
+  } else {
+    auto over = [&](double i) { return q.reach ? p.m + (i + 1.0) * p.w >= q.mass : p.m + (i + 1.0) * p.w > q.mass; };
+    double i = p.w > 0.0 ? floor((q.mass - p.m) / p.w) : 0.0;
+    i = fmin(fmax(i, 0.0), (double)(p.eq - 1));
+    while (i > 0.0 && over(i - 1.0)) i -= 1.0;
+    while (i < (double)(p.eq - 1) && !over(i)) i += 1.0;
+    p.at = (uint32_t)i;
+  }
+  return p;
+}
+
+template <class E, int NV>
+__global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
+  constexpr size_t kBytes = sizeof(Keys) > sizeof(Shared) ? sizeof(Keys) : sizeof(Shared);
+  __shared__ __attribute__((aligned(16))) unsigned char lds[kBytes];
+  Keys& s = *reinterpret_cast<Keys*>(lds);
+  const int n = blockIdx.x, t = threadIdx.x, lane = t & 63, wid = t >> 6, V = a.V;
+  const typename E::t* row = static_cast<const typename E::t*>(a.logits) + n * a.stride;
+  const float scale = a.scales ? a.scales[n] : a.scale;
+  const int top_k = a.top_ks ? a.top_ks[n] : a.top_k;
+  const float top_p = a.top_ps ? a.top_ps[n] : a.top_p, min_p = a.min_ps ? a.min_ps[n] : a.min_p;
+
+  uint32_t v[NV][4];   // vector j holds tokens 8 (t + 1024 j) .. of the row
+  const int steps = (V + 8 * kThreads - 1) / (8 * kThreads);
+  Eight<E> end_of_row;
+  constexpr uint32_t kLows = Slots<E>::low * 0x10001u;
+  end_of_row.v = u32x4{kLows, kLows, kLows, kLows};
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    u32x4 x = {kLows, kLows, kLows, kLows};
+    if (j < steps - 1) x = reinterpret_cast<const Any16*>(row + 8 * (t + j * kThreads))->v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[j][e] = x[e];
+  }
+  if (8 * (t + (steps - 1) * kThreads) < V) load_eight<E>(row, 8 * (t + (steps - 1) * kThreads), V, end_of_row);
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[j][e] = j == steps - 1 ? end_of_row.v[e] : v[j][e];
+  for (int i = t; i < 8192; i += kThreads) reinterpret_cast<u32x4*>(s.count)[i] = u32x4{0u, 0u, 0u, 0u};
+  if (t < 64) s.slab[t] = 0;
+  if (t == 0) {
+    s.give_up = 0;
+    s.token = -1;
+  }
+  u16x2 lo = {0xffff, 0xffff}, hi = {0, 0};
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[j][e] = slots_of(v[j][e]);
+      asm("" : "+v"(v[j][e]));   // kept in place of what it came from
+      lo = __builtin_elementwise_min(lo, __builtin_bit_cast(u16x2, v[j][e]));
+      hi = __builtin_elementwise_max(hi, __builtin_bit_cast(u16x2, v[j][e]));
+    }
+  }
+  uint32_t first = min((uint32_t)lo.x, (uint32_t)lo.y), last = max((uint32_t)hi.x, (uint32_t)hi.y);
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) {
+    first = min(first, (uint32_t)__shfl_xor((int)first, k));
+    last = max(last, (uint32_t)__shfl_xor((int)last, k));
+  }
+  if (lane == 0) {
+    s.wave_lo[wid] = first;
+    s.wave_hi[wid] = last;
+  }
+  __syncthreads();
+  for (int k = 0; k < kWaves; ++k) {
+    first = min(first, s.wave_lo[k]);
+    last = max(last, s.wave_hi[k]);
+  }
+  if (first == kMinusZero) first = kZero;
+  const float top = slot_value<E>(first), sc = scale == 0.f ? 1.f : scale;
+  // NaN (on either side) or +inf in the row, nothing but -inf, or no temperature
+  if (last > Slots<E>::low || first >= Slots<E>::low || !(fabsf(top) < INFINITY) || !(sc > 0.f && sc < INFINITY)) {
+    __syncthreads();
+    sample_row<E>(a, n, *reinterpret_cast<Shared*>(lds));
+    return;
+  }
+  const Weigh w(top, sc);
+  const bool least = min_p > 0.f;
+  const double limit = least ? -log(fmin((double)min_p, 1.0)) * kPerNat : 0.0;
+  // slots beyond `end` are not counted: 64 nats below; of min_p alone, what it leaves out (`limit` and a little more)
+  const bool min_alone = least && top_k <= 0 && !(top_p < 1.f);
+  const double reach_bins = min_alone ? fmin(limit + 1.0, 64.0 * kPerNat) : 64.0 * kPerNat;
+  const uint32_t end = min(slot_of<E>((float)((double)top - reach_bins / ((double)sc * kPerNat))), Slots<E>::low - 1);
+  uint32_t infs = 0, seen = 0;   // seen: what was counted
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    if (j < steps) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t x = v[j][e], x0 = x & 0xffff, x1 = x >> 16;
+        if (x0 <= end) atomicAdd(&s.count[x0 >> 1], x0 & 1 ? 0x10000u : 1u);
+        if (x1 <= end) atomicAdd(&s.count[x1 >> 1], x1 & 1 ? 0x10000u : 1u);
+        infs += (x0 == Slots<E>::low) + (x1 == Slots<E>::low);
+        seen += (x0 <= end) + (x1 <= end);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);   // one vector at a time: the row takes most of the registers
+  }
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) {
+    infs += __shfl_xor(infs, k);
+    seen += __shfl_xor(seen, k);
+  }
+  if (lane == 0) {
+    s.wave_n[wid] = infs;
+    s.wave_hi[wid] = seen;
+  }
+  __syncthreads();
+  infs = seen = 0;
+  for (int k = 0; k < kWaves; ++k) {
+    infs += s.wave_n[k];
+    seen += s.wave_hi[k];
+  }
+  const uint32_t finite = (uint32_t)(steps * 8 * kThreads) - infs;   // (what is past the row's end is -inf as well)
+  if (t == 0) {   // the two zeros are equal
+    const uint32_t minus = s.count[kMinusZero >> 1] & 0xffff;
+    if (minus) {
+      if ((s.count[kZero >> 1] >> 16) + minus > 0xffff) s.give_up = 1;
+      s.count[kZero >> 1] += minus << 16;
+      s.count[kMinusZero >> 1] -= minus;
+    }
+  }
+  __syncthreads();
+  // the block of 64 values: z_i = z_0 - i u from the maximum's slot on, so the masses are e_0 rho^i
+  uint32_t bn = 0;
+  double bm = 0.0;
+  {
+    const u32x4* p = reinterpret_cast<const u32x4*>(&s.count[t * 32]);
+    uint32_t any = 0;
+#pragma unroll 4
+    for (int j = 0; j < 8; ++j) {
+      const u32x4 c = p[(j + t) & 7];   // lanes 128 bytes apart: spread over the banks
+      any |= c[0] | c[1] | c[2] | c[3];
+    }
+    if (any) {
+      const uint32_t start = t * 64;
+      const int i0 = first > start ? (int)(first - start) : 0;
+      const float z0 = slot_value<E>(start + i0), u = slot_value<E>(start) - slot_value<E>(start + 1);
+      const double e0 = exp(w.bins_below(z0) * (-1.0 / kPerNat)), rho = exp(-(double)u * w.k * (1.0 / kPerNat));
+#pragma unroll 2
+      for (int i = 31; i >= 0; --i) {
+        const uint32_t x = s.count[t * 32 + i];
+        if (2 * i + 1 >= i0) {
+          bm = fma(bm, rho, (double)(x >> 16));
+          if (2 * i >= i0) bm = fma(bm, rho, (double)(x & 0xffff));
+        }
+        bn += (x & 0xffff) + (x >> 16);
+      }
+      bm *= e0;
+    }
+  }
+  uint32_t un = bn;
+  double um = bm;
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) {
+    const uint32_t on = __shfl_up(un, k);
+    const double om = __shfl_up(um, k);
+    un += lane >= k ? on : 0;
+    um += lane >= k ? om : 0.0;
+  }
+  if (lane == 63) {
+    s.wave_lo[wid] = un;
+    s.wave_m[wid] = um;
+  }
+  __syncthreads();
+  uint32_t counted = 0, base_n = 0;
+  double base_m = 0.0;
+  for (int k = 0; k < kWaves; ++k) {
+    base_n += k < wid ? s.wave_lo[k] : 0;
+    base_m += k < wid ? s.wave_m[k] : 0.0;
+    counted += s.wave_lo[k];
+  }
+  s.n_upto[t] = base_n + un;
+  s.m_upto[t] = base_m + um;
+  __syncthreads();
+  // A count that ran over its 16 bits shows in their sum. Those, and ranks among what is not counted, are rare and left
+  // to the other way.
+  const bool far = top_k > 0 && (uint32_t)top_k > counted && (uint32_t)top_k < finite;
+  const bool low = least && limit > 63.0 * kPerNat;
+  if (seen != counted || s.give_up || far || low) {
+    __syncthreads();
+    sample_row<E>(a, n, *reinterpret_cast<Shared*>(lds));
+    return;
+  }
+  if (wid == 0) {
+    uint32_t kept = finite;
+    double mass = s.m_upto[kThreads - 1];
+    KeyPlace cut{};
+    bool is_cut = false;
+    if (top_k > 0 && (uint32_t)top_k < kept) {
+      cut = find_key<E>(s, w, KeyBound{true, false, (uint32_t)top_k - 1, 0.0});
+      is_cut = true;
+      kept = top_k;
+      mass = cut.upto();
+    }
+    if (top_p < 1.f) {
+      const KeyPlace p = find_key<E>(s, w, KeyBound{false, true, 0, fmax((double)top_p, 0.0) * mass});
+      if (p.rank() + 1 < kept) {
+        cut = p;
+        is_cut = true;
+        kept = p.rank() + 1;
+        mass = p.upto();
+      }
+    }
+    if (least) {
+      // the blocks whose first value min_p leaves, then the values of the last of them
+      int b = 0;
+#pragma unroll 2
+      for (int j = 0; j < 16; ++j) {
+        const int k = lane * 16 + j;
+        const uint32_t x = min(max((uint32_t)k * 64, first), Slots<E>::low - 1);
+        if (w.bins_below(slot_value<E>(x)) <= limit) b = k;
+      }
+#pragma unroll
+      for (int k = 32; k >= 1; k >>= 1) b = max(b, __shfl_xor(b, k));
+      const uint32_t slot = b * 64 + lane, word = s.count[slot >> 1], c = slot & 1 ? word >> 16 : word & 0xffff;
+      uint32_t in = c && w.bins_below(slot_value<E>(slot)) <= limit ? c : 0;
+#pragma unroll
+      for (int k = 32; k >= 1; k >>= 1) in += __shfl_xor(in, k);
+      in += b ? s.n_upto[b - 1] : 0;
+      if (in < kept) {
+        cut = find_key<E>(s, w, KeyBound{true, false, in - 1, 0.0});
+        is_cut = true;
+        kept = in;
+        mass = cut.upto();
+      }
+    }
+    KeyPlace p = find_key<E>(s, w, KeyBound{false, false, 0, (double)a.r[n] * mass});
+    if (is_cut && p.rank() > cut.rank()) p = cut;   // by rounding alone
+    if (lane == 0) {
+      s.pick = p;
+      s.cut = cut;
+      s.is_cut = is_cut;
+      if (a.prob) a.prob[n] = (float)(p.w / mass);
+      if (a.kept) a.kept[n] = (int)kept;
+    }
+  }
+  __syncthreads();
+  // the index of the at-th token of a slot: in order of j, then of the threads, then inside the vector
+  auto index_of = [&](const KeyPlace& p) __attribute__((always_inline)) {
+    auto same = [&](uint32_t x) __attribute__((always_inline)) { return x == p.slot || (p.slot == kZero && x == kMinusZero); };
+    __syncthreads();
+    if (t == 0) s.token = -1;
+    if (t < 64) s.slab[t] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      if (j >= steps) continue;
+      uint32_t c = 0;
+      int at = 0;
+#pragma unroll
+      for (int e = 3; e >= 0; --e) {
+        const bool h = same(v[j][e] >> 16), l = same(v[j][e] & 0xffff);
+        at = l ? 2 * e : h ? 2 * e + 1 : at;
+        c += h + l;
+      }
+      if (c) {
+        if (p.eq == 1) s.token = 8 * (t + j * kThreads) + at;
+        else atomicAdd(&s.slab[j], c);
+      }
+    }
+    __syncthreads();
+    if (p.eq > 1) {
+      uint32_t before = 0;
+      int slab = 0;
+      for (; slab < NV - 1 && before + s.slab[slab] <= p.at; ++slab) before += s.slab[slab];
+      uint32_t c = 0, mask = 0;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (j == slab) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) mask |= (uint32_t)same(e & 1 ? v[j][e >> 1] >> 16 : v[j][e >> 1] & 0xffff) << e;
+        }
+      c = __popc(mask);
+      uint32_t upto = c;
+#pragma unroll
+      for (int k = 1; k < 64; k <<= 1) {
+        const uint32_t o = __shfl_up(upto, k);
+        upto += lane >= k ? o : 0;
+      }
+      if (lane == 63) s.wave_n[wid] = upto;
+      __syncthreads();
+      for (int k = 0; k < wid; ++k) before += s.wave_n[k];
+      before += upto - c;
+      if (p.at >= before && p.at < before + c) {
+        for (uint32_t i = before; i < p.at; ++i) mask &= mask - 1;
+        s.token = 8 * (t + slab * kThreads) + __builtin_ctz(mask);
+      }
+      __syncthreads();
+    }
+    return s.token;
+  };
+  const int token = index_of(s.pick);
+  if (t == 0) a.token[n] = token;
+  if (!a.filtered) return;
+  typename E::t* out = static_cast<typename E::t*>(a.filtered) + n * a.filtered_stride;
+  // what comes before the cut's slot stays, and of its tokens those up to the last kept one
+  const KeyPlace cut = s.cut;
+  const bool is_cut = s.is_cut;
+  uint32_t slot = is_cut ? cut.slot : Slots<E>::low;
+  int until = V;
+  if (is_cut && cut.at + 1 < cut.eq) until = index_of(cut);
+  if (slot == kZero) slot = kMinusZero;
+  const uint32_t after = slot, tie = is_cut && cut.slot == kZero ? kZero : slot;   // ties: tie .. after
+  const uint32_t gone = E::to(-INFINITY);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int i0 = 8 * (t + j * kThreads);
+    if (j >= steps || i0 >= V) continue;
+    u32x4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t x = v[j][e], x0 = x & 0xffff, x1 = x >> 16;
+      const bool k0 = x0 < tie || (x0 <= after && i0 + 2 * e <= until), k1 = x1 < tie || (x1 <= after && i0 + 2 * e + 1 <= until);
+      const uint32_t b = slots_of(x);   // its own inverse on the sign's halves
+      o[e] = (k0 ? b & 0xffff : gone) | (k1 ? b & 0xffff0000u : gone << 16);
+    }
+    if (i0 + 8 <= V) {
+      reinterpret_cast<Any16*>(out + i0)->v = o;
+    } else {
+      for (int e = 0; i0 + e < V; ++e) out[i0 + e] = (typename E::t)(o[e >> 1] >> (16 * (e & 1)));
+    }
+  }
+}
+
+template <class E>
+void sample_keys(const SampleCall& a, hipStream_t s) {
+  constexpr int kStep = 8 * kThreads;
+  if (a.V <= 4 * kStep)
+    k_sample_keys<E, 4><<<a.N, kThreads, 0, s>>>(a);
+  else if (a.V <= 10 * kStep)
+    k_sample_keys<E, 10><<<a.N, kThreads, 0, s>>>(a);
+  else if (a.V <= 16 * kStep)
+    k_sample_keys<E, 16><<<a.N, kThreads, 0, s>>>(a);
+  else if (a.V <= 20 * kStep)
+    k_sample_keys<E, 20><<<a.N, kThreads, 0, s>>>(a);
+  else
+    k_sample<E><<<a.N, kThreads, 0, s>>>(a);
+}
+
 }  // namespace
 
 hipError_t launch_sample(const SampleCall& a, hipStream_t s) {
   switch (a.dtype) {
-    case RPD_DTYPE_BF16: k_sample<Bf16><<<a.N, kThreads, 0, s>>>(a); break;
-    case RPD_DTYPE_F16: k_sample<F16><<<a.N, kThreads, 0, s>>>(a); break;
+    case RPD_DTYPE_BF16: sample_keys<Bf16>(a, s); break;
+    case RPD_DTYPE_F16: sample_keys<F16>(a, s); break;
     default: k_sample<F32><<<a.N, kThreads, 0, s>>>(a); break;
   }
   return hipGetLastError();

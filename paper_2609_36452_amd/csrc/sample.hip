@@ -506,8 +506,9 @@ __device__ __forceinline__ uint32_t slot_of(float z) {
 }
 // both halves
 __device__ __forceinline__ uint32_t slots_of(uint32_t w) {
-  const uint32_t sign = (w >> 15) & 0x10001u;
-  return w ^ (0x7fff7fffu - sign * 0x7fffu);
+  typedef short i16x2 __attribute__((ext_vector_type(2)));
+  const uint32_t sign = __builtin_bit_cast(uint32_t, __builtin_bit_cast(i16x2, w) >> (short)15);
+  return (sign & w) | (~sign & (w ^ 0x7fff7fffu));
 }
 
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
@@ -525,7 +526,7 @@ struct KeyPlace {   // as Place, with a slot in place of the key
 };
 
 struct Keys {
-  uint32_t count[32768];   // two values a word
+  uint32_t count[32768];   // of slot s in word s % 32768: the positive values in the low halves, the negative in the high ones
   uint32_t n_upto[kThreads];
   double m_upto[kThreads];
   uint32_t wave_n[kWaves];
@@ -538,55 +539,69 @@ struct Keys {
   uint32_t slab[64];
 };
 
+__device__ __forceinline__ uint32_t count_of(const Keys& s, uint32_t slot) {
+  const uint32_t w = s.count[slot & 0x7fff];
+  return slot & 0x8000 ? w >> 16 : w & 0xffff;
+}
+
+// inclusive sums over a wave's lanes, by moves between neighbouring registers' lanes (a shuffle through LDS takes ten
+// times as long, and these stand in a chain)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t lanes_below(uint32_t v) {   // of the lane that CTRL names, 0 where there is none
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double lanes_below(double v) {
+  return __hiloint2double((int)lanes_below<CTRL, ROWS>((uint32_t)__double2hiint(v)),
+                          (int)lanes_below<CTRL, ROWS>((uint32_t)__double2loint(v)));
+}
+template <class T>
+__device__ __forceinline__ T wave_scan(T v) {
+  v += lanes_below<0x111, 0xf>(v);   // 1, 2, 4, 8 lanes below in a row of 16
+  v += lanes_below<0x112, 0xf>(v);
+  v += lanes_below<0x114, 0xf>(v);
+  v += lanes_below<0x118, 0xf>(v);
+  v += lanes_below<0x142, 0xa>(v);   // the last lane of the row below, into rows 1 and 3
+  v += lanes_below<0x143, 0xc>(v);   // lane 31, into rows 2 and 3
+  return v;
+}
+__device__ __forceinline__ double lane_of(double v, int at) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), at), __builtin_amdgcn_readlane(__double2loint(v), at));
+}
+
 // By the first wave: the token at which a bound is passed.
 template <class E>
 __device__ __forceinline__ KeyPlace find_key(const Keys& s, const Weigh& w, const KeyBound& q) {
   const int lane = threadIdx.x & 63;
-  // the block: each lane looks at 16 in a row
-  int first = kThreads, last = -1;
-#pragma unroll 4
-  for (int j = 15; j >= 0; --j) {
-    const int b = lane * 16 + j;
-    const uint32_t upto = s.n_upto[b], n = upto - (b ? s.n_upto[b - 1] : 0);
-    const double m = s.m_upto[b];
-    const bool past = q.by_rank ? upto > q.rank : q.reach ? m >= q.mass : m > q.mass;
-    if (n > 0 && past) first = b;
-    if (n > 0) last = max(last, b);
-  }
-#pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) {
-    first = min(first, __shfl_xor(first, k));
-    last = max(last, __shfl_xor(last, k));
-  }
-  const int b = first < kThreads ? first : last;   // by rounding alone: the last that holds anything
+  auto passed = [&](uint32_t n, double m) { return q.by_rank ? n > q.rank : q.reach ? m >= q.mass : m > q.mass; };
+  // the first of the lanes in whose running sums the bound is passed (by rounding alone, the last that holds anything)
+  auto first_of = [&](uint32_t n, double m, uint32_t before, bool in) {
+    const bool some = in && n > before;
+    const unsigned long long hits = __ballot(some && passed(n, m)), any = __ballot(some);
+    return hits ? __builtin_ctzll(hits) : any ? 63 - __builtin_clzll(any) : 0;
+  };
+  // 64 blocks of the 16 times 64, the block, the value
+  const int g = lane & 15;
+  const int group = first_of(s.n_upto[g * 64 + 63], s.m_upto[g * 64 + 63], g ? s.n_upto[g * 64 - 1] : 0, lane < 16);
+  const int b0 = group * 64 + lane;
+  const int b = group * 64 + first_of(s.n_upto[b0], s.m_upto[b0], b0 ? s.n_upto[b0 - 1] : 0, true);
   const uint32_t n0 = b ? s.n_upto[b - 1] : 0;
   const double m0 = b ? s.m_upto[b - 1] : 0.0;
-  // the value, a lane each
-  const uint32_t slot = b * 64 + lane, word = s.count[slot >> 1], c = slot & 1 ? word >> 16 : word & 0xffff;
+  const uint32_t slot = b * 64 + lane, c = count_of(s, slot);
   const double e = c ? exp(w.bins_below(slot_value<E>(slot)) * (-1.0 / kPerNat)) : 0.0;
-  uint32_t n = c;
-  double m = c * e;
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) {
-    const uint32_t on = __shfl_up(n, k);
-    const double om = __shfl_up(m, k);
-    n += lane >= k ? on : 0;
-    m += lane >= k ? om : 0.0;
-  }
-  const bool past = c > 0 && (q.by_rank ? n0 + n > q.rank : q.reach ? m0 + m >= q.mass : m0 + m > q.mass);
-  const unsigned long long hits = __ballot(past), some = __ballot(c > 0);
-  const int at = hits ? __builtin_ctzll(hits) : 63 - __builtin_clzll(some);
-  const uint32_t before = __shfl_up(n, 1);
-  const double m_before = __shfl_up(m, 1);
+  const uint32_t n = n0 + wave_scan(c);
+  const double m = m0 + wave_scan((double)c * e);
+  const int at = first_of(n, m, n - c, true);
   KeyPlace p;
   p.slot = b * 64 + at;
-  p.eq = __shfl(c, at);
-  p.n = n0 + (at ? __shfl(before, at) : 0);
-  p.m = m0 + (at ? __shfl(m_before, at) : 0.0);
-  p.w = __shfl(e, at);
+  p.eq = __builtin_amdgcn_readlane(c, at);
+  p.n = __builtin_amdgcn_readlane(n, at) - p.eq;
+  p.m = at ? lane_of(m, at - 1) : m0;
+  p.w = lane_of(e, at);
+  p.at = 0;
   if (q.by_rank) {
     p.at = min(q.rank - p.n, p.eq - 1);
-  } else {
+  } else if (p.eq > 1) {
     auto over = [&](double i) { return q.reach ? p.m + (i + 1.0) * p.w >= q.mass : p.m + (i + 1.0) * p.w > q.mass; };
     double i = p.w > 0.0 ? floor((q.mass - p.m) / p.w) : 0.0;
     i = fmin(fmax(i, 0.0), (double)(p.eq - 1));
@@ -597,70 +612,102 @@ __device__ __forceinline__ KeyPlace find_key(const Keys& s, const Weigh& w, cons
   return p;
 }
 
+// NV: vectors of 8 tokens a thread, without the row's last 8192 (at most)
 template <class E, int NV>
 __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
   constexpr size_t kBytes = sizeof(Keys) > sizeof(Shared) ? sizeof(Keys) : sizeof(Shared);
   __shared__ __attribute__((aligned(16))) unsigned char lds[kBytes];
   Keys& s = *reinterpret_cast<Keys*>(lds);
+  constexpr uint32_t kLow = Slots<E>::low;
   const int n = blockIdx.x, t = threadIdx.x, lane = t & 63, wid = t >> 6, V = a.V;
   const typename E::t* row = static_cast<const typename E::t*>(a.logits) + n * a.stride;
   const float scale = a.scales ? a.scales[n] : a.scale;
   const int top_k = a.top_ks ? a.top_ks[n] : a.top_k;
   const float top_p = a.top_ps ? a.top_ps[n] : a.top_p, min_p = a.min_ps ? a.min_ps[n] : a.min_p;
 
-  uint32_t v[NV][4];   // vector j holds tokens 8 (t + 1024 j) .. of the row
-  const int steps = (V + 8 * kThreads - 1) / (8 * kThreads);
-  Eight<E> end_of_row;
-  constexpr uint32_t kLows = Slots<E>::low * 0x10001u;
-  end_of_row.v = u32x4{kLows, kLows, kLows, kLows};
+  // vector j holds tokens 8 (t + 1024 j) .., the tail what is left, `tails` of them; its other places a token again that
+  // the thread holds already, if it holds any
+  uint32_t v[NV][4], tail[4];
+  const int steps = (V - 1) / (8 * kThreads), tail_at = 8 * (t + steps * kThreads), tails = min(max(V - tail_at, 0), 8);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    u32x4 x = {kLows, kLows, kLows, kLows};
-    if (j < steps - 1) x = reinterpret_cast<const Any16*>(row + 8 * (t + j * kThreads))->v;
+    u32x4 x = {0u, 0u, 0u, 0u};
+    if (j < steps) x = reinterpret_cast<const Any16*>(row + 8 * (t + j * kThreads))->v;
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[j][e] = x[e];
   }
-  if (8 * (t + (steps - 1) * kThreads) < V) load_eight<E>(row, 8 * (t + (steps - 1) * kThreads), V, end_of_row);
+  if (tails == 8) {
+    const u32x4 x = reinterpret_cast<const Any16*>(row + tail_at)->v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) tail[e] = x[e];
+  } else {
+    const uint32_t some = tails > 0 ? row[tail_at] : steps > 0 ? v[0][0] & 0xffff : row[0];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      tail[e] = (2 * e < tails ? row[tail_at + 2 * e] : some) | (2 * e + 1 < tails ? row[tail_at + 2 * e + 1] : some) << 16;
+  }
+  for (int i = t; i < 8192; i += kThreads) reinterpret_cast<u32x4*>(s.count)[i] = u32x4{0u, 0u, 0u, 0u};
+  if (t == 0) s.give_up = 0;
+  u16x2 lo = {0xffff, 0xffff}, hi = {0, 0};
+  auto take = [&](uint32_t& x) __attribute__((always_inline)) {
+    x = slots_of(x);
+    asm("" : "+v"(x));   // kept in place of what it came from
+    lo = __builtin_elementwise_min(lo, __builtin_bit_cast(u16x2, x));
+    hi = __builtin_elementwise_max(hi, __builtin_bit_cast(u16x2, x));
+  };
 #pragma unroll
   for (int j = 0; j < NV; ++j)
+    if (j < steps) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[j][e] = j == steps - 1 ? end_of_row.v[e] : v[j][e];
-  for (int i = t; i < 8192; i += kThreads) reinterpret_cast<u32x4*>(s.count)[i] = u32x4{0u, 0u, 0u, 0u};
-  if (t < 64) s.slab[t] = 0;
-  if (t == 0) {
-    s.give_up = 0;
-    s.token = -1;
-  }
-  u16x2 lo = {0xffff, 0xffff}, hi = {0, 0};
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[j][e] = slots_of(v[j][e]);
-      asm("" : "+v"(v[j][e]));   // kept in place of what it came from
-      lo = __builtin_elementwise_min(lo, __builtin_bit_cast(u16x2, v[j][e]));
-      hi = __builtin_elementwise_max(hi, __builtin_bit_cast(u16x2, v[j][e]));
+      for (int e = 0; e < 4; ++e) take(v[j][e]);
     }
-  }
-  uint32_t first = min((uint32_t)lo.x, (uint32_t)lo.y), last = max((uint32_t)hi.x, (uint32_t)hi.y);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) take(tail[e]);
+  const uint32_t mine = min((uint32_t)lo.x, (uint32_t)lo.y);
+  uint32_t first = mine, last = max((uint32_t)hi.x, (uint32_t)hi.y);
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) {
     first = min(first, (uint32_t)__shfl_xor((int)first, k));
     last = max(last, (uint32_t)__shfl_xor((int)last, k));
   }
+  // Of a short list (top_k): a sixteenth of it, the j-th smallest of the lanes' slots, bit by bit: of the lanes that agree
+  // with it so far, those with a 0 come first. The worst of the waves' is a bound for the whole list.
+  uint32_t bound = 0;
+  const bool few = top_k > 0 && top_k <= kThreads;
+  if (few) {
+    const uint32_t own = tails == 0 && steps == 0 ? kLow : mine;   // a lane without a token of its own
+    int j = (top_k + kWaves - 1) / kWaves;
+    unsigned long long left = ~0ull;
+#pragma unroll
+    for (int bit = 15; bit >= 0; --bit) {
+      const unsigned long long zeros = left & ~__ballot(own >> bit & 1);
+      const int c = __popcll(zeros);
+      if (j <= c) {
+        left = zeros;
+      } else {
+        left &= ~zeros;
+        j -= c;
+        bound |= 1u << bit;
+      }
+    }
+  }
   if (lane == 0) {
     s.wave_lo[wid] = first;
     s.wave_hi[wid] = last;
+    s.wave_n[wid] = bound;
   }
   __syncthreads();
+  bound = 0;
   for (int k = 0; k < kWaves; ++k) {
     first = min(first, s.wave_lo[k]);
     last = max(last, s.wave_hi[k]);
+    bound = max(bound, s.wave_n[k]);
   }
-  if (first == kMinusZero) first = kZero;
+  first = __builtin_amdgcn_readfirstlane(first == kMinusZero ? kZero : first);
+  last = __builtin_amdgcn_readfirstlane(last);
   const float top = slot_value<E>(first), sc = scale == 0.f ? 1.f : scale;
   // NaN (on either side) or +inf in the row, nothing but -inf, or no temperature
-  if (last > Slots<E>::low || first >= Slots<E>::low || !(fabsf(top) < INFINITY) || !(sc > 0.f && sc < INFINITY)) {
+  if (last > kLow || first >= kLow || !(fabsf(top) < INFINITY) || !(sc > 0.f && sc < INFINITY)) {
     __syncthreads();
     sample_row<E>(a, n, *reinterpret_cast<Shared*>(lds));
     return;
@@ -668,87 +715,128 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
   const Weigh w(top, sc);
   const bool least = min_p > 0.f;
   const double limit = least ? -log(fmin((double)min_p, 1.0)) * kPerNat : 0.0;
-  // slots beyond `end` are not counted: 64 nats below; of min_p alone, what it leaves out (`limit` and a little more)
+  // Slots beyond `end` are not counted: 64 nats below; of min_p alone, what it leaves out (`limit` and a little more); of
+  // a short list, what no token of it can be.
   const bool min_alone = least && top_k <= 0 && !(top_p < 1.f);
   const double reach_bins = min_alone ? fmin(limit + 1.0, 64.0 * kPerNat) : 64.0 * kPerNat;
-  const uint32_t end = min(slot_of<E>((float)((double)top - reach_bins / ((double)sc * kPerNat))), Slots<E>::low - 1);
-  uint32_t infs = 0, seen = 0;   // seen: what was counted
+  uint32_t end = min(slot_of<E>((float)((double)top - reach_bins / ((double)sc * kPerNat))), kLow - 1);
+  if (few) end = min(end, bound);
+  end = __builtin_amdgcn_readfirstlane(end == kZero ? kMinusZero : end);   // -0 is equal
+  uint32_t infs = 0, seen = V;   // -inf, and what was counted
+  auto count = [&](uint32_t x) __attribute__((always_inline)) {
+    atomicAdd(&s.count[x & 0x7fff], 1u + (x >> 15) * 0xffffu);
+  };
+  if (last <= end) {   // everything
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    if (j < steps) {
+    for (int j = 0; j < NV; ++j) {
+      if (j < steps) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t x = v[j][e], x0 = x & 0xffff, x1 = x >> 16;
-        if (x0 <= end) atomicAdd(&s.count[x0 >> 1], x0 & 1 ? 0x10000u : 1u);
-        if (x1 <= end) atomicAdd(&s.count[x1 >> 1], x1 & 1 ? 0x10000u : 1u);
-        infs += (x0 == Slots<E>::low) + (x1 == Slots<E>::low);
-        seen += (x0 <= end) + (x1 <= end);
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);   // one vector at a time: the row takes most of the registers
-  }
-#pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) {
-    infs += __shfl_xor(infs, k);
-    seen += __shfl_xor(seen, k);
-  }
-  if (lane == 0) {
-    s.wave_n[wid] = infs;
-    s.wave_hi[wid] = seen;
-  }
-  __syncthreads();
-  infs = seen = 0;
-  for (int k = 0; k < kWaves; ++k) {
-    infs += s.wave_n[k];
-    seen += s.wave_hi[k];
-  }
-  const uint32_t finite = (uint32_t)(steps * 8 * kThreads) - infs;   // (what is past the row's end is -inf as well)
-  if (t == 0) {   // the two zeros are equal
-    const uint32_t minus = s.count[kMinusZero >> 1] & 0xffff;
-    if (minus) {
-      if ((s.count[kZero >> 1] >> 16) + minus > 0xffff) s.give_up = 1;
-      s.count[kZero >> 1] += minus << 16;
-      s.count[kMinusZero >> 1] -= minus;
-    }
-  }
-  __syncthreads();
-  // the block of 64 values: z_i = z_0 - i u from the maximum's slot on, so the masses are e_0 rho^i
-  uint32_t bn = 0;
-  double bm = 0.0;
-  {
-    const u32x4* p = reinterpret_cast<const u32x4*>(&s.count[t * 32]);
-    uint32_t any = 0;
-#pragma unroll 4
-    for (int j = 0; j < 8; ++j) {
-      const u32x4 c = p[(j + t) & 7];   // lanes 128 bytes apart: spread over the banks
-      any |= c[0] | c[1] | c[2] | c[3];
-    }
-    if (any) {
-      const uint32_t start = t * 64;
-      const int i0 = first > start ? (int)(first - start) : 0;
-      const float z0 = slot_value<E>(start + i0), u = slot_value<E>(start) - slot_value<E>(start + 1);
-      const double e0 = exp(w.bins_below(z0) * (-1.0 / kPerNat)), rho = exp(-(double)u * w.k * (1.0 / kPerNat));
-#pragma unroll 2
-      for (int i = 31; i >= 0; --i) {
-        const uint32_t x = s.count[t * 32 + i];
-        if (2 * i + 1 >= i0) {
-          bm = fma(bm, rho, (double)(x >> 16));
-          if (2 * i >= i0) bm = fma(bm, rho, (double)(x & 0xffff));
+        for (int e = 0; e < 4; ++e) {
+          count(v[j][e] & 0xffff);
+          count(v[j][e] >> 16);
         }
-        bn += (x & 0xffff) + (x >> 16);
       }
-      bm *= e0;
+      __builtin_amdgcn_sched_barrier(0);   // one vector at a time: the row takes most of the registers
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (2 * e < tails) count(tail[e] & 0xffff);
+      if (2 * e + 1 < tails) count(tail[e] >> 16);
+    }
+  } else {
+    uint32_t in = 0, inf = 0;
+    auto vector = [&](const uint32_t (&x)[4], int tokens) __attribute__((always_inline)) {
+      u16x2 m = {0xffff, 0xffff};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m = __builtin_elementwise_min(m, __builtin_bit_cast(u16x2, x[e]));
+      if (min((uint32_t)m.x, (uint32_t)m.y) <= end) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t y = e & 1 ? x[e >> 1] >> 16 : x[e >> 1] & 0xffff;
+          if (y <= end && e < tokens) {
+            count(y);
+            ++in;
+          }
+        }
+      }
+      if (last == kLow) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) inf += (e & 1 ? x[e >> 1] >> 16 : x[e >> 1] & 0xffff) == kLow && e < tokens;
+      }
+    };
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      if (j < steps) vector(v[j], 8);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    vector(tail, tails);
+#pragma unroll
+    for (int k = 32; k >= 1; k >>= 1) {
+      inf += __shfl_xor(inf, k);
+      in += __shfl_xor(in, k);
+    }
+    __syncthreads();
+    if (lane == 0) {
+      s.wave_n[wid] = inf;
+      s.wave_hi[wid] = in;
+    }
+    __syncthreads();
+    seen = 0;
+    for (int k = 0; k < kWaves; ++k) {
+      infs += s.wave_n[k];
+      seen += s.wave_hi[k];
     }
   }
-  uint32_t un = bn;
-  double um = bm;
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) {
-    const uint32_t on = __shfl_up(un, k);
-    const double om = __shfl_up(um, k);
-    un += lane >= k ? on : 0;
-    um += lane >= k ? om : 0.0;
+  __syncthreads();
+  const uint32_t finite = V - infs;
+  if (t == 0) {   // the two zeros are equal
+    const uint32_t minus = count_of(s, kMinusZero);
+    if (minus) {
+      if (count_of(s, kZero) + minus > 0xffff) s.give_up = 1;
+      s.count[kZero] += minus;
+      s.count[0] -= minus << 16;
+    }
   }
+  __syncthreads();
+  // Four lanes a block of 64 values, 16 values each: equally spaced by u, so the masses are e_0 rho^i.
+  for (int r = 0; r < 4; ++r) {
+    const int at = (r * kThreads + t) * 16, half = at & 0x8000 ? 16 : 0;
+    const u32x4* p = reinterpret_cast<const u32x4*>(&s.count[at & 0x7fff]);
+    u32x4 c[4];
+    uint32_t any = 0, bn = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      c[j] = p[j];
+      any |= c[j][0] | c[j][1] | c[j][2] | c[j][3];
+    }
+    double bm = 0.0;
+    if (any >> half & 0xffff) {
+      const float z0 = slot_value<E>(at), u = z0 - slot_value<E>(at + 1);
+      const double per = -(double)u * w.k * (1.0 / kPerNat), d0 = w.bins_below(z0) * (-1.0 / kPerNat);
+      if (d0 > 600.0) s.give_up = 1;   // so steep that the values above the maximum in its block overflow
+      const double e0 = exp(d0), rho = exp(per), rho2 = rho * rho;
+      double even = 0.0, odd = 0.0;
+#pragma unroll
+      for (int i = 14; i >= 0; i -= 2) {
+        const uint32_t x = c[i >> 2][i & 3] >> half & 0xffff, y = c[i >> 2][(i & 3) + 1] >> half & 0xffff;
+        bn += x + y;
+        even = fma(even, rho2, (double)x);
+        odd = fma(odd, rho2, (double)y);
+      }
+      bm = fma(odd, rho, even) * e0;
+    }
+    bn += __shfl_xor(bn, 1);
+    bm += __shfl_xor(bm, 1);
+    bn += __shfl_xor(bn, 2);
+    bm += __shfl_xor(bm, 2);
+    if ((t & 3) == 0) {
+      s.n_upto[at >> 6] = bn;
+      s.m_upto[at >> 6] = bm;
+    }
+  }
+  __syncthreads();
+  const uint32_t un = wave_scan(s.n_upto[t]);
+  const double um = wave_scan(s.m_upto[t]);
   if (lane == 63) {
     s.wave_lo[wid] = un;
     s.wave_m[wid] = um;
@@ -795,17 +883,13 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
     }
     if (least) {
       // the blocks whose first value min_p leaves, then the values of the last of them
-      int b = 0;
-#pragma unroll 2
-      for (int j = 0; j < 16; ++j) {
-        const int k = lane * 16 + j;
-        const uint32_t x = min(max((uint32_t)k * 64, first), Slots<E>::low - 1);
-        if (w.bins_below(slot_value<E>(x)) <= limit) b = k;
-      }
-#pragma unroll
-      for (int k = 32; k >= 1; k >>= 1) b = max(b, __shfl_xor(b, k));
-      const uint32_t slot = b * 64 + lane, word = s.count[slot >> 1], c = slot & 1 ? word >> 16 : word & 0xffff;
-      uint32_t in = c && w.bins_below(slot_value<E>(slot)) <= limit ? c : 0;
+      auto leaves = [&](uint32_t slot) {
+        return w.bins_below(slot_value<E>(min(max(slot, first), kLow - 1))) <= limit;
+      };
+      const int group = __popcll(__ballot(lane < 16 && leaves(lane * 4096))) - 1;
+      const int b = group * 64 + __popcll(__ballot(leaves(group * 4096 + lane * 64))) - 1;
+      const uint32_t slot = b * 64 + lane, c = count_of(s, slot);
+      uint32_t in = c && leaves(slot) ? c : 0;
 #pragma unroll
       for (int k = 32; k >= 1; k >>= 1) in += __shfl_xor(in, k);
       in += b ? s.n_upto[b - 1] : 0;
@@ -826,105 +910,113 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
       if (a.kept) a.kept[n] = (int)kept;
     }
   }
-  __syncthreads();
-  // the index of the at-th token of a slot: in order of j, then of the threads, then inside the vector
+  // the index of the at-th token of a slot: in order of the vectors, then of the threads, then inside the vector
   auto index_of = [&](const KeyPlace& p) __attribute__((always_inline)) {
-    auto same = [&](uint32_t x) __attribute__((always_inline)) { return x == p.slot || (p.slot == kZero && x == kMinusZero); };
     __syncthreads();
+    const uint32_t slot = __builtin_amdgcn_readfirstlane(p.slot), eq = __builtin_amdgcn_readfirstlane(p.eq),
+                   at = __builtin_amdgcn_readfirstlane(p.at);
+    const bool zero = slot == kZero;
     if (t == 0) s.token = -1;
-    if (t < 64) s.slab[t] = 0;
+    if (t <= NV) s.slab[t] = 0;
     __syncthreads();
+    auto same = [&](uint32_t x) __attribute__((always_inline)) { return x == slot || (zero && x == kMinusZero); };
+    auto matches = [&](const uint32_t (&x)[4], int tokens) __attribute__((always_inline)) {   // a bit a token
+      uint32_t m = 0;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      if (j >= steps) continue;
-      uint32_t c = 0;
-      int at = 0;
+      for (int e = 0; e < 8; ++e) m |= (uint32_t)(same(e & 1 ? x[e >> 1] >> 16 : x[e >> 1] & 0xffff) && e < tokens) << e;
+      return m;
+    };
+    auto vector = [&](const uint32_t (&x)[4], int j, int tokens) __attribute__((always_inline)) {
+      // a half that is equal leaves 0 in place of 1
+      auto differ = [&](uint32_t key) __attribute__((always_inline)) {
+        uint32_t r = 0x10001u;
 #pragma unroll
-      for (int e = 3; e >= 0; --e) {
-        const bool h = same(v[j][e] >> 16), l = same(v[j][e] & 0xffff);
-        at = l ? 2 * e : h ? 2 * e + 1 : at;
-        c += h + l;
+        for (int e = 0; e < 4; ++e)
+          r &= __builtin_bit_cast(uint32_t,
+                                  __builtin_elementwise_min(__builtin_bit_cast(u16x2, x[e] ^ key * 0x10001u), u16x2{1, 1}));
+        return r;
+      };
+      uint32_t d = differ(slot);
+      if (zero) d &= differ(kMinusZero);
+      if (d != 0x10001u) {
+        const uint32_t m = matches(x, tokens);
+        if (m && eq == 1) s.token = 8 * (t + j * kThreads) + __builtin_ctz(m);
+        else if (m) atomicAdd(&s.slab[j < steps ? j : NV], __popc(m));
       }
-      if (c) {
-        if (p.eq == 1) s.token = 8 * (t + j * kThreads) + at;
-        else atomicAdd(&s.slab[j], c);
-      }
-    }
+    };
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j < steps) vector(v[j], j, 8);
+    vector(tail, steps, tails);
     __syncthreads();
-    if (p.eq > 1) {
+    if (eq > 1) {
       uint32_t before = 0;
-      int slab = 0;
-      for (; slab < NV - 1 && before + s.slab[slab] <= p.at; ++slab) before += s.slab[slab];
-      uint32_t c = 0, mask = 0;
+      int slab = 0;   // NV: the tail
+      for (; slab < NV && before + s.slab[slab] <= at; ++slab) before += s.slab[slab];
+      uint32_t m = slab == NV ? matches(tail, tails) : 0;
 #pragma unroll
       for (int j = 0; j < NV; ++j)
-        if (j == slab) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) mask |= (uint32_t)same(e & 1 ? v[j][e >> 1] >> 16 : v[j][e >> 1] & 0xffff) << e;
-        }
-      c = __popc(mask);
-      uint32_t upto = c;
-#pragma unroll
-      for (int k = 1; k < 64; k <<= 1) {
-        const uint32_t o = __shfl_up(upto, k);
-        upto += lane >= k ? o : 0;
-      }
+        if (j == slab) m = matches(v[j], 8);
+      const uint32_t c = __popc(m), upto = wave_scan(c);
       if (lane == 63) s.wave_n[wid] = upto;
       __syncthreads();
       for (int k = 0; k < wid; ++k) before += s.wave_n[k];
       before += upto - c;
-      if (p.at >= before && p.at < before + c) {
-        for (uint32_t i = before; i < p.at; ++i) mask &= mask - 1;
-        s.token = 8 * (t + slab * kThreads) + __builtin_ctz(mask);
+      if (at >= before && at < before + c) {
+        for (uint32_t i = before; i < at; ++i) m &= m - 1;
+        s.token = 8 * (t + (slab == NV ? steps : slab) * kThreads) + __builtin_ctz(m);
       }
       __syncthreads();
     }
     return s.token;
   };
+  __syncthreads();
   const int token = index_of(s.pick);
   if (t == 0) a.token[n] = token;
   if (!a.filtered) return;
   typename E::t* out = static_cast<typename E::t*>(a.filtered) + n * a.filtered_stride;
   // what comes before the cut's slot stays, and of its tokens those up to the last kept one
-  const KeyPlace cut = s.cut;
   const bool is_cut = s.is_cut;
-  uint32_t slot = is_cut ? cut.slot : Slots<E>::low;
+  uint32_t slot = __builtin_amdgcn_readfirstlane(is_cut ? s.cut.slot : kLow);
   int until = V;
-  if (is_cut && cut.at + 1 < cut.eq) until = index_of(cut);
-  if (slot == kZero) slot = kMinusZero;
-  const uint32_t after = slot, tie = is_cut && cut.slot == kZero ? kZero : slot;   // ties: tie .. after
+  if (is_cut && s.cut.at + 1 < s.cut.eq) until = index_of(s.cut);
+  const uint32_t tie = slot, after = slot == kZero ? kMinusZero : slot;   // ties: tie .. after
   const uint32_t gone = E::to(-INFINITY);
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int i0 = 8 * (t + j * kThreads);
-    if (j >= steps || i0 >= V) continue;
+  auto left = [&](const uint32_t (&x)[4], int i0) __attribute__((always_inline)) {
     u32x4 o;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const uint32_t x = v[j][e], x0 = x & 0xffff, x1 = x >> 16;
+      const uint32_t x0 = x[e] & 0xffff, x1 = x[e] >> 16;
       const bool k0 = x0 < tie || (x0 <= after && i0 + 2 * e <= until), k1 = x1 < tie || (x1 <= after && i0 + 2 * e + 1 <= until);
-      const uint32_t b = slots_of(x);   // its own inverse on the sign's halves
+      const uint32_t b = slots_of(x[e]);   // its own inverse
       o[e] = (k0 ? b & 0xffff : gone) | (k1 ? b & 0xffff0000u : gone << 16);
     }
-    if (i0 + 8 <= V) {
-      reinterpret_cast<Any16*>(out + i0)->v = o;
-    } else {
-      for (int e = 0; i0 + e < V; ++e) out[i0 + e] = (typename E::t)(o[e >> 1] >> (16 * (e & 1)));
-    }
+    return o;
+  };
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+    if (j < steps) reinterpret_cast<Any16*>(out + 8 * (t + j * kThreads))->v = left(v[j], 8 * (t + j * kThreads));
+  const u32x4 o = left(tail, tail_at);
+  if (tails == 8) {
+    reinterpret_cast<Any16*>(out + tail_at)->v = o;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < tails) out[tail_at + e] = (typename E::t)(o[e >> 1] >> (16 * (e & 1)));
   }
 }
 
 template <class E>
 void sample_keys(const SampleCall& a, hipStream_t s) {
   constexpr int kStep = 8 * kThreads;
-  if (a.V <= 4 * kStep)
+  if (a.V <= 5 * kStep)
     k_sample_keys<E, 4><<<a.N, kThreads, 0, s>>>(a);
   else if (a.V <= 10 * kStep)
-    k_sample_keys<E, 10><<<a.N, kThreads, 0, s>>>(a);
+    k_sample_keys<E, 9><<<a.N, kThreads, 0, s>>>(a);
   else if (a.V <= 16 * kStep)
-    k_sample_keys<E, 16><<<a.N, kThreads, 0, s>>>(a);
+    k_sample_keys<E, 15><<<a.N, kThreads, 0, s>>>(a);
   else if (a.V <= 20 * kStep)
-    k_sample_keys<E, 20><<<a.N, kThreads, 0, s>>>(a);
+    k_sample_keys<E, 19><<<a.N, kThreads, 0, s>>>(a);
   else
     k_sample<E><<<a.N, kThreads, 0, s>>>(a);
 }

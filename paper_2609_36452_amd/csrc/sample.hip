@@ -60,6 +60,15 @@ struct Weigh {
   static __device__ __forceinline__ double unit(int b) { return b == kFar ? 0.0 : exp(-(double)b / kPerNat) / kUnit; }
 };
 
+// The token found: the `at`-th (by index) of `eq` tokens of the logit `key`, before which lie n tokens of mass m; each has mass w.
+struct Place {
+  uint32_t key, n, eq, at;
+  int index;   // or -1: not known yet
+  double m, w;
+  __device__ __forceinline__ uint32_t rank() const { return n + at; }
+  __device__ __forceinline__ double upto() const { return m + (double)(at + 1) * w; }
+};
+
 struct Bins {
   uint32_t n[kBins];               // tokens
   unsigned long long mass[kBins];
@@ -71,10 +80,13 @@ constexpr int kListed = 4096;   // tokens of a bin that are taken out of the row
 
 struct Shared {
   Bins all, part;
-  uint32_t list_key[kListed];
+  uint32_t list_key[kListed];      // the tokens with keys list_lo .. list_hi (an empty range at first)
   int list_index[kListed];
-  uint32_t listed;
-  int list_bin;                    // whose tokens the list holds, or -1
+  uint32_t listed, list_lo, list_hi;
+  uint32_t from;                   // keys below are not counted
+  uint32_t few_key[64];            // a bin's tokens, where they are few
+  int few_index[64];
+  uint32_t few;
   uint32_t wave_n[kWaves];
   double wave_m[kWaves];
   float wave_top[kWaves];
@@ -86,6 +98,7 @@ struct Shared {
   double m;
   int token;
   uint32_t slab[64];
+  Place place;
 };
 
 // eight entries at a time of the row, f(value, index), -inf left out by the caller
@@ -159,15 +172,6 @@ struct Bound {
   uint32_t rank;
   double mass;
 };
-// The token found: the `at`-th (by index) of `eq` tokens of the logit `key`, before which lie n tokens of mass m; each has mass w.
-struct Place {
-  uint32_t key, n, eq, at;
-  int bin;
-  double m, w;
-  __device__ __forceinline__ uint32_t rank() const { return n + at; }
-  __device__ __forceinline__ double upto() const { return m + (double)(at + 1) * w; }
-};
-
 // the bin in which the bound falls, with what lies before it (added to n, m)
 __device__ __forceinline__ int choose(const Bins& b, const Bound& q, uint32_t& n, double& m, Shared& s) {
   if (threadIdx.x == 0) {
@@ -231,23 +235,73 @@ __device__ Place find(const typename E::t* row, int V, const Weigh& w, uint32_t 
     }
     __syncthreads();
   }
-  uint32_t lo = s.lo, hi = s.hi;
-  const bool listed = count <= kListed;
-  if (listed && s.list_bin != b) {
+  uint32_t lo = max(s.lo, s.from), hi = s.hi;
+  // a list of the bin's tokens, and of all before them where they fit as well (the next bound falls there)
+  bool listed = s.list_lo <= lo && hi <= s.list_hi;
+  if (!listed && count <= kListed) {
+    const uint32_t to = s.all.n_upto[b] <= kListed ? top : hi;
     __syncthreads();
     if (threadIdx.x == 0) {
       s.listed = 0;
-      s.list_bin = b;
+      s.list_lo = lo;
+      s.list_hi = to;
     }
     __syncthreads();
     each<E>(row, V, [&](float z, int i) {
       const uint32_t k = key_of(z);
-      if (k >= lo && k <= hi) {
-        const uint32_t at = atomicAdd(&s.listed, 1u);
-        s.list_key[at] = k;
-        s.list_index[at] = i;
+      if (k >= lo && k <= to) {
+        const uint32_t at = atomicAdd(&s.listed, 1u);   // (as many as were counted)
+        if (at < kListed) {
+          s.list_key[at] = k;
+          s.list_index[at] = i;
+        }
       }
     });
+    listed = true;
+  }
+  __syncthreads();
+  if (listed && count <= 64) {   // a lane a token: each sees how many, and what mass, come before it
+    if (threadIdx.x == 0) s.few = 0;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < s.listed; i += kThreads) {
+      const uint32_t k = s.list_key[i];
+      if (k >= lo && k <= hi) {
+        const uint32_t at = atomicAdd(&s.few, 1u);
+        if (at < 64) {
+          s.few_key[at] = k;
+          s.few_index[at] = s.list_index[i];
+        }
+      }
+    }
+    __syncthreads();
+    if (threadIdx.x < 64) {
+      const int lane = threadIdx.x;
+      const bool in = lane < (int)count;
+      const uint32_t key = in ? s.few_key[lane] : 0;
+      const int index = in ? s.few_index[lane] : 0;
+      const double e = in ? (double)Weigh::mass(w.bins_below(value_of(key)), b) * unit : 0.0;
+      uint32_t above = 0, equal = 0, at = 0;
+      double mass = m;   // of what is above
+      for (int j = 0; j < (int)count; ++j) {
+        const uint32_t kj = __shfl(key, j);
+        const int ij = __shfl(index, j);
+        const double ej = __shfl(e, j);
+        above += kj > key;
+        mass += kj > key ? ej : 0.0;
+        equal += kj == key;
+        at += kj == key && ij < index;
+      }
+      const uint32_t order = above + at;
+      const double upto = mass + (double)(at + 1) * e;
+      const bool past = in && (q.by_rank ? n + order >= q.rank : q.reach ? upto >= q.mass : upto > q.mass);
+      // the first that is past the bound, by rounding alone the last of all
+      uint32_t best = past ? order : in ? 0x10000u + 64 - order : 0x20000u;
+#pragma unroll
+      for (int k = 32; k >= 1; k >>= 1) best = min(best, (uint32_t)__shfl_xor((int)best, k));
+      if (in && best == (past ? order : 0x10000u + 64 - order)) s.place = Place{key, n + above, equal, at, index, mass, e};
+    }
+    __syncthreads();
+    return s.place;
   }
   while (lo < hi) {
     const uint32_t span = hi - lo;
@@ -280,7 +334,7 @@ __device__ Place find(const typename E::t* row, int V, const Weigh& w, uint32_t 
   p.key = hi;
   p.n = n;
   p.eq = count;
-  p.bin = b;
+  p.index = -1;
   p.m = m;
   const float z = value_of(hi);
   p.w = (double)Weigh::mass(w.bins_below(z), b) * unit;
@@ -301,22 +355,12 @@ __device__ Place find(const typename E::t* row, int V, const Weigh& w, uint32_t 
 // the index of the at-th token (by index) of the logit `key`
 template <class E>
 __device__ int index_of(const typename E::t* row, int V, const Place& p, Shared& s) {
+  if (p.index >= 0) return p.index;
   const int t = threadIdx.x, lane = t & 63, wid = t >> 6;
   __syncthreads();
   if (t < 64) s.slab[t] = 0;
   if (t == 0) s.token = -1;
   __syncthreads();
-  if (s.list_bin == p.bin && p.eq <= 64) {
-    for (uint32_t i = t; i < s.listed; i += kThreads) {
-      if (s.list_key[i] != p.key) continue;
-      uint32_t before = 0;
-      for (uint32_t j = 0; p.eq > 1 && j < s.listed; ++j)
-        before += s.list_key[j] == p.key && s.list_index[j] < s.list_index[i];
-      if (before == p.at) s.token = s.list_index[i];
-    }
-    __syncthreads();
-    return s.token;
-  }
   // 64 slabs of whole vectors
   const int slab = ((V + 63) / 64 + 7) / 8 * 8;
   each<E>(row, V, [&](float z, int i) {
@@ -367,14 +411,34 @@ __device__ __noinline__ void sample_row(const SampleCall a, int n, Shared& s) {
     top = fmaxf(top, z);
     bad |= z != z;
   });
+  // Of a short list (top_k): a sixteenth of it, the j-th largest of the lanes' own best, bit by bit: of the lanes that
+  // agree with it so far, those with a 1 come first. The worst of the waves' is a bound for the whole list.
+  uint32_t bound = 0;
+  const bool few = top_k > 0 && top_k <= kThreads;
+  if (few) {
+    const uint32_t own = key_of(top);
+    int j = (top_k + kWaves - 1) / kWaves;
+    unsigned long long left = ~0ull;
+    for (int bit = 31; bit >= 0; --bit) {
+      const unsigned long long ones = left & __ballot(own >> bit & 1);
+      const int c = __popcll(ones);
+      if (j <= c) {
+        left = ones;
+        bound |= 1u << bit;
+      } else {
+        left &= ~ones;
+        j -= c;
+      }
+    }
+  }
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
   const bool any_bad = __any(bad);
   if (lane == 0) {
     s.wave_top[wid] = top;
     s.wave_bad[wid] = any_bad;
+    s.wave_in[wid] = bound;
   }
-  if (t == 0) s.list_bin = -1;
   clear(s.all);
   __syncthreads();
   for (int w = 0; w < kWaves; ++w) {
@@ -393,28 +457,63 @@ __device__ __noinline__ void sample_row(const SampleCall a, int n, Shared& s) {
     return;
   }
   const Weigh w(top, sc);
+  const uint32_t key_top = key_of(top);
   const bool least = min_p > 0.f;
   const double limit = least ? -log(fmin((double)min_p, 1.0)) * kPerNat : 0.0;
-  uint32_t inside = 0;
-  each<E>(row, V, [&](float z, int) {
-    if (z > -INFINITY) {
+  // What cannot be kept is not counted: what min_p alone leaves out (`limit` and a little more), and of a short list what
+  // is below the worst of the waves' bounds.
+  uint32_t from = key_of(-3.402823466e38f);
+  if (least && top_k <= 0 && !(top_p < 1.f)) from = max(from, key_of((float)((double)top - (limit + 1.0) / w.k)));
+  if (few) {
+    bound = ~0u;
+    for (int v = 0; v < kWaves; ++v) bound = min(bound, s.wave_in[v]);
+    from = max(from, bound);
+  }
+  const bool list = from > key_of(-3.402823466e38f);   // then they are few, and listed at once
+  if (t == 0) {
+    s.listed = 0;
+    s.from = from;
+  }
+  __syncthreads();
+  uint32_t inside = 0, finite = 0;
+  each<E>(row, V, [&](float z, int i) {
+    finite += z > -INFINITY;
+    const uint32_t key = key_of(z);
+    if (key >= from) {
       const double d = w.bins_below(z);
       const int b = d < (double)kFar ? (int)d : kFar;
       atomicAdd(&s.all.n[b], 1u);
       if (b != kFar) atomicAdd(&s.all.mass[b], Weigh::mass(d, b));
       inside += d <= limit;
+      if (list) {
+        const uint32_t at = atomicAdd(&s.listed, 1u);
+        if (at < kListed) {
+          s.list_key[at] = key;
+          s.list_index[at] = i;
+        }
+      }
     }
   });
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) finite += __shfl_xor(finite, k);
+  if (lane == 0) s.wave_n[wid] = finite;
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) inside += __shfl_xor(inside, k);
   if (lane == 0) s.wave_in[wid] = inside;
   __syncthreads();
   inside = 0;
-  for (int v = 0; v < kWaves; ++v) inside += s.wave_in[v];
+  uint32_t kept = 0;
+  for (int v = 0; v < kWaves; ++v) {
+    inside += s.wave_in[v];
+    kept += s.wave_n[v];
+  }
+  if (t == 0) {
+    s.list_lo = list && s.listed <= kListed ? from : 1;
+    s.list_hi = list && s.listed <= kListed ? key_top : 0;
+  }
+  __syncthreads();
   scan<true>(s.all, 0.0, s);
 
-  const uint32_t key_top = key_of(top);
-  uint32_t kept = s.all.n_upto[kBins - 1];
   double mass = s.all.m_upto[kBins - 1];
   Place cut{};
   bool is_cut = false;

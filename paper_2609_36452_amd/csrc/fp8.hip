@@ -277,18 +277,18 @@ __global__ __launch_bounds__(256, 2) void k_fp8_tile(Fp8Dims q, Fp8Call a) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) acc[j][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  auto load_w = [&](int c) {
+  auto load_w = [&](int c, int past) {
 #pragma unroll
     for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        raw[u][h] = __builtin_amdgcn_raw_buffer_load_b128(wrs, wo + h * 1024, (u * q.nc + c) * 2048, NT ? 2 : 0);
+        raw[u][h] = __builtin_amdgcn_raw_buffer_load_b128(wrs, (wo + past) + h * 1024, (u * q.nc + c) * 2048, NT ? 2 : 0);
   };
-  auto load_x = [&](int c, uint8_t* stage) {
+  auto load_x = [&](int c, int past, uint8_t* stage) {
 #pragma unroll
     for (int j = 0; j < NB; ++j)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          xrs, (__attribute__((address_space(3))) void*)(stage + j * 4096 + wid * 1024), 16, xo, (j * q.nc + c) * 4096, 0, 0);
+          xrs, (__attribute__((address_space(3))) void*)(stage + j * 4096 + wid * 1024), 16, xo + past, (j * q.nc + c) * 4096, 0, 0);
   };
   // what this wave has loaded has landed; then all waves' has. (A fence alone does not wait for loads into LDS.)
   auto landed = [] {
@@ -314,13 +314,14 @@ __global__ __launch_bounds__(256, 2) void k_fp8_tile(Fp8Dims q, Fp8Call a) {
         }
         wf[u][t] = __builtin_bit_cast(bf16x8, o);
       }
-    if (c + 1 < c1) {
-      load_x(c + 1, next);
-      load_w(c + 1);
-    }
+    // behind the last chunk: past the resource's end, where nothing is fetched (a branch would cost 30 registers)
+    const int past = c + 1 < c1 ? 0 : INT_MIN;
+    load_x(c + 1, past, next);
+    load_w(c + 1, past);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
+      if (NB > 4) __builtin_amdgcn_sched_barrier(0);   // one block of rows at a time: no registers for the next one's
       bf16x8 xf[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) xf[t] = *reinterpret_cast<const bf16x8*>(stage + j * 4096 + t * 1024 + lane * 16);
@@ -340,8 +341,8 @@ __global__ __launch_bounds__(256, 2) void k_fp8_tile(Fp8Dims q, Fp8Call a) {
   };
 
   if (c0 < c1) {
-    load_x(c0, sx0);
-    load_w(c0);
+    load_x(c0, 0, sx0);
+    load_w(c0, 0);
     landed();
     int c = c0;
     for (; c + 2 <= c1; c += 2) {
@@ -515,7 +516,9 @@ hipError_t launch_fp8_project(const Fp8Dims& q, const Fp8Call& a, hipStream_t s)
     case 3: tile<3>(q, a, s); break;
     case 4: tile<4>(q, a, s); break;
     case 5: tile<5>(q, a, s); break;
-    default: tile<6>(q, a, s); break;
+    case 6: tile<6>(q, a, s); break;
+    case 7: tile<7>(q, a, s); break;
+    default: tile<8>(q, a, s); break;
   }
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (a.argmax) {

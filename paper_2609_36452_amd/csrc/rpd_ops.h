@@ -137,7 +137,7 @@ hipError_t launch_distill_grad(const DistillCall& a, hipStream_t s);
 
 constexpr int kFp8Block = 128;       // columns, and rows of a matrix, that share a scale
 constexpr int kFp8TileRows = 256;    // rows of the head a workgroup
-constexpr int kFp8TileBlocks = 4;    // blocks of 16 rows of x a workgroup, at most
+constexpr int kFp8TileBlocks = 8;    // blocks of 16 rows of x a workgroup, at most
 
 struct Fp8Quantize {
   int rows, d, nb, dtype;   // nb: blocks of columns

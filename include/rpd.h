@@ -594,15 +594,16 @@ size_t rpd_fp8_packed_size(int32_t V, int32_t d); /* 0 if out of range */
 rpd_status rpd_fp8_pack(int32_t V, int32_t d, const uint8_t* codes, const float* scales, int32_t transpose, void* packed,
                         size_t packed_bytes, void* stream);
 
-/* Workspace bytes of rpd_fp8_project for M rows; 0 if out of range. */
+/* Workspace bytes of rpd_fp8_project for M rows (0 for the logits of up to 16
+ * rows of a large head; 0 too if out of range). */
 size_t rpd_fp8_workspace_size(int32_t V, int32_t d, int32_t M, int32_t statistics);
 
 /*
  * M rows through a packed head of V rows and d columns. The rows are quantized
  * first, as rpd_fp8_quantize does with block_rows 1; with x^ what their codes
  * and scales stand for, logits y = W x^, or the softmax statistics of
- * logit_scale * y as rpd_gate_commit takes them (the logits then never reach
- * memory). Codes and x^ are exact operands (magnitudes below 2^-126 may count
+ * logit_scale * y as rpd_gate_commit takes them (of a head of 131072 rows and
+ * more, or of many x, the logits then never reach memory). Codes and x^ are exact operands (magnitudes below 2^-126 may count
  * as 0), sums are float32. Equal rows of the head give equal logits; of equal
  * logits the lowest index is the argmax.
  *   M          0 <= M <= 2^20 (0: nothing is done)
@@ -610,8 +611,8 @@ size_t rpd_fp8_workspace_size(int32_t V, int32_t d, int32_t M, int32_t statistic
  *   logits     device [M][V] of type logits_dtype (any of the three), rows
  *              logits_stride >= V apart; or NULL
  *   argmax, confidence, entropy, logit_scale   as rpd_quant_project's
- *   workspace  rpd_fp8_workspace_size bytes, 256-byte aligned; its prior
- *              contents do not matter
+ *   workspace  rpd_fp8_workspace_size bytes, 256-byte aligned (may be NULL where
+ *              that is 0); its prior contents do not matter
  */
 rpd_status rpd_fp8_project(int32_t V, int32_t d, const void* packed, int32_t M, const void* x, int64_t x_stride,
                            int32_t x_dtype, void* logits, int64_t logits_stride, int32_t logits_dtype, int32_t* argmax,

@@ -17,6 +17,7 @@
 // block, where the bf16 ones are off by 1e-8 to 7e-8. That is too much for
 // float32 logits and for the statistics.)
 #include <cstdint>
+#include <type_traits>
 
 #include "logit_rows.h"
 #include "reduce_device.h"
@@ -211,6 +212,24 @@ __global__ __launch_bounds__(256) void k_fp8_pack_scales(const float* scales, fl
   out[at] = transpose ? scales[(long long)c * nr + r] : scales[at];
 }
 
+// eight quantized entries as bf16 operands (4 significant bits times a power of two); the 16 lanes of a row's block
+__device__ __forceinline__ u32x4 operands_of_eight(const float (&z)[8]) {
+  float top = top_of_eight(z);
+#pragma unroll
+  for (int k = 8; k >= 1; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
+  const float s = scale_of_top(top);
+  const u32x2 c = codes_of_eight(z, inverse_of_power(s));
+  u32x4 o;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    o[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c[h], s, false));
+    o[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c[h], s, true));
+  }
+  return o;
+}
+// where they go in a block of 16 rows x 128 columns: columns 8 i .. of row r, lane quad i / 4, product i % 4
+__device__ __forceinline__ int operand_at(int r, int i) { return (i & 3) * 1024 + ((i >> 2) * 16 + r) * 16; }
+
 // Rows of x quantized, as bf16 operands: blocks of 16 rows x 128 columns, 4 KB
 // each in the order of the four products, [block of rows][chunk]. Rows past
 // the last are zeros.
@@ -227,19 +246,8 @@ __global__ __launch_bounds__(256) void k_fp8_rows(Fp8Dims q, Fp8Call a) {
 #pragma unroll
   for (int j = 0; j < kRowChunks; ++j) {
     if (c0 + j >= q.nc) break;
-    float top = top_of_eight(z[j]);
-#pragma unroll
-    for (int k = 8; k >= 1; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
-    const float s = scale_of_top(top);
-    const u32x2 c = codes_of_eight(z[j], inverse_of_power(s));
-    u32x4 o;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {   // 4 significant bits times a power of two
-      o[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c[h], s, false));
-      o[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c[h], s, true));
-    }
-    // columns 8 i .. of the chunk: lane quad i / 4, product i % 4
-    *reinterpret_cast<u32x4*>(a.xrows + ((long long)mb * q.nc + c0 + j) * 4096 + (i & 3) * 1024 + ((i >> 2) * 16 + r) * 16) = o;
+    const u32x4 o = operands_of_eight(z[j]);
+    *reinterpret_cast<u32x4*>(a.xrows + ((long long)mb * q.nc + c0 + j) * 4096 + operand_at(r, i)) = o;
   }
 }
 
@@ -247,12 +255,17 @@ __global__ __launch_bounds__(256) void k_fp8_rows(Fp8Dims q, Fp8Call a) {
 // chunks. The head goes from memory into registers, a chunk ahead, and is
 // converted there once (a wave has its rows for itself); x goes straight into
 // LDS, which the four waves share, a chunk ahead in two stages.
-// NT: the head past the caches (nobody else reads this part of it).
-template <int NB, bool NT>
+// NT: the head past the caches (nobody else reads this part of it): 82 against
+// 90 us for 16 rows, 92 and 104 for 48, 130 and 136 for 112. E: the workgroup
+// quantizes x itself (a single block of 16 rows: there is time for it beside
+// the loads, while k_fp8_rows' launch and round trip cost 4 us of 85; of two
+// blocks it costs 3 us more than it saves); else (void) x is laid out.
+template <int NB, bool NT, class E>
 __global__ __launch_bounds__(256, 2) void k_fp8_tile(Fp8Dims q, Fp8Call a) {
   __shared__ __attribute__((aligned(1024))) uint8_t sx0[NB * 4096], sx1[NB * 4096];
   int job = 0, vt = 0;
-  if (!map_job(blockIdx.x, a.nvt, a.nrt * a.splits, 0, job, vt)) return;
+  if (!map_job(blockIdx.x, a.tiles, a.nrt * a.splits, 0, job, vt)) return;
+  vt += a.vt0;
   const int rt = job % a.nrt, sp = job / a.nrt;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c0 = (int)((long long)q.nc * sp / a.splits), c1 = (int)((long long)q.nc * (sp + 1) / a.splits);
@@ -266,7 +279,10 @@ __global__ __launch_bounds__(256, 2) void k_fp8_tile(Fp8Dims q, Fp8Call a) {
   };
   const long long wrow = (long long)q.nc * 2048, xrow = (long long)q.nc * 4096;
   const __amdgpu_buffer_rsrc_t wrs = resource(a.packed + min(v0 / 16, q.n16) * wrow, (q.n16 - v0 / 16) * wrow);
-  const __amdgpu_buffer_rsrc_t xrs = resource(a.xrows + mb0 * xrow, (a.mb - mb0) * xrow);
+  constexpr bool kOwn = !std::is_void<E>::value;
+  using X = std::conditional_t<kOwn, E, F32>;
+  const __amdgpu_buffer_rsrc_t xrs =
+      kOwn ? resource(nullptr, 0) : resource(a.xrows + mb0 * xrow, (a.mb - mb0) * xrow);
   const float* sc = a.scales + (long long)min(v0 / kBlock, q.nr - 1) * q.nc;
   const int wo = lane * 16, xo = threadIdx.x * 16;
 
@@ -289,6 +305,21 @@ __global__ __launch_bounds__(256, 2) void k_fp8_tile(Fp8Dims q, Fp8Call a) {
     for (int j = 0; j < NB; ++j)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           xrs, (__attribute__((address_space(3))) void*)(stage + j * 4096 + wid * 1024), 16, xo + past, (j * q.nc + c) * 4096, 0, 0);
+  };
+  // or a thread's 8 columns of a row of each block
+  float own[kOwn ? NB : 1][8];
+  auto fetch_x = [&](int c) {
+    const int r = threadIdx.x >> 4, k = c * kBlock + 8 * (threadIdx.x & 15);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int m = (mb0 + j) * 16 + r;
+      row_eight<X>(m < a.M ? static_cast<const typename X::t*>(a.x) + m * a.x_stride : nullptr, k, q.d, own[j]);
+    }
+  };
+  auto store_x = [&](uint8_t* stage) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      *reinterpret_cast<u32x4*>(stage + j * 4096 + operand_at(threadIdx.x >> 4, threadIdx.x & 15)) = operands_of_eight(own[j]);
   };
   // what this wave has loaded has landed; then all waves' has. (A fence alone does not wait for loads into LDS.)
   auto landed = [] {
@@ -316,7 +347,8 @@ __global__ __launch_bounds__(256, 2) void k_fp8_tile(Fp8Dims q, Fp8Call a) {
       }
     // behind the last chunk: past the resource's end, where nothing is fetched (a branch would cost 30 registers)
     const int past = c + 1 < c1 ? 0 : INT_MIN;
-    load_x(c + 1, past, next);
+    if constexpr (kOwn) fetch_x(c + 1 < c1 ? c + 1 : q.nc);   // (zeros past the columns)
+    else load_x(c + 1, past, next);
     load_w(c + 1, past);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -337,12 +369,15 @@ __global__ __launch_bounds__(256, 2) void k_fp8_tile(Fp8Dims q, Fp8Call a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[j][u][e] = fmaf(s, part[u][e], acc[j][u][e]);
     }
+    if constexpr (kOwn) store_x(next);
     landed();   // the next chunk's, and this stage is free
   };
 
   if (c0 < c1) {
-    load_x(c0, 0, sx0);
+    if constexpr (kOwn) fetch_x(c0);
+    else load_x(c0, 0, sx0);
     load_w(c0, 0);
+    if constexpr (kOwn) store_x(sx0);
     landed();
     int c = c0;
     for (; c + 2 <= c1; c += 2) {
@@ -354,7 +389,7 @@ __global__ __launch_bounds__(256, 2) void k_fp8_tile(Fp8Dims q, Fp8Call a) {
 
   // lane l holds row (l % 16) of a block of x against rows 4 (l / 16) + e of a tile of the head
   const int m0 = mb0 * 16 + (lane & 15), vq = v0 + 4 * (lane >> 4);
-  if (a.argmax) {
+  if (a.argmax && a.splits == 1) {
     float4 (*red)[NB * 16] = reinterpret_cast<float4 (*)[NB * 16]>(sx0);
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
@@ -440,6 +475,40 @@ __global__ __launch_bounds__(256) void k_fp8_join(Fp8Dims q, Fp8Call a) {
   }
 }
 
+// a workgroup a row: the same into its softmax statistics (a small head, whose tiles alone would not fill the GPU)
+__global__ __launch_bounds__(256) void k_fp8_join_stats(Fp8Dims q, Fp8Call a) {
+  __shared__ float4 s_wave[4];
+  const int m = blockIdx.x, lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  const float* p = a.sums + (long long)m * q.n16 * 16;
+  const long long part = (long long)a.M * q.n16 * 16;
+  Soft st = soft_empty();
+  for (int v = 4 * threadIdx.x; v < q.V; v += 1024) {
+    f32x4 y = *reinterpret_cast<const f32x4*>(p + v);
+    for (int s = 1; s < a.splits; ++s) y += *reinterpret_cast<const f32x4*>(p + v + s * part);
+    float z[4];
+    int vi[4];
+    bool ok[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      z[e] = y[e] * a.logit_scale;
+      vi[e] = v + e;
+      ok[e] = v + e < q.V;
+    }
+    st = soft_merge(st, soft_from_values(z, vi, ok));
+  }
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) st = soft_merge(st, soft_shfl_xor(st, k));
+  if (lane == 0) s_wave[wid] = soft_pack(st);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int w = 1; w < 4; ++w) st = soft_merge(st, soft_unpack(s_wave[w]));
+    a.argmax[m] = st.idx == INT_MAX ? -1 : st.idx;
+    a.confidence[m] = 1.f / st.S;
+    a.entropy[m] = logf(st.S) - st.T / st.S;
+  }
+}
+
 // one wave a row: the tiles' states -> argmax, top probability, entropy
 __global__ __launch_bounds__(64) void k_fp8_stats(Fp8Call a) {
   const int m = blockIdx.x, lane = threadIdx.x;
@@ -452,13 +521,35 @@ __global__ __launch_bounds__(64) void k_fp8_stats(Fp8Call a) {
   }
 }
 
+int tile_grid(const Fp8Call& a) { return 8 * ((a.tiles + 7) / 8) * a.nrt * a.splits; }
+
+// more than 16 rows: tiles of 2 to 8 blocks of 16
 template <int NB>
-void tile(const Fp8Dims& q, const Fp8Call& a, hipStream_t s) {
-  const int grid = 8 * ((a.nvt + 7) / 8) * a.nrt * a.splits;
+void tile_of(const Fp8Dims& q, const Fp8Call& a, hipStream_t s) {
   if (a.nrt == 1)
-    k_fp8_tile<NB, true><<<grid, 256, 0, s>>>(q, a);
+    k_fp8_tile<NB, true, void><<<tile_grid(a), 256, 0, s>>>(q, a);
   else
-    k_fp8_tile<NB, false><<<grid, 256, 0, s>>>(q, a);
+    k_fp8_tile<NB, false, void><<<tile_grid(a), 256, 0, s>>>(q, a);
+}
+void tile(const Fp8Dims& q, const Fp8Call& a, hipStream_t s) {
+  switch (a.nb) {
+    case 1: k_fp8_tile<1, false, void><<<tile_grid(a), 256, 0, s>>>(q, a); break;   // a last round's
+    case 2: tile_of<2>(q, a, s); break;
+    case 3: tile_of<3>(q, a, s); break;
+    case 4: tile_of<4>(q, a, s); break;
+    case 5: tile_of<5>(q, a, s); break;
+    case 6: tile_of<6>(q, a, s); break;
+    case 7: tile_of<7>(q, a, s); break;
+    default: tile_of<8>(q, a, s); break;
+  }
+}
+template <class E>
+void own_tile(const Fp8Dims& q, const Fp8Call& a, hipStream_t s) {
+  k_fp8_tile<1, true, E><<<tile_grid(a), 256, 0, s>>>(q, a);
+}
+template <class E>
+void rows(const Fp8Dims& q, const Fp8Call& a, hipStream_t s) {
+  k_fp8_rows<E><<<(unsigned)(a.mb * ((q.nc + kRowChunks - 1) / kRowChunks)), 256, 0, s>>>(q, a);
 }
 
 }  // namespace
@@ -502,26 +593,38 @@ hipError_t launch_fp8_pack(const Fp8Dims& q, const uint8_t* codes, const float* 
 
 hipError_t launch_fp8_project(const Fp8Dims& q, const Fp8Call& a, hipStream_t s) {
   hipError_t e;
-  const unsigned rows = (unsigned)(a.mb * ((q.nc + kRowChunks - 1) / kRowChunks));
-  if (a.x_type == RPD_DTYPE_BF16)
-    k_fp8_rows<Bf16><<<rows, 256, 0, s>>>(q, a);
-  else if (a.x_type == RPD_DTYPE_F16)
-    k_fp8_rows<F16><<<rows, 256, 0, s>>>(q, a);
-  else
-    k_fp8_rows<F32><<<rows, 256, 0, s>>>(q, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  switch (a.nb) {
-    case 1: tile<1>(q, a, s); break;
-    case 2: tile<2>(q, a, s); break;
-    case 3: tile<3>(q, a, s); break;
-    case 4: tile<4>(q, a, s); break;
-    case 5: tile<5>(q, a, s); break;
-    case 6: tile<6>(q, a, s); break;
-    case 7: tile<7>(q, a, s); break;
-    default: tile<8>(q, a, s); break;
+  Fp8Call whole = a;
+  whole.vt0 = 0;
+  whole.tiles = a.vt0;
+  if (!a.xrows) {
+    if (a.x_type == RPD_DTYPE_BF16)
+      own_tile<Bf16>(q, whole, s);
+    else if (a.x_type == RPD_DTYPE_F16)
+      own_tile<F16>(q, whole, s);
+    else
+      own_tile<F32>(q, whole, s);
+  } else {
+    if (a.x_type == RPD_DTYPE_BF16)
+      rows<Bf16>(q, a, s);
+    else if (a.x_type == RPD_DTYPE_F16)
+      rows<F16>(q, a, s);
+    else
+      rows<F32>(q, a, s);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    tile(q, whole, s);
+    if (a.vt0 < a.nvt) {   // the tiles of the last round, in smaller pieces
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      Fp8Call last = a;
+      last.tiles = a.nvt - a.vt0;
+      last.nb = a.last_nb;
+      last.nrt = (a.mb + a.last_nb - 1) / a.last_nb;
+      tile(q, last, s);
+    }
   }
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (a.argmax) {
+  if (a.argmax && a.splits > 1) {
+    k_fp8_join_stats<<<a.M, 256, 0, s>>>(q, a);
+  } else if (a.argmax) {
     k_fp8_stats<<<a.M, 64, 0, s>>>(a);
   } else if (a.splits > 1) {
     const long long n = (long long)a.M * ((q.V + 3) / 4);

@@ -30,16 +30,34 @@ Fp8Dims fp8_dims(int V, int d) {
 constexpr int kWanted = 512;      // workgroups: two on each of 256 CUs
 constexpr int kLeastChunks = 4;   // of a split
 
-void fp8_plan(const Fp8Dims& q, bool stats, Fp8Call& a) {
+// Up to as many rows, the workgroups quantize them themselves: 126464 x 4096, bf16, one row 80 us so and 84 laid out
+// first, 16 rows 82 and 86; 32 rows 90 and 88.
+constexpr int kOwnRows = 16;
+
+void fp8_plan(const Fp8Dims& q, Fp8Call& a) {
+  // As few tiles as 8 blocks of rows allow (no more fit the registers), all of about one size: 1024 rows of 126464 x 4096
+  // 850 us so, 910 in tiles of up to 6 blocks, 963 of up to 4.
   a.mb = (int)up_div(a.M, 16);
   a.nrt = (int)up_div(a.mb, kFp8TileBlocks);
   a.nb = (int)up_div(a.mb, a.nrt);
   a.nrt = (int)up_div(a.mb, a.nb);
   a.nvt = (int)up_div(q.V, kFp8TileRows);
+  // a small head is cut along its columns as well, the parts' sums joined in order
   a.splits = 1;
   const long long tiles = (long long)a.nrt * a.nvt;
-  if (!stats && tiles < kWanted)
+  if (tiles < kWanted)
     a.splits = (int)std::max(1LL, std::min(kWanted / tiles, (long long)q.nc / kLeastChunks));
+  // Where a last round after full ones has at most a quarter of the workgroups that run at a time, its tiles are cut into as
+  // many pieces as fit one (a launch of its own, so of little use to more): 152064 x 3584, bf16, 64 rows 120 us so and 132
+  // in whole tiles, 101 rows 156 and 164, 128 rows 164 and 175; 256 rows, with a third of a round left, 292 and 274.
+  a.vt0 = a.nvt;
+  const long long jobs = tiles * a.splits, rest = jobs % kWanted;
+  if (a.nb >= 4 && jobs > kWanted && rest > 0 && rest <= kWanted / 4) {
+    a.vt0 = (int)((jobs - rest) / a.nrt);
+    const int pieces = std::max(1, kWanted / (a.nvt - a.vt0));
+    a.last_nb = std::min(a.nb, (int)up_div(a.mb, pieces));
+    if (a.last_nb == a.nb) a.vt0 = a.nvt;
+  }
 }
 
 struct Fp8Space {
@@ -47,8 +65,8 @@ struct Fp8Space {
 };
 Fp8Space fp8_space(const Fp8Dims& q, const Fp8Call& a, bool stats) {
   Fp8Space w{};
-  w.partials = round256((size_t)a.mb * q.nc * 4096);
-  w.sums = w.partials + (stats ? round256((size_t)a.M * a.nvt * 16) : 0);
+  w.partials = a.M > kOwnRows ? round256((size_t)a.mb * q.nc * 4096) : 0;
+  w.sums = w.partials + (stats && a.splits == 1 ? round256((size_t)a.M * a.nvt * 16) : 0);
   w.bytes = w.sums + (a.splits > 1 ? round256((size_t)a.splits * a.M * q.n16 * 64) : 0);
   return w;
 }
@@ -122,7 +140,7 @@ size_t rpd_fp8_workspace_size(int32_t V, int32_t d, int32_t M, int32_t statistic
   const Fp8Dims q = fp8_dims(V, d);
   Fp8Call a{};
   a.M = M;
-  fp8_plan(q, statistics != 0, a);
+  fp8_plan(q, a);
   return fp8_space(q, a, statistics != 0).bytes;
 }
 
@@ -166,17 +184,19 @@ rpd_status rpd_fp8_project(int32_t V, int32_t d, const void* packed, int32_t M, 
   a.argmax = argmax;
   a.confidence = confidence;
   a.entropy = entropy;
-  fp8_plan(q, logits == nullptr, a);
+  fp8_plan(q, a);
   if ((long long)a.nrt * (a.nvt + 7) * a.splits > kMaxBlocks || (long long)a.mb * q.nc > kMaxBlocks ||
       (long long)M * up_div(V, 4) / 256 > kMaxBlocks)
     return fail(RPD_ERR_BAD_SHAPE, "M * V or M * d is too large (M=%d V=%d d=%d)", M, V, d);
   const Fp8Space w = fp8_space(q, a, logits == nullptr);
-  st = check_workspace(workspace, workspace_bytes, w.bytes);
-  if (st != RPD_OK) return st;
-  char* ws = static_cast<char*>(workspace);
-  a.xrows = reinterpret_cast<uint8_t*>(ws);
-  a.partials = reinterpret_cast<float4*>(ws + w.partials);
-  a.sums = reinterpret_cast<float*>(ws + w.sums);
+  if (w.bytes > 0) {
+    st = check_workspace(workspace, workspace_bytes, w.bytes);
+    if (st != RPD_OK) return st;
+    char* ws = static_cast<char*>(workspace);
+    a.xrows = M > kOwnRows ? reinterpret_cast<uint8_t*>(ws) : nullptr;
+    a.partials = reinterpret_cast<float4*>(ws + w.partials);
+    a.sums = reinterpret_cast<float*>(ws + w.sums);
+  }
   const hipError_t e = launch_fp8_project(q, a, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(RPD_ERR_HIP, "launch: %s", hipGetErrorString(e));
   return RPD_OK;

@@ -170,12 +170,14 @@ struct Fp8Call {
   float* confidence;
   float* entropy;
   // workspace
-  uint8_t* xrows;           // [mb][nc][4096]: bf16 operands
+  uint8_t* xrows;           // [mb][nc][4096]: bf16 operands; NULL: the workgroups quantize x themselves
   float4* partials;         // [M][nvt]
   float* sums;              // [splits][M][16 n16], of more than one split
   // plan
   int mb, nb;               // blocks of 16 rows of x: all of them, and of a workgroup
   int nrt, nvt, splits;     // workgroups = nrt x nvt x splits
+  int vt0, last_nb;         // tiles from vt0 on, a last round of few, take last_nb blocks of x each (vt0 = nvt: none)
+  int tiles;                // of a launch: vt0 .. vt0 + tiles - 1 (set there)
 };
 
 hipError_t launch_fp8_quantize(const Fp8Quantize& a, int block_rows, hipStream_t s);

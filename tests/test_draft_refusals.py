@@ -44,11 +44,14 @@ def test_head_sizes():
     r = lambda n: (n + 255) // 256 * 256   # noqa: E731
     # 63 tiles of 16 rows, 2 chunks of 128 columns, 2 KB each; 8 x 2 scales
     assert L.rpd_fp8_packed_size(1000, 200) == 63 * 2 * 2048 + r(8 * 2 * 4)
-    # rows as bf16 operands, blocks of 16 x 128; a state for each of 4 tiles
+    # more than 16 rows as bf16 operands, blocks of 16 x 128; a state for each of 4 tiles
+    assert L.rpd_fp8_workspace_size(1000, 200, 33, 0) == 3 * 2 * 4096
+    assert L.rpd_fp8_workspace_size(1000, 200, 33, 1) == 3 * 2 * 4096 + r(33 * 4 * 16)
     assert L.rpd_fp8_workspace_size(1000, 200, 17, 0) == 2 * 2 * 4096
-    assert L.rpd_fp8_workspace_size(1000, 200, 17, 1) == 2 * 2 * 4096 + r(17 * 4 * 16)
-    # a long sum in parts of 4 chunks or more: 20 chunks, 5 parts
-    assert L.rpd_fp8_workspace_size(1000, 20 * 128, 1, 0) == 20 * 4096 + r(5 * 63 * 64)
+    assert L.rpd_fp8_workspace_size(1000, 200, 16, 0) == 0 and L.rpd_fp8_workspace_size(1000, 200, 16, 1) == r(16 * 64)
+    # a long sum in parts of 4 chunks or more: 20 chunks, 5 parts; the statistics of those need no states
+    assert L.rpd_fp8_workspace_size(1000, 20 * 128, 1, 0) == r(5 * 63 * 64)
+    assert L.rpd_fp8_workspace_size(1000, 20 * 128, 40, 1) == 3 * 20 * 4096 + r(5 * 40 * 63 * 64)
     assert L.rpd_fp8_workspace_size(1000, 200, 0, 0) == 0 and L.rpd_fp8_workspace_size(1000, 200, (1 << 20) + 1, 0) == 0
 
 
@@ -68,7 +71,7 @@ def test_pack_refusals(kw, status):
     (dict(out=P + 1), 5), (dict(ot=rpd.DTYPE_F32, out=P + 2), 5), (dict(out=None, am=P + 2, cf=P, en=P), 5),
     (dict(ws=None), 1), (dict(ws=P + 8), 5), (dict(nbytes=16), 4)])
 def test_project_refusals(kw, status):
-    a = dict(packed=P, M=4, x=P, xs=200, xt=rpd.DTYPE_BF16, out=P, os=1000, ot=rpd.DTYPE_BF16, am=None, cf=None, en=None,
+    a = dict(packed=P, M=40, x=P, xs=200, xt=rpd.DTYPE_BF16, out=P, os=1000, ot=rpd.DTYPE_BF16, am=None, cf=None, en=None,
              scale=1.0, ws=P, nbytes=1 << 30)
     a.update(kw)
     s = rpd.lib().rpd_fp8_project(1000, 200, a["packed"], a["M"], a["x"], a["xs"], a["xt"], a["out"], a["os"], a["ot"],

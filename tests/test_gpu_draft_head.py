@@ -182,6 +182,24 @@ def test_head_input_grad(M, d, V, dtype):
     _check(head.input_grad(g), wt, gq)
 
 
+@pytest.mark.parametrize("V,M", [(131073 + 400, 64), (140000, 101), (135500, 49), (131100, 128), (70001, 256)])
+def test_head_last_round_of_tiles(V, M):
+    """Heads whose last tiles are cut into pieces of fewer rows."""
+    note(f"  fp8 last round V={V} M={M}")
+    d = 200
+    codes, scales = R.make_head(V, d, M, DEV)
+    head = rpd.Fp8Head(codes, scales)
+    x = _x(M, d, BF, V)
+    w, xq = R.values(codes.float(), scales, 128), _values_of(x)
+    y = head.logits(x, out_dtype=F32)
+    _check(y, w, xq)
+    o = head.stats(x)
+    assert torch.equal(o["argmax"].long(), y.argmax(1))
+    _, c, h = R.stats(y.double())
+    assert bool(((o["confidence"].double() - c).abs() <= 1e-4 * c).all())
+    assert bool(((o["entropy"].double() - h).abs() <= 1e-4 * (h + 1)).all())
+
+
 def test_head_gradient_of_long_rows():
     """The gradient's sum over a vocabulary is cut into parts, joined in order: twice the same."""
     codes, scales = R.make_head(20011, 333, 3, DEV)

@@ -186,11 +186,20 @@ __global__ __launch_bounds__(256) void k_fp8_pack(const uint8_t* codes, uint8_t*
 // the same of the transposed head (rows k, columns v) by 128 x 128 blocks through LDS
 __global__ __launch_bounds__(256) void k_fp8_pack_transposed(const uint8_t* codes, uint8_t* out, int V, int d, int nc) {
   // row v of the block in LDS at 132 v: a lane reads 16 rows of one column
-  __shared__ uint8_t s[kBlock * 132];
+  __shared__ __attribute__((aligned(4))) uint8_t s[kBlock * 132];
   const int c = blockIdx.x % nc, kb = blockIdx.x / nc, tid = threadIdx.x;   // block of columns (v), of rows (k)
-  for (int i = tid; i < kBlock * kBlock; i += 256) {
-    const int v = c * kBlock + (i >> 7), k = kb * kBlock + (i & 127);
-    s[(i >> 7) * 132 + (i & 127)] = v < V && k < d ? codes[(long long)v * d + k] : 0;
+  if (d % 4 == 0 && (reinterpret_cast<uintptr_t>(codes) & 3) == 0) {
+#pragma unroll 8
+    for (int i = tid; i < kBlock * 32; i += 256) {   // four columns at once
+      const int v = c * kBlock + (i >> 5), k = kb * kBlock + 4 * (i & 31);
+      reinterpret_cast<uint32_t*>(s)[(i >> 5) * 33 + (i & 31)] =
+          v < V && k < d ? *reinterpret_cast<const uint32_t*>(codes + (long long)v * d + k) : 0;
+    }
+  } else {
+    for (int i = tid; i < kBlock * kBlock; i += 256) {
+      const int v = c * kBlock + (i >> 7), k = kb * kBlock + (i & 127);
+      s[(i >> 7) * 132 + (i & 127)] = v < V && k < d ? codes[(long long)v * d + k] : 0;
+    }
   }
   __syncthreads();
   const int rows16 = (d + 15) / 16;

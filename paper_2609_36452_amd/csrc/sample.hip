@@ -901,12 +901,15 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
   for (int r = 0; r < 4; ++r) {
     const int at = (r * kThreads + t) * 16, half = at & 0x8000 ? 16 : 0;
     const u32x4* p = reinterpret_cast<const u32x4*>(&s.count[at & 0x7fff]);
-    u32x4 c[4];
     uint32_t any = 0, bn = 0;
+    const uint32_t from = (uint32_t)(r * kThreads + wid * 64) * 16;   // of the wave's first lane
+    if (from <= end && from + 1024 > first) {
+      // lanes are 64 bytes apart: beginning at another quarter each, they meet all banks
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      c[j] = p[j];
-      any |= c[j][0] | c[j][1] | c[j][2] | c[j][3];
+      for (int j = 0; j < 4; ++j) {
+        const u32x4 c = p[(j + (t >> 2)) & 3];
+        any |= c[0] | c[1] | c[2] | c[3];
+      }
     }
     double bm = 0.0;
     if (any >> half & 0xffff) {
@@ -915,6 +918,9 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
       if (d0 > 600.0) s.give_up = 1;   // so steep that the values above the maximum in its block overflow
       const double e0 = exp(d0), rho = exp(per), rho2 = rho * rho;
       double even = 0.0, odd = 0.0;
+      u32x4 c[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) c[j] = p[j];
 #pragma unroll
       for (int i = 14; i >= 0; i -= 2) {
         const uint32_t x = c[i >> 2][i & 3] >> half & 0xffff, y = c[i >> 2][(i & 3) + 1] >> half & 0xffff;
@@ -1078,17 +1084,23 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
   const bool is_cut = s.is_cut;
   uint32_t slot = __builtin_amdgcn_readfirstlane(is_cut ? s.cut.slot : kLow);
   int until = V;
-  if (is_cut && s.cut.at + 1 < s.cut.eq) until = index_of(s.cut);
-  const uint32_t tie = slot, after = slot == kZero ? kMinusZero : slot;   // ties: tie .. after
-  const uint32_t gone = E::to(-INFINITY);
+  if (is_cut && s.cut.at + 1 < s.cut.eq) until = __builtin_amdgcn_readfirstlane(index_of(s.cut));
+  const uint32_t after = slot == kZero ? kMinusZero : slot;
+  const uint32_t gone = (uint32_t)E::to(-INFINITY) * 0x10001u;
   auto left = [&](const uint32_t (&x)[4], int i0) __attribute__((always_inline)) {
     u32x4 o;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const uint32_t x0 = x[e] & 0xffff, x1 = x[e] >> 16;
-      const bool k0 = x0 < tie || (x0 <= after && i0 + 2 * e <= until), k1 = x1 < tie || (x1 <= after && i0 + 2 * e + 1 <= until);
-      const uint32_t b = slots_of(x[e]);   // its own inverse
-      o[e] = (k0 ? b & 0xffff : gone) | (k1 ? b & 0xffff0000u : gone << 16);
+      // halves above `after` go: 0xffff there
+      const u16x2 y = __builtin_bit_cast(u16x2, x[e]);
+      const u16x2 over = y ^ __builtin_elementwise_min(y, u16x2{(unsigned short)after, (unsigned short)after});
+      uint32_t drop = __builtin_bit_cast(uint32_t, u16x2{0, 0} - __builtin_elementwise_min(over, u16x2{1, 1}));
+      if (until < V) {   // and of the cut's own those behind the last kept one
+        const uint32_t x0 = x[e] & 0xffff, x1 = x[e] >> 16;
+        drop |= x0 >= slot && i0 + 2 * e > until ? 0xffffu : 0;
+        drop |= x1 >= slot && i0 + 2 * e + 1 > until ? 0xffff0000u : 0;
+      }
+      o[e] = (drop & gone) | (~drop & slots_of(x[e]));   // (its own inverse)
     }
     return o;
   };

@@ -636,10 +636,10 @@ rpd_status rpd_fp8_project(int32_t V, int32_t d, const void* packed, int32_t M, 
  *   logits     device [N][V], rows logits_stride >= V apart
  *   r          device [N] float32 in [0, 1)
  *   logit_scale, top_k, top_p, min_p   for all rows: an inverse temperature,
- *              finite and > 0, or 0 for 1; >= 0; > 0; in 0 .. 1
+ *              > 0 and at most 2^100, or 0 for 1; >= 0; > 0; in 0 .. 1
  *   scales, top_ks, top_ps, min_ps   device [N] float32 (top_ks int32), one for
  *              each row, in place of the number, or NULL. Values out of range:
- *              a scale of 0 is 1, one below 0 or not finite leaves the row no
+ *              a scale of 0 is 1, one below 0 or above 2^100 leaves the row no
  *              distribution; top_k below 0 is off; top_p of 0 and less keeps
  *              one token, NaN is off; min_p below 0 or NaN is off, above 1 is 1
  *   token      device [N] int32

@@ -25,8 +25,8 @@ rpd_status rpd_sample_tokens(const rpd_sample* p, void* workspace, size_t worksp
   if (!p) return fail(RPD_ERR_NULL_POINTER, "problem is NULL");
   if (!shape_ok(p)) return fail(RPD_ERR_BAD_SHAPE, "need 0<=N<2^22, 1<=V<=2^20 (got N=%d V=%d)", p->N, p->V);
   if (!is_float_dtype(p->dtype)) return fail(RPD_ERR_UNSUPPORTED, "dtype %d is not supported", p->dtype);
-  if (!p->scales && !scale_ok(p->logit_scale))
-    return fail(RPD_ERR_BAD_PARAM, "logit_scale must be finite and > 0, or 0 for 1 (got %g)", p->logit_scale);
+  if (!p->scales && !(p->logit_scale >= 0.f && p->logit_scale <= kSampleMaxScale))
+    return fail(RPD_ERR_BAD_PARAM, "logit_scale must be > 0 and at most 2^100, or 0 for 1 (got %g)", p->logit_scale);
   if (!p->top_ks && p->top_k < 0) return fail(RPD_ERR_BAD_PARAM, "top_k must be >= 0 (got %d)", p->top_k);
   if (!p->top_ps && !(p->top_p > 0.f)) return fail(RPD_ERR_BAD_PARAM, "top_p must be > 0 (got %g)", p->top_p);
   if (!p->min_ps && !(p->min_p >= 0.f && p->min_p <= 1.f))

@@ -34,31 +34,59 @@ __device__ __forceinline__ float value_of(uint32_t key) {
   return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu));
 }
 
-// Bin and mass of a logit. With d the distance below the maximum in bins, the
-// mass relative to the bin's top is e^(-frac(d) / 32), by its series.
+// Bin and mass of a logit. The bin is the nearest one in float32 (it falls as
+// the logit rises, which is all that is asked of it); the mass relative to the
+// bin's middle, e^x with x the distance from there, is of float64: its series
+// to the fourth power, the fifth spread over the others as Chebyshev
+// polynomials are (x^5 = 5/4 h^2 x^3 - 5/16 h^4 x to within h^5 / 16 for |x| <=
+// h = 1/64: 5e-13 of the mass).
 struct Weigh {
-  double m, k;   // maximum, bins per unit of logit
-  __device__ __forceinline__ Weigh(float top, float scale) : m((double)top), k((double)scale * kPerNat) {}
-  __device__ __forceinline__ double bins_below(float z) const { return (m - (double)z) * k; }
-  __device__ __forceinline__ int bin(float z) const {
-    const double d = bins_below(z);
-    return d < (double)kFar ? (int)d : kFar;
-  }
-  // fixed-point mass of a logit that is d bins below the maximum, in bin b
-  static __device__ __forceinline__ unsigned long long mass(double d, int b) {
-    if (b == kFar) return 0;
-    const double x = ((double)b - d) * (1.0 / kPerNat);   // -1/32 .. 0
-    double p = fma(x, 1.0 / 720, 1.0 / 120);
-    p = fma(x, p, 1.0 / 24);
-    p = fma(x, p, 1.0 / 6);
+  float top, k;       // maximum, bins per unit of logit
+  double m, scale;
+  __device__ __forceinline__ Weigh(float t, float s) : top(t), k(s * (float)kPerNat), m((double)t), scale((double)s) {}
+  // nats below the maximum
+  __device__ __forceinline__ double below(float z) const { return (m - (double)z) * scale; }
+  __device__ __forceinline__ float bin_of(float z) const { return rintf(fminf((top - z) * k, (float)kFar)); }
+  __device__ __forceinline__ int bin(float z) const { return (int)bin_of(z); }
+  // fixed-point mass of a logit in bin b
+  __device__ __forceinline__ unsigned long long mass(float z, float b) const {
+    const double x = fma((double)z - m, scale, (double)(b * (float)(1.0 / kPerNat)));   // |x| about 1/64 at most
+    constexpr double h2 = 1.0 / 4096;
+    double p = fma(x, 1.0 / 24, 1.0 / 6 + 1.25 / 120 * h2);
     p = fma(x, p, 0.5);
-    p = fma(x, p, 1.0);
+    p = fma(x, p, 1.0 - 0.3125 / 120 * h2 * h2);
     p = fma(x, p, 1.0);
     // 2^52 added: the integer nearest to p 2^42 is the sum's low bits
     return (unsigned long long)__double_as_longlong(fma(p, kUnit, 4503599627370496.0)) & 0xfffffffffffffull;
   }
+  // what a bin's fixed-point masses are worth: nothing in the last one
   static __device__ __forceinline__ double unit(int b) { return b == kFar ? 0.0 : exp(-(double)b / kPerNat) / kUnit; }
 };
+
+// inclusive sums over a wave's lanes, by moves between neighbouring registers' lanes (a shuffle through LDS takes ten
+// times as long, and these stand in a chain)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t lanes_below(uint32_t v) {   // of the lane that CTRL names, 0 where there is none
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double lanes_below(double v) {
+  return __hiloint2double((int)lanes_below<CTRL, ROWS>((uint32_t)__double2hiint(v)),
+                          (int)lanes_below<CTRL, ROWS>((uint32_t)__double2loint(v)));
+}
+template <class T>
+__device__ __forceinline__ T wave_scan(T v) {
+  v += lanes_below<0x111, 0xf>(v);   // 1, 2, 4, 8 lanes below in a row of 16
+  v += lanes_below<0x112, 0xf>(v);
+  v += lanes_below<0x114, 0xf>(v);
+  v += lanes_below<0x118, 0xf>(v);
+  v += lanes_below<0x142, 0xa>(v);   // the last lane of the row below, into rows 1 and 3
+  v += lanes_below<0x143, 0xc>(v);   // lane 31, into rows 2 and 3
+  return v;
+}
+__device__ __forceinline__ double lane_of(double v, int at) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), at), __builtin_amdgcn_readlane(__double2loint(v), at));
+}
 
 // The token found: the `at`-th (by index) of `eq` tokens of the logit `key`, before which lie n tokens of mass m; each has mass w.
 struct Place {
@@ -69,33 +97,43 @@ struct Place {
   __device__ __forceinline__ double upto() const { return m + (double)(at + 1) * w; }
 };
 
-struct Bins {
-  uint32_t n[kBins];               // tokens
+// Where a bound falls among the bins, with what lies before it: n tokens of mass m before the bin of `count`.
+struct Spot {
+  int bin;
+  uint32_t n, count;
+  double m;
+};
+struct Counts {
+  uint32_t n[kBins];   // tokens
   unsigned long long mass[kBins];
-  uint32_t n_upto[kBins];          // and up to the bin's end
+};
+struct Bins : Counts {
+  uint32_t n_upto[kBins];   // and up to the bin's end
   double m_upto[kBins];
 };
 
 constexpr int kListed = 4096;   // tokens of a bin that are taken out of the row
 
 struct Shared {
-  Bins all, part;
+  union {
+    struct {
+      Bins all, part;
+    };
+    Counts copies[4];   // a row's tokens are counted by every fourth lane apart: half of a wave would meet in one place
+  };
   uint32_t list_key[kListed];      // the tokens with keys list_lo .. list_hi (an empty range at first)
   int list_index[kListed];
   uint32_t listed, list_lo, list_hi;
   uint32_t from;                   // keys below are not counted
   uint32_t few_key[64];            // a bin's tokens, where they are few
   int few_index[64];
-  uint32_t few;
   uint32_t wave_n[kWaves];
   double wave_m[kWaves];
   float wave_top[kWaves];
   int wave_bad[kWaves];
   uint32_t wave_in[kWaves];
-  int found, last;
   uint32_t lo, hi;
-  uint32_t n, eq;
-  double m;
+  Spot spot;
   int token;
   uint32_t slab[64];
   Place place;
@@ -139,15 +177,8 @@ __device__ __forceinline__ void scan(Bins& b, double unit, Shared& s) {
     n[j] = b.n[2 * t + j];
     m[j] = (double)b.mass[2 * t + j] * (COARSE ? Weigh::unit(2 * t + j) : unit);
   }
-  uint32_t sn = n[0] + n[1];
-  double sm = m[0] + m[1];
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) {
-    const uint32_t on = __shfl_up(sn, k);
-    const double om = __shfl_up(sm, k);
-    sn += lane >= k ? on : 0;
-    sm += lane >= k ? om : 0.0;
-  }
+  const uint32_t sn = wave_scan(n[0] + n[1]);
+  const double sm = wave_scan(m[0] + m[1]);
   if (lane == 63) {
     s.wave_n[wid] = sn;
     s.wave_m[wid] = sm;
@@ -172,69 +203,62 @@ struct Bound {
   uint32_t rank;
   double mass;
 };
-// the bin in which the bound falls, with what lies before it (added to n, m)
-__device__ __forceinline__ int choose(const Bins& b, const Bound& q, uint32_t& n, double& m, Shared& s) {
-  if (threadIdx.x == 0) {
-    s.found = kBins;
-    s.last = -1;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int i = 2 * threadIdx.x + j;
-    if (b.n[i] == 0) continue;
-    const double upto = m + b.m_upto[i];
-    const bool past = q.by_rank ? n + b.n_upto[i] > q.rank : q.reach ? upto >= q.mass : upto > q.mass;
-    if (past) atomicMin(&s.found, i);
-    else atomicMax(&s.last, i);
-  }
-  __syncthreads();
-  const int i = s.found < kBins ? s.found : s.last;   // by rounding alone: the last that holds anything
-  const uint32_t before = b.n_upto[i] - b.n[i];
-  const double mass_before = before == 0 ? 0.0 : b.m_upto[max(i - 1, 0)];
-  n += before;
-  m += mass_before;
-  __syncthreads();
-  return i;
+// By the first wave: the first of its lanes in whose running sums the bound is passed (by rounding alone, the last that
+// holds anything).
+__device__ __forceinline__ int first_of(const Bound& q, uint32_t n, double m, uint32_t before, bool in) {
+  const bool some = in && n > before;
+  const bool past = q.by_rank ? n > q.rank : q.reach ? m >= q.mass : m > q.mass;
+  const unsigned long long hits = __ballot(some && past), any = __ballot(some);
+  return hits ? __builtin_ctzll(hits) : any ? 63 - __builtin_clzll(any) : 0;
+}
+
+// by the first wave: of 32 times 64 bins, whose sums follow n0 tokens of mass m0
+__device__ __forceinline__ Spot locate(const Bins& b, const Bound& q, uint32_t n0, double m0) {
+  const int lane = threadIdx.x & 63, g = (lane & 31) * 64;
+  const int group = first_of(q, n0 + b.n_upto[g + 63], m0 + b.m_upto[g + 63], n0 + (g ? b.n_upto[g - 1] : 0), lane < 32);
+  const int i = group * 64 + lane;
+  const int bin = group * 64 + first_of(q, n0 + b.n_upto[i], m0 + b.m_upto[i], n0 + b.n_upto[i] - b.n[i], true);
+  const uint32_t before = b.n_upto[bin] - b.n[bin];
+  return Spot{bin, n0 + before, b.n[bin], before == 0 ? m0 : m0 + b.m_upto[bin - 1]};
 }
 
 template <class E>
-__device__ Place find(const typename E::t* row, int V, const Weigh& w, uint32_t top, const Bound& q, Shared& s) {
-  uint32_t n = 0;
-  double m = 0.0;
-  const int b = choose(s.all, q, n, m, s);
-  const double unit = Weigh::unit(b);
-  uint32_t count = s.all.n[b];
-  // The bin's logits are an interval: the first two waves find its ends, 64 steps at once. The bin falls as the key rises.
-  {
-    const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    if (wid < 2) {
-      // wave 0: the largest key of a bin >= b; wave 1: the smallest key of a bin <= b
-      uint32_t lo = key_of(-3.402823466e38f), hi = top;   // bin(hi) = 0
-      if (wid == 0) {
-        while (lo < hi) {   // bin(lo) >= b, the answer in lo .. hi
-          const uint32_t step = (hi - lo) / 64 + 1;
-          const uint32_t k = lo + (uint32_t)(lane + 1) * step;
-          const bool ok = k <= hi && k > lo && w.bin(value_of(k)) >= b;
-          const int c = __popcll(__ballot(ok));   // the first c hold
-          lo += c * step;
-          hi = c == 64 ? hi : min(hi, lo + step - 1);
-        }
-        if (lane == 0) s.hi = lo;
-      } else {
-        while (lo < hi) {   // bin(hi) <= b
-          const uint32_t step = (hi - lo) / 64 + 1;
-          const uint32_t k = hi - (uint32_t)(lane + 1) * step;
-          const bool ok = k >= lo && k < hi && w.bin(value_of(k)) <= b;
-          const int c = __popcll(__ballot(ok));
-          hi -= c * step;
-          lo = c == 64 ? lo : hi - lo >= step ? hi - step + 1 : lo;
-        }
-        if (lane == 0) s.lo = hi;
-      }
+__device__ __forceinline__ Place find(const typename E::t* row, int V, const Weigh& w, uint32_t top, const Bound& q, Shared& s) {
+  const int lane = threadIdx.x & 63;
+  if (threadIdx.x < 64) {
+    const Spot p = locate(s.all, q, 0, 0.0);
+    const int b = p.bin;
+    // The bin's logits are an interval; its ends, 64 steps at once. The bin falls as the key rises: the largest key of a
+    // bin >= b, then the smallest of a bin <= b.
+    uint32_t lo = key_of(-3.402823466e38f), hi = top;
+    while (lo < hi) {   // bin(lo) >= b, the answer in lo .. hi
+      const uint32_t step = (hi - lo) / 64 + 1;
+      const uint32_t k = lo + (uint32_t)(lane + 1) * step;
+      const int c = __popcll(__ballot(k <= hi && k > lo && w.bin(value_of(k)) >= b));   // the first c hold
+      lo += c * step;
+      hi = min(hi, lo + step - 1);
     }
-    __syncthreads();
+    const uint32_t last = lo;
+    lo = key_of(-3.402823466e38f);
+    hi = last;
+    while (lo < hi) {   // bin(hi) <= b
+      const uint32_t step = (hi - lo) / 64 + 1;
+      const uint32_t k = hi - (uint32_t)(lane + 1) * step;
+      const int c = __popcll(__ballot(k >= lo && k < hi && w.bin(value_of(k)) <= b));
+      hi -= c * step;
+      lo = hi - lo >= step ? hi - step + 1 : lo;
+    }
+    if (lane == 0) {
+      s.spot = p;
+      s.lo = hi;
+      s.hi = last;
+    }
   }
+  __syncthreads();
+  const int b = s.spot.bin;
+  uint32_t n = s.spot.n, count = s.spot.count;
+  double m = s.spot.m;
+  const double unit = Weigh::unit(b);
   uint32_t lo = max(s.lo, s.from), hi = s.hi;
   // a list of the bin's tokens, and of all before them where they fit as well (the next bound falls there)
   bool listed = s.list_lo <= lo && hi <= s.list_hi;
@@ -260,32 +284,31 @@ __device__ Place find(const typename E::t* row, int V, const Weigh& w, uint32_t 
     listed = true;
   }
   __syncthreads();
-  if (listed && count <= 64) {   // a lane a token: each sees how many, and what mass, come before it
-    if (threadIdx.x == 0) s.few = 0;
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < s.listed; i += kThreads) {
-      const uint32_t k = s.list_key[i];
-      if (k >= lo && k <= hi) {
-        const uint32_t at = atomicAdd(&s.few, 1u);
-        if (at < 64) {
-          s.few_key[at] = k;
-          s.few_index[at] = s.list_index[i];
-        }
-      }
-    }
-    __syncthreads();
+  if (listed && count <= 64) {   // by the first wave, a lane a token: each sees how many, and what mass, come before it
     if (threadIdx.x < 64) {
-      const int lane = threadIdx.x;
+      uint32_t found = 0;
+      for (uint32_t i0 = 0; i0 < s.listed; i0 += 64) {
+        const uint32_t k = i0 + lane < s.listed ? s.list_key[i0 + lane] : 0;
+        const bool mine = k >= lo && k <= hi;   // (lo > 0)
+        const unsigned long long all = __ballot(mine);
+        const uint32_t at = found + __popcll(all & ((1ull << lane) - 1ull));
+        if (mine && at < 64) {
+          s.few_key[at] = k;
+          s.few_index[at] = s.list_index[i0 + lane];
+        }
+        found += __popcll(all);
+      }
+      __builtin_amdgcn_wave_barrier();
       const bool in = lane < (int)count;
       const uint32_t key = in ? s.few_key[lane] : 0;
       const int index = in ? s.few_index[lane] : 0;
-      const double e = in ? (double)Weigh::mass(w.bins_below(value_of(key)), b) * unit : 0.0;
+      const double e = in ? (double)w.mass(value_of(key), (float)b) * unit : 0.0;
       uint32_t above = 0, equal = 0, at = 0;
       double mass = m;   // of what is above
       for (int j = 0; j < (int)count; ++j) {
-        const uint32_t kj = __shfl(key, j);
-        const int ij = __shfl(index, j);
-        const double ej = __shfl(e, j);
+        const uint32_t kj = __builtin_amdgcn_readlane(key, j);
+        const int ij = __builtin_amdgcn_readlane(index, j);
+        const double ej = lane_of(e, j);
         above += kj > key;
         mass += kj > key ? ej : 0.0;
         equal += kj == key;
@@ -313,7 +336,7 @@ __device__ Place find(const typename E::t* row, int V, const Weigh& w, uint32_t 
       if (k >= lo && k <= hi) {
         const int i = (int)((hi - k) >> shift);
         atomicAdd(&s.part.n[i], 1u);
-        atomicAdd(&s.part.mass[i], Weigh::mass(w.bins_below(value_of(k)), b));
+        atomicAdd(&s.part.mass[i], w.mass(value_of(k), (float)b));
       }
     };
     if (listed) {
@@ -323,8 +346,15 @@ __device__ Place find(const typename E::t* row, int V, const Weigh& w, uint32_t 
     }
     __syncthreads();
     scan<false>(s.part, unit, s);
-    const uint32_t i = (uint32_t)choose(s.part, q, n, m, s);
-    count = s.part.n[i];
+    if (threadIdx.x < 64) {
+      const Spot p = locate(s.part, q, n, m);
+      if (lane == 0) s.spot = p;
+    }
+    __syncthreads();
+    const uint32_t i = s.spot.bin;
+    n = s.spot.n;
+    m = s.spot.m;
+    count = s.spot.count;
     hi -= i << shift;
     const uint32_t width = (1u << shift) - 1;
     lo = hi - lo > width ? hi - width : lo;
@@ -336,8 +366,7 @@ __device__ Place find(const typename E::t* row, int V, const Weigh& w, uint32_t 
   p.eq = count;
   p.index = -1;
   p.m = m;
-  const float z = value_of(hi);
-  p.w = (double)Weigh::mass(w.bins_below(z), b) * unit;
+  p.w = (double)w.mass(value_of(hi), (float)b) * unit;
   if (q.by_rank) {
     p.at = min(q.rank - n, count - 1);
   } else {
@@ -439,14 +468,14 @@ __device__ __noinline__ void sample_row(const SampleCall a, int n, Shared& s) {
     s.wave_bad[wid] = any_bad;
     s.wave_in[wid] = bound;
   }
-  clear(s.all);
+  for (uint32_t i = t; i < sizeof(s.copies) / 16; i += kThreads) reinterpret_cast<u32x4*>(s.copies)[i] = u32x4{0u, 0u, 0u, 0u};
   __syncthreads();
   for (int w = 0; w < kWaves; ++w) {
     top = fmaxf(top, s.wave_top[w]);
     bad |= s.wave_bad[w] != 0;
   }
   const float sc = scale == 0.f ? 1.f : scale;
-  if (bad || !(fabsf(top) < INFINITY) || !(sc > 0.f && sc < INFINITY)) {
+  if (bad || !(fabsf(top) < INFINITY) || !(sc > 0.f && sc <= kSampleMaxScale)) {
     if (t == 0) {
       a.token[n] = -1;
       if (a.prob) a.prob[n] = NAN;
@@ -459,11 +488,11 @@ __device__ __noinline__ void sample_row(const SampleCall a, int n, Shared& s) {
   const Weigh w(top, sc);
   const uint32_t key_top = key_of(top);
   const bool least = min_p > 0.f;
-  const double limit = least ? -log(fmin((double)min_p, 1.0)) * kPerNat : 0.0;
+  const double limit = least ? -log(fmin((double)min_p, 1.0)) : 0.0;   // nats below the maximum
   // What cannot be kept is not counted: what min_p alone leaves out (`limit` and a little more), and of a short list what
   // is below the worst of the waves' bounds.
   uint32_t from = key_of(-3.402823466e38f);
-  if (least && top_k <= 0 && !(top_p < 1.f)) from = max(from, key_of((float)((double)top - (limit + 1.0) / w.k)));
+  if (least && top_k <= 0 && !(top_p < 1.f)) from = max(from, key_of((float)((double)top - (limit + 0.03) / w.scale)));
   if (few) {
     bound = ~0u;
     for (int v = 0; v < kWaves; ++v) bound = min(bound, s.wave_in[v]);
@@ -476,26 +505,24 @@ __device__ __noinline__ void sample_row(const SampleCall a, int n, Shared& s) {
   }
   __syncthreads();
   uint32_t inside = 0, finite = 0;
+  Counts& counts = s.copies[lane & 3];
   each<E>(row, V, [&](float z, int i) {
-    finite += z > -INFINITY;
-    const uint32_t key = key_of(z);
-    if (key >= from) {
-      const double d = w.bins_below(z);
-      const int b = d < (double)kFar ? (int)d : kFar;
-      atomicAdd(&s.all.n[b], 1u);
-      if (b != kFar) atomicAdd(&s.all.mass[b], Weigh::mass(d, b));
-      inside += d <= limit;
+    const bool some = z > -INFINITY;
+    finite += __popcll(__ballot(some));   // of the wave
+    if (some && (!list || key_of(z) >= from)) {
+      const float b = w.bin_of(z);
+      atomicAdd(&counts.n[(int)b], 1u);
+      atomicAdd(&counts.mass[(int)b], w.mass(z, b));   // (of the last bin anything: it is worth nothing)
+      if (least) inside += w.below(z) <= limit;
       if (list) {
         const uint32_t at = atomicAdd(&s.listed, 1u);
         if (at < kListed) {
-          s.list_key[at] = key;
+          s.list_key[at] = key_of(z);
           s.list_index[at] = i;
         }
       }
     }
   });
-#pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) finite += __shfl_xor(finite, k);
   if (lane == 0) s.wave_n[wid] = finite;
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) inside += __shfl_xor(inside, k);
@@ -511,34 +538,47 @@ __device__ __noinline__ void sample_row(const SampleCall a, int n, Shared& s) {
     s.list_lo = list && s.listed <= kListed ? from : 1;
     s.list_hi = list && s.listed <= kListed ? key_top : 0;
   }
+  for (int i = t; i < kBins; i += kThreads) {
+    uint32_t c = 0;
+    unsigned long long m = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      c += s.copies[k].n[i];
+      m += s.copies[k].mass[i];
+    }
+    s.copies[0].n[i] = c;   // those of `all`
+    s.copies[0].mass[i] = m;
+  }
   __syncthreads();
   scan<true>(s.all, 0.0, s);
 
   double mass = s.all.m_upto[kBins - 1];
   Place cut{};
   bool is_cut = false;
-  if (top_k > 0 && (uint32_t)top_k < kept) {
-    cut = find<E>(row, V, w, key_top, Bound{true, false, (uint32_t)top_k - 1, 0.0}, s);
-    is_cut = true;
-    kept = top_k;
-    mass = cut.upto();
-  }
-  if (top_p < 1.f) {
-    const Place p = find<E>(row, V, w, key_top, Bound{false, true, 0, fmax((double)top_p, 0.0) * mass}, s);
-    if (p.rank() + 1 < kept) {
+  // top_k, top_p, min_p, the draw
+  Place p{};
+  for (int step = 0; step < 4; ++step) {
+    Bound q{};
+    if (step == 0) {
+      if (top_k <= 0 || (uint32_t)top_k >= kept) continue;
+      q = Bound{true, false, (uint32_t)top_k - 1, 0.0};
+    } else if (step == 1) {
+      if (!(top_p < 1.f)) continue;
+      q = Bound{false, true, 0, fmax((double)top_p, 0.0) * mass};
+    } else if (step == 2) {
+      if (!least || inside >= kept) continue;
+      q = Bound{true, false, inside - 1, 0.0};
+    } else {
+      q = Bound{false, false, 0, (double)a.r[n] * mass};
+    }
+    p = find<E>(row, V, w, key_top, q, s);
+    if (step < 3 && p.rank() + 1 < kept) {
       cut = p;
       is_cut = true;
       kept = p.rank() + 1;
       mass = p.upto();
     }
   }
-  if (least && inside < kept) {
-    cut = find<E>(row, V, w, key_top, Bound{true, false, inside - 1, 0.0}, s);
-    is_cut = true;
-    kept = inside;
-    mass = cut.upto();
-  }
-  Place p = find<E>(row, V, w, key_top, Bound{false, false, 0, (double)a.r[n] * mass}, s);
   if (is_cut && p.rank() > cut.rank()) p = cut;   // by rounding alone
   const int token = index_of<E>(row, V, p, s);
   if (t == 0) {
@@ -643,31 +683,6 @@ __device__ __forceinline__ uint32_t count_of(const Keys& s, uint32_t slot) {
   return slot & 0x8000 ? w >> 16 : w & 0xffff;
 }
 
-// inclusive sums over a wave's lanes, by moves between neighbouring registers' lanes (a shuffle through LDS takes ten
-// times as long, and these stand in a chain)
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t lanes_below(uint32_t v) {   // of the lane that CTRL names, 0 where there is none
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
-}
-template <int CTRL, int ROWS>
-__device__ __forceinline__ double lanes_below(double v) {
-  return __hiloint2double((int)lanes_below<CTRL, ROWS>((uint32_t)__double2hiint(v)),
-                          (int)lanes_below<CTRL, ROWS>((uint32_t)__double2loint(v)));
-}
-template <class T>
-__device__ __forceinline__ T wave_scan(T v) {
-  v += lanes_below<0x111, 0xf>(v);   // 1, 2, 4, 8 lanes below in a row of 16
-  v += lanes_below<0x112, 0xf>(v);
-  v += lanes_below<0x114, 0xf>(v);
-  v += lanes_below<0x118, 0xf>(v);
-  v += lanes_below<0x142, 0xa>(v);   // the last lane of the row below, into rows 1 and 3
-  v += lanes_below<0x143, 0xc>(v);   // lane 31, into rows 2 and 3
-  return v;
-}
-__device__ __forceinline__ double lane_of(double v, int at) {
-  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), at), __builtin_amdgcn_readlane(__double2loint(v), at));
-}
-
 // By the first wave: the token at which a bound is passed.
 template <class E>
 __device__ __forceinline__ KeyPlace find_key(const Keys& s, const Weigh& w, const KeyBound& q) {
@@ -687,7 +702,7 @@ __device__ __forceinline__ KeyPlace find_key(const Keys& s, const Weigh& w, cons
   const uint32_t n0 = b ? s.n_upto[b - 1] : 0;
   const double m0 = b ? s.m_upto[b - 1] : 0.0;
   const uint32_t slot = b * 64 + lane, c = count_of(s, slot);
-  const double e = c ? exp(w.bins_below(slot_value<E>(slot)) * (-1.0 / kPerNat)) : 0.0;
+  const double e = c ? exp(-w.below(slot_value<E>(slot))) : 0.0;
   const uint32_t n = n0 + wave_scan(c);
   const double m = m0 + wave_scan((double)c * e);
   const int at = first_of(n, m, n - c, true);
@@ -806,19 +821,19 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
   last = __builtin_amdgcn_readfirstlane(last);
   const float top = slot_value<E>(first), sc = scale == 0.f ? 1.f : scale;
   // NaN (on either side) or +inf in the row, nothing but -inf, or no temperature
-  if (last > kLow || first >= kLow || !(fabsf(top) < INFINITY) || !(sc > 0.f && sc < INFINITY)) {
+  if (last > kLow || first >= kLow || !(fabsf(top) < INFINITY) || !(sc > 0.f && sc <= kSampleMaxScale)) {
     __syncthreads();
     sample_row<E>(a, n, *reinterpret_cast<Shared*>(lds));
     return;
   }
   const Weigh w(top, sc);
   const bool least = min_p > 0.f;
-  const double limit = least ? -log(fmin((double)min_p, 1.0)) * kPerNat : 0.0;
+  const double limit = least ? -log(fmin((double)min_p, 1.0)) : 0.0;   // nats below the maximum
   // Slots beyond `end` are not counted: 64 nats below; of min_p alone, what it leaves out (`limit` and a little more); of
   // a short list, what no token of it can be.
   const bool min_alone = least && top_k <= 0 && !(top_p < 1.f);
-  const double reach_bins = min_alone ? fmin(limit + 1.0, 64.0 * kPerNat) : 64.0 * kPerNat;
-  uint32_t end = min(slot_of<E>((float)((double)top - reach_bins / ((double)sc * kPerNat))), kLow - 1);
+  const double reach = min_alone ? fmin(limit + 0.03, 64.0) : 64.0;
+  uint32_t end = min(slot_of<E>((float)((double)top - reach / (double)sc)), kLow - 1);
   if (few) end = min(end, bound);
   end = __builtin_amdgcn_readfirstlane(end == kZero ? kMinusZero : end);   // -0 is equal
   uint32_t infs = 0, seen = V;   // -inf, and what was counted
@@ -914,7 +929,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
     double bm = 0.0;
     if (any >> half & 0xffff) {
       const float z0 = slot_value<E>(at), u = z0 - slot_value<E>(at + 1);
-      const double per = -(double)u * w.k * (1.0 / kPerNat), d0 = w.bins_below(z0) * (-1.0 / kPerNat);
+      const double per = -(double)u * w.scale, d0 = -w.below(z0);
       if (d0 > 600.0) s.give_up = 1;   // so steep that the values above the maximum in its block overflow
       const double e0 = exp(d0), rho = exp(per), rho2 = rho * rho;
       double even = 0.0, odd = 0.0;
@@ -960,7 +975,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
   // A count that ran over its 16 bits shows in their sum. Those, and ranks among what is not counted, are rare and left
   // to the other way.
   const bool far = top_k > 0 && (uint32_t)top_k > counted && (uint32_t)top_k < finite;
-  const bool low = least && limit > 63.0 * kPerNat;
+  const bool low = least && limit > 63.0;
   if (seen != counted || s.give_up || far || low) {
     __syncthreads();
     sample_row<E>(a, n, *reinterpret_cast<Shared*>(lds));
@@ -989,7 +1004,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
     if (least) {
       // the blocks whose first value min_p leaves, then the values of the last of them
       auto leaves = [&](uint32_t slot) {
-        return w.bins_below(slot_value<E>(min(max(slot, first), kLow - 1))) <= limit;
+        return w.below(slot_value<E>(min(max(slot, first), kLow - 1))) <= limit;
       };
       const int group = __popcll(__ballot(lane < 16 && leaves(lane * 4096))) - 1;
       const int b = group * 64 + __popcll(__ballot(leaves(group * 4096 + lane * 64))) - 1;

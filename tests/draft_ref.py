@@ -91,7 +91,7 @@ def check_sample(z, r, scale, top_k, top_p, min_p, token, prob, kept, filtered=N
     scale, top_p, min_p = f32(scale), f32(top_p), f32(min_p)
     scale = 1.0 if scale == 0 else scale
     zz = z.double()
-    if bool(zz.isnan().any()) or not bool(zz.isfinite().any()) or bool((zz == math.inf).any()) or not 0 < scale < math.inf:
+    if bool(zz.isnan().any()) or not bool(zz.isfinite().any()) or bool((zz == math.inf).any()) or not 0 < scale <= 2.0 ** 100:
         assert token == -1 and kept == 0 and math.isnan(prob)
         if filtered is not None:
             assert bool((filtered == -math.inf).all())

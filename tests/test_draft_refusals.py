@@ -115,7 +115,7 @@ def _sample(**kw):
 @pytest.mark.parametrize("kw,status", [
     (dict(N=-1), 2), (dict(N=1 << 22), 2), (dict(V=0), 2), (dict(V=(1 << 20) + 1, ls=1 << 21), 2), (dict(dtype=4), 5),
     (dict(ls=999), 2), (dict(filtered=4 * P, fs=999), 2), (dict(scale=-1.0), 3), (dict(scale=math.nan), 3),
-    (dict(scale=math.inf), 3), (dict(k=-1), 3), (dict(p=0.0), 3), (dict(p=-0.5), 3), (dict(p=math.nan), 3),
+    (dict(scale=math.inf), 3), (dict(scale=1.3e30), 3), (dict(k=-1), 3), (dict(p=0.0), 3), (dict(p=-0.5), 3), (dict(p=math.nan), 3),
     (dict(least=-0.1), 3), (dict(least=1.1), 3), (dict(least=math.nan), 3), (dict(logits=None), 1), (dict(r=None), 1),
     (dict(token=None), 1), (dict(logits=P + 1), 5), (dict(dtype=rpd.DTYPE_F32, logits=P + 2), 5), (dict(r=P + 2), 5),
     (dict(token=P + 1), 5), (dict(prob=P + 2), 5), (dict(kept=P + 2), 5), (dict(scales=P + 2), 5), (dict(ks=P + 2), 5),

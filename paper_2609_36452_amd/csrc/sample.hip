@@ -139,24 +139,27 @@ struct Shared {
   Place place;
 };
 
-// eight entries at a time of the row, f(value, index), -inf left out by the caller
+// f(value, index) of the row's entries, eight at a time and at last one
 template <class E, class F>
 __device__ __forceinline__ void each(const typename E::t* row, int V, F f) {
   constexpr int kFlight = 4;
-  for (int i0 = 8 * threadIdx.x; i0 < V; i0 += kFlight * 8 * kThreads) {
+  const int whole = V & ~7;
+  for (int i0 = 8 * threadIdx.x; i0 < whole; i0 += kFlight * 8 * kThreads) {
     Eight<E> v[kFlight];
 #pragma unroll
     for (int u = 0; u < kFlight; ++u)
-      if (i0 + u * 8 * kThreads < V) load_eight<E>(row, i0 + u * 8 * kThreads, V, v[u]);
+      if (i0 + u * 8 * kThreads < whole) v[u].load(row + i0 + u * 8 * kThreads);
 #pragma unroll
     for (int u = 0; u < kFlight; ++u) {
       const int i = i0 + u * 8 * kThreads;
-      if (i < V) {
+      if (i < whole) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f(v[u].at(e) + 0.f, i + e);   // (past the end: -inf)
+        for (int e = 0; e < 8; ++e) f(v[u].at(e) + 0.f, i + e);
       }
     }
   }
+  const int i = whole + threadIdx.x;
+  if (i < V) f(E::one(row + i) + 0.f, i);
 }
 
 __device__ __forceinline__ void clear(Bins& b) {
@@ -594,7 +597,6 @@ __device__ __noinline__ void sample_row(const SampleCall a, int n, Shared& s) {
     if (cut.at + 1 < cut.eq) last = index_of<E>(row, V, cut, s);
   }
   each<E>(row, V, [&](float z, int i) {
-    if (i >= V) return;
     const uint32_t k = key_of(z);
     out[i] = k > key || (k == key && i <= last) ? row[i] : E::to(-INFINITY);
   });

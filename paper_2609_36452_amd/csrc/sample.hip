@@ -139,9 +139,9 @@ struct Shared {
   Place place;
 };
 
-// f(value, index) of the row's entries, eight at a time and at last one
+// f(values, their number, index) of the row's entries: eight at a time, and at last one
 template <class E, class F>
-__device__ __forceinline__ void each(const typename E::t* row, int V, F f) {
+__device__ __forceinline__ void each_eight(const typename E::t* row, int V, F f) {
   constexpr int kFlight = 4;
   const int whole = V & ~7;
   for (int i0 = 8 * threadIdx.x; i0 < whole; i0 += kFlight * 8 * kThreads) {
@@ -153,13 +153,40 @@ __device__ __forceinline__ void each(const typename E::t* row, int V, F f) {
     for (int u = 0; u < kFlight; ++u) {
       const int i = i0 + u * 8 * kThreads;
       if (i < whole) {
+        float z[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f(v[u].at(e) + 0.f, i + e);
+        for (int e = 0; e < 8; ++e) z[e] = v[u].at(e);
+        f(z, i);
       }
     }
   }
   const int i = whole + threadIdx.x;
-  if (i < V) f(E::one(row + i) + 0.f, i);
+  if (i < V) {
+    const float z[1] = {E::one(row + i)};
+    f(z, i);
+  }
+}
+// f(value, index), a negative zero made positive
+template <class E, class F>
+__device__ __forceinline__ void each(const typename E::t* row, int V, F f) {
+  each_eight<E>(row, V, [&](auto& z, int i) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < (int)(sizeof(z) / sizeof(float)); ++e) f(z[e] + 0.f, i + e);
+  });
+}
+// the largest of some values (NaN if there is one), three at a time
+template <int N>
+__device__ __forceinline__ float largest(float top, const float (&z)[N]) {
+#pragma unroll
+  for (int e = 0; e + 1 < N; e += 2) top = __builtin_elementwise_maximum(top, __builtin_elementwise_maximum(z[e], z[e + 1]));
+  return N == 1 ? __builtin_elementwise_maximum(top, z[0]) : top;
+}
+template <int N>
+__device__ __forceinline__ float smallest(const float (&z)[N]) {
+  float low = z[0];
+#pragma unroll
+  for (int e = 1; e < N; ++e) low = __builtin_elementwise_minimum(low, z[e]);
+  return low;
 }
 
 __device__ __forceinline__ void clear(Bins& b) {
@@ -438,11 +465,9 @@ __device__ __noinline__ void sample_row(const SampleCall a, int n, Shared& s) {
 
   // the maximum; NaN, and +inf, leave no distribution
   float top = -INFINITY;
-  bool bad = false;
-  each<E>(row, V, [&](float z, int) {
-    top = fmaxf(top, z);
-    bad |= z != z;
-  });
+  each_eight<E>(row, V, [&](auto& z, int) __attribute__((always_inline)) { top = largest(top, z); });
+  bool bad = top != top;
+  top += 0.f;   // (of zeros the positive one)
   // Of a short list (top_k): a sixteenth of it, the j-th largest of the lanes' own best, bit by bit: of the lanes that
   // agree with it so far, those with a 1 come first. The worst of the waves' is a bound for the whole list.
   uint32_t bound = 0;
@@ -464,7 +489,7 @@ __device__ __noinline__ void sample_row(const SampleCall a, int n, Shared& s) {
     }
   }
 #pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
+  for (int k = 32; k >= 1; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));   // (NaN is in `bad`)
   const bool any_bad = __any(bad);
   if (lane == 0) {
     s.wave_top[wid] = top;
@@ -507,36 +532,51 @@ __device__ __noinline__ void sample_row(const SampleCall a, int n, Shared& s) {
     s.from = from;
   }
   __syncthreads();
-  uint32_t inside = 0, finite = 0;
+  uint32_t inside = 0, infs = 0;
   Counts& counts = s.copies[lane & 3];
-  each<E>(row, V, [&](float z, int i) {
-    const bool some = z > -INFINITY;
-    finite += __popcll(__ballot(some));   // of the wave
-    if (some && (!list || key_of(z) >= from)) {
-      const float b = w.bin_of(z);
-      atomicAdd(&counts.n[(int)b], 1u);
-      atomicAdd(&counts.mass[(int)b], w.mass(z, b));   // (of the last bin anything: it is worth nothing)
-      if (least) inside += w.below(z) <= limit;
-      if (list) {
+  const float above = value_of(from);
+  auto add = [&](float z) __attribute__((always_inline)) {
+    const float b = w.bin_of(z);
+    atomicAdd(&counts.n[(int)b], 1u);   // (-inf in the last bin, subtracted below)
+    atomicAdd(&counts.mass[(int)b], w.mass(z, b));   // (of the last bin anything: it is worth nothing)
+    if (least) inside += w.below(z) <= limit;
+  };
+  each_eight<E>(row, V, [&](auto& z, int i) __attribute__((always_inline)) {
+    constexpr int N = sizeof(z) / sizeof(float);
+    if (smallest(z) == -INFINITY) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) infs += z[e] == -INFINITY;
+    }
+    if (!list) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) add(z[e]);
+    } else if (largest(z[0], z) >= above) {
+#pragma unroll 1
+      for (int e = 0; e < N; ++e) {
+        const float y = E::one(row + i + e) + 0.f;   // (read again: they are few)
+        if (!(y >= above)) continue;
+        add(y);
         const uint32_t at = atomicAdd(&s.listed, 1u);
         if (at < kListed) {
-          s.list_key[at] = key_of(z);
-          s.list_index[at] = i;
+          s.list_key[at] = key_of(y);
+          s.list_index[at] = i + e;
         }
       }
     }
   });
-  if (lane == 0) s.wave_n[wid] = finite;
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) infs += __shfl_xor(infs, k);
+  if (lane == 0) s.wave_n[wid] = infs;
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) inside += __shfl_xor(inside, k);
   if (lane == 0) s.wave_in[wid] = inside;
   __syncthreads();
-  inside = 0;
-  uint32_t kept = 0;
+  inside = infs = 0;
   for (int v = 0; v < kWaves; ++v) {
     inside += s.wave_in[v];
-    kept += s.wave_n[v];
+    infs += s.wave_n[v];
   }
+  uint32_t kept = V - infs;
   if (t == 0) {
     s.list_lo = list && s.listed <= kListed ? from : 1;
     s.list_hi = list && s.listed <= kListed ? key_top : 0;
@@ -549,7 +589,7 @@ __device__ __noinline__ void sample_row(const SampleCall a, int n, Shared& s) {
       c += s.copies[k].n[i];
       m += s.copies[k].mass[i];
     }
-    s.copies[0].n[i] = c;   // those of `all`
+    s.copies[0].n[i] = i == kFar && !list ? c - infs : c;   // those of `all`
     s.copies[0].mass[i] = m;
   }
   __syncthreads();

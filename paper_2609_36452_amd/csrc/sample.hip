@@ -260,7 +260,11 @@ __device__ __forceinline__ Place find(const typename E::t* row, int V, const Wei
     const int b = p.bin;
     // The bin's logits are an interval; its ends, 64 steps at once. The bin falls as the key rises: the largest key of a
     // bin >= b, then the smallest of a bin <= b.
-    uint32_t lo = key_of(-3.402823466e38f), hi = top;
+    // It lies within 0.6 of its middle's place, a step of the floats around.
+    const uint32_t least = key_of(-3.402823466e38f);
+    const float far = w.top - ((float)b + 0.6f) / w.k, near = w.top - ((float)b - 0.6f) / w.k;
+    const uint32_t from = b == kFar || !(far > -3.0e38f) ? least : key_of(far) - 2;
+    uint32_t lo = from, hi = b == 0 || !(near < w.top) ? top : min(top, key_of(near) + 2);
     while (lo < hi) {   // bin(lo) >= b, the answer in lo .. hi
       const uint32_t step = (hi - lo) / 64 + 1;
       const uint32_t k = lo + (uint32_t)(lane + 1) * step;
@@ -269,7 +273,7 @@ __device__ __forceinline__ Place find(const typename E::t* row, int V, const Wei
       hi = min(hi, lo + step - 1);
     }
     const uint32_t last = lo;
-    lo = key_of(-3.402823466e38f);
+    lo = from;
     hi = last;
     while (lo < hi) {   // bin(hi) <= b
       const uint32_t step = (hi - lo) / 64 + 1;
@@ -455,7 +459,7 @@ __device__ int index_of(const typename E::t* row, int V, const Place& p, Shared&
 
 // a row of any type and length, read from memory in each pass
 template <class E>
-__device__ __noinline__ void sample_row(const SampleCall a, int n, Shared& s) {
+__device__ __forceinline__ void sample_row(const SampleCall& a, int n, Shared& s) {
   const int t = threadIdx.x, lane = t & 63, wid = t >> 6, V = a.V;
   const typename E::t* row = static_cast<const typename E::t*>(a.logits) + n * a.stride;
   typename E::t* out = a.filtered ? static_cast<typename E::t*>(a.filtered) + n * a.filtered_stride : nullptr;
@@ -642,6 +646,11 @@ __device__ __noinline__ void sample_row(const SampleCall a, int n, Shared& s) {
   });
 }
 
+// the same where it is rare
+template <class E>
+__device__ __noinline__ void sample_row_apart(const SampleCall a, int n, Shared& s) {
+  sample_row<E>(a, n, s);
+}
 template <class E>
 __global__ __launch_bounds__(kThreads) void k_sample(SampleCall a) {
   __shared__ Shared s;
@@ -865,7 +874,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
   // NaN (on either side) or +inf in the row, nothing but -inf, or no temperature
   if (last > kLow || first >= kLow || !(fabsf(top) < INFINITY) || !(sc > 0.f && sc <= kSampleMaxScale)) {
     __syncthreads();
-    sample_row<E>(a, n, *reinterpret_cast<Shared*>(lds));
+    sample_row_apart<E>(a, n, *reinterpret_cast<Shared*>(lds));
     return;
   }
   const Weigh w(top, sc);
@@ -1020,7 +1029,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
   const bool low = least && limit > 63.0;
   if (seen != counted || s.give_up || far || low) {
     __syncthreads();
-    sample_row<E>(a, n, *reinterpret_cast<Shared*>(lds));
+    sample_row_apart<E>(a, n, *reinterpret_cast<Shared*>(lds));
     return;
   }
   if (wid == 0) {

@@ -581,7 +581,7 @@ rpd_status rpd_fp8_quantize(int32_t rows, int32_t d, int32_t dtype, const void* 
  * An output head in e4m3 with a scale for each block of 128 x 128 (of any
  * float32 value):
  *   W[v][k] = scales[v / 128][k / 128] * code[v][k]
- *   V, d       1 <= V, d <= 2^20, V * d <= 2^36
+ *   V, d       1 <= V, d <= 2^20, V * d <= 2^35
  *   codes      device [V][d] bytes, contiguous
  *   scales     device [ceil(V / 128)][ceil(d / 128)] float32
  *   transpose  0: packs W; 1: packs its transpose, a head of d rows and V
@@ -604,12 +604,12 @@ size_t rpd_fp8_workspace_size(int32_t V, int32_t d, int32_t M, int32_t statistic
  * and scales stand for, logits y = W x^, or the softmax statistics of
  * logit_scale * y as rpd_gate_commit takes them (of a head of 131072 rows and
  * more, or of many x, the logits then never reach memory). Codes and x^ are exact operands (magnitudes below 2^-126 may count
- * as 0), sums are float32. Equal rows of the head give equal logits; of equal
+ * as 0, and what rounds to 2^128 is infinite), sums are float32. Equal rows of the head give equal logits; of equal
  * logits the lowest index is the argmax.
  *   M          0 <= M <= 2^20 (0: nothing is done)
  *   x          device [M][d] of type x_dtype (bf16, fp16 or fp32), rows x_stride >= d apart
  *   logits     device [M][V] of type logits_dtype (any of the three), rows
- *              logits_stride >= V apart; or NULL
+ *              logits_stride >= V apart, not over x; or NULL
  *   argmax, confidence, entropy, logit_scale   as rpd_quant_project's
  *   workspace  rpd_fp8_workspace_size bytes, 256-byte aligned (may be NULL where
  *              that is 0); its prior contents do not matter

@@ -8,10 +8,10 @@ using namespace rpd;
 
 namespace {
 
-bool head_ok(int V, int d) { return V >= 1 && V <= 1 << 20 && d >= 1 && d <= 1 << 20 && (long long)V * d <= 1LL << 36; }
+bool head_ok(int V, int d) { return V >= 1 && V <= 1 << 20 && d >= 1 && d <= 1 << 20 && (long long)V * d <= 1LL << 35; }
 
 rpd_status check_head(int V, int d) {
-  if (!head_ok(V, d)) return fail(RPD_ERR_BAD_SHAPE, "need 1<=V,d<=2^20, V*d<=2^36 (got V=%d d=%d)", V, d);
+  if (!head_ok(V, d)) return fail(RPD_ERR_BAD_SHAPE, "need 1<=V,d<=2^20, V*d<=2^35 (got V=%d d=%d)", V, d);
   return RPD_OK;
 }
 
@@ -92,13 +92,11 @@ rpd_status rpd_fp8_quantize(int32_t rows, int32_t d, int32_t dtype, const void* 
   if (misaligned(x, elem_align(dtype)) || misaligned(scales, 3))
     return fail(RPD_ERR_UNSUPPORTED, "a pointer is not aligned to its element");
   // what is written must not be what other workgroups still read
-  const uintptr_t xa = reinterpret_cast<uintptr_t>(x), ca = reinterpret_cast<uintptr_t>(codes),
-                  sa = reinterpret_cast<uintptr_t>(scales);
-  const unsigned long long xn = ((unsigned long long)(rows - 1) * x_stride + d) * (dtype == RPD_DTYPE_F32 ? 4 : 2),
-                           cn = (unsigned long long)(rows - 1) * codes_stride + d,
-                           sn = (unsigned long long)(block_rows == 1 ? rows : up_div(rows, kFp8Block)) * nb * 4;
-  auto meet = [](uintptr_t p, unsigned long long n, uintptr_t q, unsigned long long k) { return p < q + k && q < p + n; };
-  if (meet(xa, xn, ca, cn) || meet(xa, xn, sa, sn) || meet(ca, cn, sa, sn))
+  const long long xs = x_stride * size_of(dtype), xn = (long long)d * size_of(dtype), span_x = (rows - 1) * xs + xn,
+                  span_c = (rows - 1) * codes_stride + d,
+                  sn = (block_rows == 1 ? rows : up_div(rows, kFp8Block)) * nb * 4;
+  if (rows_meet(x, xs, xn, codes, codes_stride, d, rows) || rows_meet(x, 0, span_x, scales, 0, sn, 1) ||
+      rows_meet(codes, 0, span_c, scales, 0, sn, 1))
     return fail(RPD_ERR_BAD_PARAM, "x, codes and scales must not overlap");
   Fp8Quantize a{};
   a.rows = rows;
@@ -168,6 +166,9 @@ rpd_status rpd_fp8_project(int32_t V, int32_t d, const void* packed, int32_t M, 
   if (misaligned(x, elem_align(x_dtype)) || misaligned(logits, elem_align(logits_dtype)) || misaligned(argmax, 3) ||
       misaligned(confidence, 3) || misaligned(entropy, 3))
     return fail(RPD_ERR_UNSUPPORTED, "a pointer is not aligned to its element");
+  const int xb = size_of(x_dtype), ob = size_of(logits_dtype);
+  if (logits && rows_meet(x, x_stride * xb, (long long)d * xb, logits, logits_stride * ob, (long long)V * ob, M))
+    return fail(RPD_ERR_BAD_PARAM, "logits must not overlap x");   // workgroups read x while others write
   const Fp8Dims q = fp8_dims(V, d);
   const uint8_t* pk = static_cast<const uint8_t*>(packed);
   Fp8Call a{};

@@ -7,13 +7,6 @@ namespace {
 
 bool shape_ok(const rpd_sample* p) { return p->N >= 0 && p->N < 1 << 22 && p->V >= 1 && p->V <= 1 << 20; }
 
-// Whether a row of the filtered logits takes memory of a row of the logits (both aligned to their elements).
-bool over(const rpd_sample* p) {
-  const __int128 size = p->dtype == RPD_DTYPE_F32 ? 4 : 2, last = p->N - 1;
-  const __int128 a = reinterpret_cast<uintptr_t>(p->logits), b = reinterpret_cast<uintptr_t>(p->filtered);
-  return a < b + (last * p->filtered_stride + p->V) * size && b < a + (last * p->logits_stride + p->V) * size;
-}
-
 }  // namespace
 
 extern "C" {
@@ -40,7 +33,10 @@ rpd_status rpd_sample_tokens(const rpd_sample* p, void* workspace, size_t worksp
       misaligned(p->top_ks, 3) || misaligned(p->top_ps, 3) || misaligned(p->min_ps, 3) || misaligned(p->token, 3) ||
       misaligned(p->prob, 3) || misaligned(p->kept, 3))
     return fail(RPD_ERR_UNSUPPORTED, "a pointer is not aligned to its element");
-  if (p->filtered && over(p)) return fail(RPD_ERR_BAD_PARAM, "filtered must not overlap the logits");
+  const int size = size_of(p->dtype);
+  if (p->filtered && rows_meet(p->logits, p->logits_stride * size, (long long)p->V * size, p->filtered,
+                               p->filtered_stride * size, (long long)p->V * size, p->N))
+    return fail(RPD_ERR_BAD_PARAM, "filtered must not overlap the logits");
   SampleCall a{};
   a.N = p->N;
   a.V = p->V;

@@ -616,7 +616,7 @@ __device__ __forceinline__ void sample_row(const SampleCall& a, int n, Shared& s
       if (!least || inside >= kept) continue;
       q = Bound{true, false, inside - 1, 0.0};
     } else {
-      q = Bound{false, false, 0, (double)a.r[n] * mass};
+      q = Bound{false, false, 0, fmin(fmax((double)a.r[n], 0.0), 1.0) * mass};
     }
     p = find<E>(row, V, w, key_top, q, s);
     if (step < 3 && p.rank() + 1 < kept) {
@@ -1071,7 +1071,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
         mass = cut.upto();
       }
     }
-    KeyPlace p = find_key<E>(s, w, KeyBound{false, false, 0, (double)a.r[n] * mass});
+    KeyPlace p = find_key<E>(s, w, KeyBound{false, false, 0, fmin(fmax((double)a.r[n], 0.0), 1.0) * mass});
     if (is_cut && p.rank() > cut.rank()) p = cut;   // by rounding alone
     if (lane == 0) {
       s.pick = p;

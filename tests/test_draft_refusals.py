@@ -27,11 +27,21 @@ def test_quantize_refusals(kw, status):
     assert s == status and rpd.last_error()
 
 
+def test_rows_between_each_other_are_apart():
+    """Rows of one stride may lie between each other: such calls pass the check (and end at another one, before anything
+    is enqueued)."""
+    L = rpd.lib()
+    # a row of 40 of x, then 30 logits, in rows of 70 elements of 2 bytes; a workspace too small ends the call
+    project = lambda out, os: L.rpd_fp8_project(30, 40, P, 40, P, 70, 0, out, os, 0, None, None, None, 1.0, P, 16, None)   # noqa: E731
+    assert project(P + 80, 70) == 4 and project(P + 78, 70) == 3 and project(P - 60, 70) == 4
+    assert project(P + 80, 71) == 3 and project(P + 70 * 2 * 40, 71) == 4
+
+
 def test_quantize_nothing():
     assert rpd.lib().rpd_fp8_quantize(0, 200, 0, None, 200, 1, None, 200, None, None) == 0
 
 
-@pytest.mark.parametrize("V,d", [(0, 128), (128, 0), ((1 << 20) + 1, 8), (8, (1 << 20) + 1), (1 << 19, (1 << 17) + 1)])
+@pytest.mark.parametrize("V,d", [(0, 128), (128, 0), ((1 << 20) + 1, 8), (8, (1 << 20) + 1), (1 << 18, (1 << 17) + 1)])
 def test_head_refusals(V, d):
     L = rpd.lib()
     assert L.rpd_fp8_packed_size(V, d) == 0 and L.rpd_fp8_workspace_size(V, d, 4, 0) == 0
@@ -68,10 +78,11 @@ def test_pack_refusals(kw, status):
     (dict(M=-1), 2), (dict(M=(1 << 20) + 1), 2), (dict(xt=5), 5), (dict(xs=199), 2), (dict(os=999), 2), (dict(ot=7), 5),
     (dict(scale=-1.0), 3), (dict(scale=math.nan), 3), (dict(scale=math.inf), 3), (dict(packed=None), 1), (dict(x=None), 1),
     (dict(out=None), 1), (dict(am=P), 1), (dict(out=None, am=P, cf=P), 1), (dict(packed=P + 2), 5), (dict(x=P + 1), 5),
-    (dict(out=P + 1), 5), (dict(ot=rpd.DTYPE_F32, out=P + 2), 5), (dict(out=None, am=P + 2, cf=P, en=P), 5),
+    (dict(out=P + 1), 5), (dict(ot=rpd.DTYPE_F32, out=P + 2), 5), (dict(out=P), 3), (dict(out=P + 15998), 3),
+    (dict(out=P - 79998), 3), (dict(xt=rpd.DTYPE_F32, out=P + 31998), 3), (dict(out=None, am=P + 2, cf=P, en=P), 5),
     (dict(ws=None), 1), (dict(ws=P + 8), 5), (dict(nbytes=16), 4)])
 def test_project_refusals(kw, status):
-    a = dict(packed=P, M=40, x=P, xs=200, xt=rpd.DTYPE_BF16, out=P, os=1000, ot=rpd.DTYPE_BF16, am=None, cf=None, en=None,
+    a = dict(packed=P, M=40, x=P, xs=200, xt=rpd.DTYPE_BF16, out=2 * P, os=1000, ot=rpd.DTYPE_BF16, am=None, cf=None, en=None,
              scale=1.0, ws=P, nbytes=1 << 30)
     a.update(kw)
     s = rpd.lib().rpd_fp8_project(1000, 200, a["packed"], a["M"], a["x"], a["xs"], a["xt"], a["out"], a["os"], a["ot"],

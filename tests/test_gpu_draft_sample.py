@@ -124,13 +124,30 @@ def test_sample_masked_rows(dtype):
         assert o["token"][[4, 5, 6]].tolist() == [-1] * 3 and o["token"][[2, 7, 8]].tolist() == [4000, 5002, 4]
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("scale", [1e-30, 1e-6, 1e-2, 50.0, 1e6, 1e30])
-def test_sample_extreme_temperatures(scale):
-    z, r = _logits(6, 3001, F32, 10), _r(6, 11)
-    z[4] = torch.randn((3001,), generator=torch.Generator().manual_seed(3)) * 1e30
-    z[5, ::5] = torch.finfo(F32).min
-    for kw in (dict(), dict(top_k=100), dict(top_p=0.6), dict(min_p=0.3)):
+def test_sample_extreme_temperatures(scale, dtype):
+    z, r = _logits(6, 3001, dtype, 10), _r(6, 11)
+    wide = 1e30 if dtype != HF else 1e4
+    z[4] = (torch.randn((3001,), generator=torch.Generator().manual_seed(3)) * wide).to(dtype)
+    z[5, ::5] = torch.finfo(dtype).min
+    for kw in (dict(), dict(top_k=100), dict(top_p=0.6), dict(min_p=0.3), dict(min_p=1e-30, top_k=2900)):
         _check(z, r, scale=scale, **kw)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_sample_short_lists(dtype):
+    """Lists around the number of lanes and of threads, of rows whose best tokens one thread or one wave holds."""
+    V = 20003
+    g = torch.Generator().manual_seed(29)
+    z = torch.randn((5, V), generator=g)
+    z[1, 8:16] += 20.0                 # a thread's
+    z[2, :512] += 9.0                  # a wave's
+    z[3] = z[3].sort(descending=True)[0]
+    z[4] = -z[3].flip(0)
+    z = z.to(dtype)
+    for k in (1, 2, 15, 16, 17, 63, 64, 65, 511, 1023, 1024, 1025, 5000):
+        _check(z, _r(5, k), top_k=k, top_p=0.99)
 
 
 def test_sample_random_numbers_at_their_ends():

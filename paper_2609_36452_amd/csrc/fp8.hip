@@ -280,18 +280,18 @@ __global__ __launch_bounds__(256, 2) void k_fp8_tile(Fp8Dims q, Fp8Call a) {
   const int c0 = (int)((long long)q.nc * sp / a.splits), c1 = (int)((long long)q.nc * (sp + 1) / a.splits);
   const int mb0 = rt * NB, v0 = vt * kFp8TileRows + 64 * wid;
 
-  // both through buffer loads: the chunk's offset in a scalar register, no address registers. Reads past the resource's
-  // end (tiles past the head's, blocks past the rows') give zeros, which are not stored.
-  auto resource = [](const uint8_t* p, long long bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), (short)0, (int)min(max(bytes, 0ll), 0x7fffffffll),
-                                             0x00020000);
+  // both through buffer loads: the chunk's offset in a scalar register, no address registers. In place of tiles past the
+  // head's and blocks past the rows' the last one is read again; what comes of it is not stored.
+  auto resource = [](const uint8_t* p, long long bytes) {   // 2^28 at most: 8 blocks of 2^20 columns
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), (short)0, (int)bytes, 0x00020000);
   };
   const long long wrow = (long long)q.nc * 2048, xrow = (long long)q.nc * 4096;
-  const __amdgpu_buffer_rsrc_t wrs = resource(a.packed + min(v0 / 16, q.n16) * wrow, (q.n16 - v0 / 16) * wrow);
+  const int w0 = min(v0 / 16, q.n16 - 1), w_last = min(q.n16 - 1 - w0, 3), x_last = min(a.mb - 1 - mb0, NB - 1);
+  const __amdgpu_buffer_rsrc_t wrs = resource(a.packed + w0 * wrow, (w_last + 1) * wrow);
   constexpr bool kOwn = !std::is_void<E>::value;
   using X = std::conditional_t<kOwn, E, F32>;
   const __amdgpu_buffer_rsrc_t xrs =
-      kOwn ? resource(nullptr, 0) : resource(a.xrows + mb0 * xrow, (a.mb - mb0) * xrow);
+      kOwn ? resource(nullptr, 0) : resource(a.xrows + mb0 * xrow, (x_last + 1) * xrow);
   const float* sc = a.scales + (long long)min(v0 / kBlock, q.nr - 1) * q.nc;
   const int wo = lane * 16, xo = threadIdx.x * 16;
 
@@ -307,13 +307,13 @@ __global__ __launch_bounds__(256, 2) void k_fp8_tile(Fp8Dims q, Fp8Call a) {
     for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        raw[u][h] = __builtin_amdgcn_raw_buffer_load_b128(wrs, (wo + past) + h * 1024, (u * q.nc + c) * 2048, NT ? 2 : 0);
+        raw[u][h] = __builtin_amdgcn_raw_buffer_load_b128(wrs, (wo + past) + h * 1024, (min(u, w_last) * q.nc + c) * 2048, NT ? 2 : 0);
   };
   auto load_x = [&](int c, int past, uint8_t* stage) {
 #pragma unroll
     for (int j = 0; j < NB; ++j)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          xrs, (__attribute__((address_space(3))) void*)(stage + j * 4096 + wid * 1024), 16, xo + past, (j * q.nc + c) * 4096, 0, 0);
+          xrs, (__attribute__((address_space(3))) void*)(stage + j * 4096 + wid * 1024), 16, xo + past, (min(j, x_last) * q.nc + c) * 4096, 0, 0);
   };
   // or a thread's 8 columns of a row of each block
   float own[kOwn ? NB : 1][8];

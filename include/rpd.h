@@ -587,7 +587,7 @@ rpd_status rpd_fp8_quantize(int32_t rows, int32_t d, int32_t dtype, const void* 
  *   transpose  0: packs W; 1: packs its transpose, a head of d rows and V
  *              columns (for the gradient of the rows: dx = dy W)
  *   packed     device, 256-byte aligned, rpd_fp8_packed_size bytes (of (d, V)
- *              with transpose)
+ *              with transpose), not over codes or scales
  * The codes are laid out once, for the matrix cores.
  */
 size_t rpd_fp8_packed_size(int32_t V, int32_t d); /* 0 if out of range */
@@ -603,9 +603,10 @@ size_t rpd_fp8_workspace_size(int32_t V, int32_t d, int32_t M, int32_t statistic
  * first, as rpd_fp8_quantize does with block_rows 1; with x^ what their codes
  * and scales stand for, logits y = W x^, or the softmax statistics of
  * logit_scale * y as rpd_gate_commit takes them (of a head of 131072 rows and
- * more, or of many x, the logits then never reach memory). Codes and x^ are exact operands (magnitudes below 2^-126 may count
- * as 0, and what rounds to 2^128 is infinite), sums are float32. Equal rows of the head give equal logits; of equal
- * logits the lowest index is the argmax.
+ * more, or of many x, the logits then never reach memory). Codes and x^ are
+ * exact operands (magnitudes below 2^-126 may count as 0, and what rounds to
+ * 2^128 is infinite), sums are float32. Equal rows of the head give equal
+ * logits; of equal logits the lowest index is the argmax.
  *   M          0 <= M <= 2^20 (0: nothing is done)
  *   x          device [M][d] of type x_dtype (bf16, fp16 or fp32), rows x_stride >= d apart
  *   logits     device [M][V] of type logits_dtype (any of the three), rows

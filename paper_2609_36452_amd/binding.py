@@ -1002,6 +1002,10 @@ def sample(logits: torch.Tensor, r: torch.Tensor, logit_scale: float | torch.Ten
     (float32, top_k int32). Returns token int32, prob float32 (the token's probability among the kept) and kept int32
     (how many were kept) of r's shape, and with ``filtered`` the logits with -inf for what was not kept, as
     ``verify_draft`` takes them. Not recorded by autograd. ``stream`` as in ``verify_draft``."""
+    if not torch.is_tensor(top_k):   # (a C int would keep the low bits of any number)
+        if int(top_k) != top_k or top_k < 0:
+            raise ValueError(f"top_k must be a whole number >= 0 (got {top_k})")
+        top_k = min(int(top_k), 2**31 - 1)
     extra = {k: v for k, v in dict(logit_scale=logit_scale, top_k=top_k, top_p=top_p, min_p=min_p).items()
              if torch.is_tensor(v)}
     dev = _one_device("logits", logits, r=r, **extra)

@@ -127,6 +127,10 @@ rpd_status rpd_fp8_pack(int32_t V, int32_t d, const uint8_t* codes, const float*
   const Fp8Dims q = transpose ? fp8_dims(d, V) : fp8_dims(V, d);
   if (packed_bytes < q.bytes)
     return fail(RPD_ERR_WORKSPACE_TOO_SMALL, "packed has %zu bytes, %zu needed", packed_bytes, q.bytes);
+  const long long bytes = (long long)q.bytes;
+  if (rows_meet(codes, 0, (long long)V * d, packed, 0, bytes, 1) ||
+      rows_meet(scales, 0, up_div(V, kFp8Block) * up_div(d, kFp8Block) * 4, packed, 0, bytes, 1))
+    return fail(RPD_ERR_BAD_PARAM, "packed must not overlap codes or scales");   // both are read while it is written
   const hipError_t e =
       launch_fp8_pack(q, codes, scales, transpose != 0, static_cast<uint8_t*>(packed), static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(RPD_ERR_HIP, "launch: %s", hipGetErrorString(e));

@@ -67,9 +67,10 @@ def test_head_sizes():
 
 @pytest.mark.parametrize("kw,status", [
     (dict(codes=None), 1), (dict(scales=None), 1), (dict(packed=None), 1), (dict(scales=P + 2), 5), (dict(packed=P + 16), 5),
-    (dict(nbytes=1000), 4), (dict(tr=2), 3)])
+    (dict(nbytes=1000), 4), (dict(tr=2), 3), (dict(codes=2 * P), 3), (dict(scales=2 * P), 3),
+    (dict(codes=2 * P - 199999), 3), (dict(codes=2 * P + 63 * 2 * 2048), 3), (dict(scales=2 * P - 60, tr=1), 3)])
 def test_pack_refusals(kw, status):
-    a = dict(codes=P, scales=P, packed=P, nbytes=1 << 30, tr=0)
+    a = dict(codes=P, scales=P, packed=2 * P, nbytes=1 << 30, tr=0)
     a.update(kw)
     assert rpd.lib().rpd_fp8_pack(1000, 200, a["codes"], a["scales"], a["tr"], a["packed"], a["nbytes"], None) == status
 
@@ -135,6 +136,12 @@ def _sample(**kw):
 def test_sample_refusals(kw, status):
     assert rpd.lib().rpd_sample_tokens(ctypes.byref(_sample(**kw)), P, 1 << 40, None) == status
     assert rpd.last_error()
+
+
+@pytest.mark.parametrize("top_k", [-1, 2.5, -2**32 + 5])
+def test_sample_whole_top_k(top_k):
+    with pytest.raises(ValueError, match="top_k"):
+        rpd.sample(torch.zeros((2, 8)), torch.zeros((2,)), top_k=top_k)
 
 
 def test_sample_nothing():

@@ -211,6 +211,8 @@ def test_sample_strided_rows_and_leading_dimensions():
     assert all(torch.equal(a[k].reshape(b[k].shape), b[k]) for k in a)
     one = rpd.sample(wide[5], r[5], top_k=9)
     assert one["token"].shape == () and int(one["token"]) == int(b["token"][5])
+    every = rpd.sample(wide, r, top_k=2**32 + 5)   # more than a C int holds: all of them
+    assert every["kept"].unique().tolist() == [3010] and torch.equal(every["token"], rpd.sample(wide, r)["token"])
     none = rpd.sample(wide[:0], r[:0], filtered=True)
     assert none["token"].shape == (0,) and none["logits"].shape == (0, 3010)
 

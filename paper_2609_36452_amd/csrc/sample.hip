@@ -737,6 +737,8 @@ struct Keys {
   uint32_t kept;
   double mass;
   uint32_t slab[64];
+  uint32_t listed, list_slot[kThreads];   // the counted tokens, where they are few: a thread each
+  int list_index[kThreads];
 };
 
 __device__ __forceinline__ uint32_t count_of(const Keys& s, uint32_t slot) {
@@ -822,7 +824,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
       tail[e] = (2 * e < tails ? row[tail_at + 2 * e] : some) | (2 * e + 1 < tails ? row[tail_at + 2 * e + 1] : some) << 16;
   }
   for (int i = t; i < 8192; i += kThreads) reinterpret_cast<u32x4*>(s.count)[i] = u32x4{0u, 0u, 0u, 0u};
-  if (t == 0) s.give_up = 0;
+  if (t == 0) s.give_up = s.listed = 0;
   u16x2 lo = {0xffff, 0xffff}, hi = {0, 0};
   auto take = [&](uint32_t& x) __attribute__((always_inline)) {
     x = slots_of(x);
@@ -901,6 +903,8 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
   auto count = [&](uint32_t x) __attribute__((always_inline)) {
     atomicAdd(&s.count[x & 0x7fff], 1u + (x >> 15) * 0xffffu);
   };
+  typename E::t* out = a.filtered ? static_cast<typename E::t*>(a.filtered) + n * a.filtered_stride : nullptr;
+  bool listed = false;
   if (last <= end) {   // everything
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -919,8 +923,9 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
       if (2 * e + 1 < tails) count(tail[e] >> 16);
     }
   } else {
+    const bool list = few || min_alone;
     uint32_t in = 0, inf = 0;
-    auto vector = [&](const uint32_t (&x)[4], int tokens) __attribute__((always_inline)) {
+    auto vector = [&](const uint32_t (&x)[4], int i0, int tokens) __attribute__((always_inline)) {
       u16x2 m = {0xffff, 0xffff};
 #pragma unroll
       for (int e = 0; e < 4; ++e) m = __builtin_elementwise_min(m, __builtin_bit_cast(u16x2, x[e]));
@@ -930,7 +935,15 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
           const uint32_t y = e & 1 ? x[e >> 1] >> 16 : x[e >> 1] & 0xffff;
           if (y <= end && e < tokens) {
             count(y);
-            ++in;
+            if (list) {
+              const uint32_t at = atomicAdd(&s.listed, 1u);
+              if (at < kThreads) {
+                s.list_slot[at] = y;
+                s.list_index[at] = i0 + e;
+              }
+            } else {
+              ++in;
+            }
           }
         }
       }
@@ -941,10 +954,10 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
     };
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      if (j < steps) vector(v[j], 8);
+      if (j < steps) vector(v[j], 8 * (t + j * kThreads), 8);
       __builtin_amdgcn_sched_barrier(0);
     }
-    vector(tail, tails);
+    vector(tail, tail_at, tails);
 #pragma unroll
     for (int k = 32; k >= 1; k >>= 1) {
       inf += __shfl_xor(inf, k);
@@ -956,10 +969,21 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
       s.wave_hi[wid] = in;
     }
     __syncthreads();
-    seen = 0;
+    seen = list ? s.listed : 0;
     for (int k = 0; k < kWaves; ++k) {
       infs += s.wave_n[k];
       seen += s.wave_hi[k];
+    }
+    seen = __builtin_amdgcn_readfirstlane(seen);
+    listed = list && seen <= kThreads;
+    // then nearly all that is filtered is -inf: written now, beside what follows, and the kept ones over it
+    if (listed && out) {
+      const uint32_t gone = (uint32_t)E::to(-INFINITY) * 0x10001u;
+#pragma unroll 1
+      for (int j = 0; j < steps; ++j)
+        reinterpret_cast<Any16*>(out + 8 * (t + j * kThreads))->v = u32x4{gone, gone, gone, gone};
+#pragma unroll 1
+      for (int e = 0; e < tails; ++e) out[tail_at + e] = (typename E::t)gone;
     }
   }
   __syncthreads();
@@ -1087,6 +1111,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
       s.pick = p;
       s.cut = cut;
       s.is_cut = is_cut;
+      s.kept = kept;
       if (a.prob) a.prob[n] = (float)(p.w / mass);
       if (a.kept) a.kept[n] = (int)kept;
     }
@@ -1097,10 +1122,28 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
     const uint32_t slot = __builtin_amdgcn_readfirstlane(p.slot), eq = __builtin_amdgcn_readfirstlane(p.eq),
                    at = __builtin_amdgcn_readfirstlane(p.at);
     const bool zero = slot == kZero;
-    if (t == 0) s.token = -1;
+    if (t == 0) {
+      s.token = -1;
+      s.wave_n[0] = 0;
+    }
     if (t <= NV) s.slab[t] = 0;
     __syncthreads();
     auto same = [&](uint32_t x) __attribute__((always_inline)) { return x == slot || (zero && x == kMinusZero); };
+    if (listed && eq <= 64) {   // among the listed: s.slab[0 ..] takes the indexes of the equal ones
+      const bool mine = t < (int)seen && same(s.list_slot[t]);
+      const uint32_t index = mine ? s.list_index[t] : 0;
+      if (mine && eq == 1) s.token = index;
+      if (eq > 1) {
+        if (mine) s.slab[atomicAdd(&s.wave_n[0], 1u)] = index;
+        __syncthreads();
+        uint32_t before = 0;
+        if (mine)
+          for (uint32_t k = 0; k < eq; ++k) before += s.slab[k] < index;
+        if (mine && before == at) s.token = index;
+      }
+      __syncthreads();
+      return s.token;
+    }
     auto matches = [&](const uint32_t (&x)[4], int tokens) __attribute__((always_inline)) {   // a bit a token
       uint32_t m = 0;
 #pragma unroll
@@ -1154,17 +1197,27 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
   __syncthreads();
   const int token = index_of(s.pick);
   if (t == 0) a.token[n] = token;
-  if (!a.filtered) return;
-  typename E::t* out = static_cast<typename E::t*>(a.filtered) + n * a.filtered_stride;
+  if (!out) return;
   // what comes before the cut's slot stays, and of its tokens those up to the last kept one
   const bool is_cut = s.is_cut;
   uint32_t slot = __builtin_amdgcn_readfirstlane(is_cut ? s.cut.slot : kLow);
   int until = V;
   if (is_cut && s.cut.at + 1 < s.cut.eq) until = __builtin_amdgcn_readfirstlane(index_of(s.cut));
   const uint32_t after = slot == kZero ? kMinusZero : slot;
+  if (listed && s.kept <= seen) {   // (else some are kept that were not counted, of no mass)
+    if (t < (int)seen) {
+      const uint32_t x = s.list_slot[t], i = s.list_index[t];
+      if (x <= after && !(x >= slot && (int)i > until)) out[i] = (typename E::t)(x & 0x8000 ? x : x ^ 0x7fff);
+    }
+    return;
+  }
   const uint32_t gone = (uint32_t)E::to(-INFINITY) * 0x10001u;
   auto left = [&](const uint32_t (&x)[4], int i0) __attribute__((always_inline)) {
-    u32x4 o;
+    u32x4 o = {gone, gone, gone, gone};
+    u16x2 m = {0xffff, 0xffff};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m = __builtin_elementwise_min(m, __builtin_bit_cast(u16x2, x[e]));
+    if (min((uint32_t)m.x, (uint32_t)m.y) > after) return o;   // most, in most rows
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       // halves above `after` go: 0xffff there

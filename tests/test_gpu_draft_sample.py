@@ -150,6 +150,24 @@ def test_sample_short_lists(dtype):
         _check(z, _r(5, k), top_k=k, top_p=0.99)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [2500, 30001, 152064])
+def test_sample_short_lists_of_equal_logits(V, dtype):
+    """A few equal tokens (zeros of both signs too) and more than a wave of them, at the ends of short lists."""
+    g = torch.Generator().manual_seed(30)
+    z = -3.0 - torch.rand((6, V), generator=g)
+    for row, (n, value) in enumerate([(2, 1.0), (40, 0.0), (64, 2.0), (65, 0.0), (300, 1.0), (1100, 0.0)]):
+        at = torch.randperm(V, generator=g)[:n]
+        z[row, at] = value
+        if value == 0.0:
+            z[row, at[::2]] = -0.0
+        z[row, (at[0] + 1) % V] = 3.0
+    z = z.to(dtype)
+    for i, kw in enumerate((dict(top_k=2), dict(top_k=21), dict(top_k=64, top_p=0.9), dict(top_k=66), dict(top_k=200),
+                            dict(top_k=1000), dict(min_p=0.04), dict(min_p=0.04, scale=0.9))):
+        _check(z, _r(6, 31 + i), **kw)
+
+
 def test_sample_random_numbers_at_their_ends():
     z = _logits(8, 2048, BF, 12)
     for r in (0.0, 2.0 ** -24, LAST):

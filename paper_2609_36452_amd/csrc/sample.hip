@@ -95,6 +95,99 @@ __device__ __forceinline__ double lane_of(double v, int at) {
   return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), at), __builtin_amdgcn_readlane(__double2loint(v), at));
 }
 
+// All that may be kept, where it is few: no bins, but the tokens in their order, each thread counting those before its own.
+constexpr int kShort = 256;
+struct Short {
+  unsigned long long key[kShort];   // places in the order, without their ties
+  double e[kShort];                 // masses in that order
+  int index[kShort];
+  uint32_t in[kShort / 64], kept;
+};
+struct Filters {
+  int top_k;
+  float top_p, r;
+  bool least;
+  double limit;
+};
+// Of thread t the t-th of `seen` tokens, of place `slot` (rising in the order) and `index`; `all` may be kept before top_k.
+// Writes the row's token, prob and kept; returns the tokens kept, and the thread's rank.
+__device__ __forceinline__ uint32_t draw_short(Short& s, const SampleCall& a, int n, const Weigh& w, const Filters& f,
+                                               uint32_t seen, uint32_t all, uint32_t slot, int index, float z, uint32_t& rank) {
+  const int t = threadIdx.x, lane = t & 63, wid = t >> 6;
+  const bool mine = t < (int)seen;
+  const unsigned long long key = mine ? (unsigned long long)slot << 32 | (uint32_t)index : ~0ull;
+  if (t < kShort) {
+    s.key[t] = key;
+    if (!mine) s.e[t] = 0.0;
+  }
+  __syncthreads();
+  rank = 0;
+  if (t < kShort) {
+    if (wid * 64 < (int)seen) {
+#pragma unroll 8
+      for (int k = 0; k < ((int)seen + 7) / 8 * 8; ++k) rank += s.key[k] < key;
+    }
+    const double below = w.below(z);
+    if (mine) {
+      s.e[rank] = exp(-below);
+      s.index[rank] = index;
+    }
+    const unsigned long long in = __ballot(mine && below <= f.limit);
+    if (lane == 0) s.in[wid] = __popcll(in);
+  }
+  __syncthreads();
+  if (wid == 0) {   // four tokens a lane
+    double e[4], m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[i] = s.e[4 * lane + i];
+    const double own = (e[0] + e[1]) + (e[2] + e[3]), upto = wave_scan(own);
+    m[0] = (upto - own) + e[0];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) m[i] = m[i - 1] + e[i];
+    auto of = [&](const double (&x)[4], uint32_t i) {
+      const uint32_t c = i & 3;
+      return lane_of(c == 0 ? x[0] : c == 1 ? x[1] : c == 2 ? x[2] : x[3], i >> 2);
+    };
+    // of the first `among`, how many hold
+    auto count = [&](uint32_t among, auto holds) {
+      uint32_t c = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c += __popcll(__ballot(4 * lane + i < (int)among && holds(m[i])));
+      return c;
+    };
+    uint32_t kept = all;
+    if (f.top_k > 0) kept = min(kept, (uint32_t)f.top_k);
+    double mass = of(m, kept - 1);
+    if (f.top_p < 1.f) {
+      const double bound = fmax((double)f.top_p, 0.0) * mass;
+      kept = min(kept, 1 + count(kept, [&](double x) { return x < bound; }));
+    }
+    if (f.least) {
+      uint32_t in = 0;
+#pragma unroll
+      for (int i = 0; i < kShort / 64; ++i) in += s.in[i];
+      kept = min(kept, in);
+    }
+    kept = __builtin_amdgcn_readfirstlane(kept);
+    mass = of(m, kept - 1);
+    const double bound = fmin(fmax((double)f.r, 0.0), 1.0) * mass;
+    const uint32_t at = __builtin_amdgcn_readfirstlane(min(kept - 1, count(kept, [&](double x) { return x <= bound; })));
+    const double p = of(e, at);
+    if (lane == 0) {
+      a.token[n] = s.index[at];
+      if (a.prob) a.prob[n] = (float)(p / mass);
+      if (a.kept) a.kept[n] = (int)kept;
+      s.kept = kept;
+    }
+  }
+  __syncthreads();
+  return s.kept;
+}
+// whether it can: what top_k keeps has been seen
+__device__ __forceinline__ bool short_enough(uint32_t seen, uint32_t all, int top_k) {
+  return seen <= kShort && (top_k <= 0 || ((uint32_t)top_k < all ? (uint32_t)top_k <= seen : seen == all));
+}
+
 // The token found: the `at`-th (by index) of `eq` tokens of the logit `key`, before which lie n tokens of mass m; each has mass w.
 struct Place {
   uint32_t key, n, eq, at;
@@ -126,6 +219,7 @@ struct Shared {
     struct {
       Bins all, part;
     };
+    Short few;
     Counts copies[4];   // a row's tokens are counted by every fourth lane apart: half of a wave would meet in one place
   };
   uint32_t list_key[kListed];      // the tokens with keys list_lo .. list_hi (an empty range at first)
@@ -562,15 +656,15 @@ __device__ __forceinline__ void sample_row(const SampleCall& a, int n, Shared& s
 #pragma unroll
       for (int e = 0; e < N; ++e) add(z[e]);
     } else if (largest(z[0], z) >= above) {
-#pragma unroll 1
+#pragma unroll
       for (int e = 0; e < N; ++e) {
-        const float y = E::one(row + i + e) + 0.f;   // (read again: they are few)
-        if (!(y >= above)) continue;
-        add(y);
-        const uint32_t at = atomicAdd(&s.listed, 1u);
-        if (at < kListed) {
-          s.list_key[at] = key_of(y);
-          s.list_index[at] = i + e;
+        const float y = z[e] + 0.f;
+        if (y >= above) {
+          const uint32_t at = atomicAdd(&s.listed, 1u);
+          if (at < kListed) {
+            s.list_key[at] = key_of(y);
+            s.list_index[at] = i + e;
+          }
         }
       }
     }
@@ -578,16 +672,34 @@ __device__ __forceinline__ void sample_row(const SampleCall& a, int n, Shared& s
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) infs += __shfl_xor(infs, k);
   if (lane == 0) s.wave_n[wid] = infs;
+  __syncthreads();
+  infs = 0;
+  for (int v = 0; v < kWaves; ++v) infs += s.wave_n[v];
+  uint32_t kept = V - infs;
+  if (list && short_enough(s.listed, kept, top_k)) {
+    if (out)
+      for (int i = t; i < V; i += kThreads) out[i] = E::to(-INFINITY);
+    const uint32_t key = s.list_key[t];   // (of the listed only)
+    const int index = s.list_index[t];
+    uint32_t rank;
+    const uint32_t seen = s.listed;
+    const uint32_t n_kept = draw_short(s.few, a, n, w, Filters{top_k, top_p, a.r[n], least, limit}, seen,
+                                       top_k > 0 ? kept : seen, ~key, index, value_of(key), rank);
+    if (out && t < (int)seen && rank < n_kept) out[index] = row[index];
+    return;
+  }
+  if (list && s.listed <= kListed)
+    for (uint32_t i = t; i < s.listed; i += kThreads) add(value_of(s.list_key[i]));
+  else if (list)
+    each<E>(row, V, [&](float z, int) {
+      if (z >= above) add(z);
+    });
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) inside += __shfl_xor(inside, k);
   if (lane == 0) s.wave_in[wid] = inside;
   __syncthreads();
-  inside = infs = 0;
-  for (int v = 0; v < kWaves; ++v) {
-    inside += s.wave_in[v];
-    infs += s.wave_n[v];
-  }
-  uint32_t kept = V - infs;
+  inside = 0;
+  for (int v = 0; v < kWaves; ++v) inside += s.wave_in[v];
   if (t == 0) {
     s.list_lo = list && s.listed <= kListed ? from : 1;
     s.list_hi = list && s.listed <= kListed ? key_top : 0;
@@ -725,6 +837,8 @@ struct KeyPlace {   // as Place, with a slot in place of the key
   __device__ __forceinline__ double upto() const { return m + (double)(at + 1) * w; }
 };
 
+constexpr int kCounted = 2 * kThreads;   // as many as fit beside the table
+
 struct Keys {
   uint32_t count[32768];   // of slot s in word s % 32768: the positive values in the low halves, the negative in the high ones
   uint32_t n_upto[kThreads];
@@ -737,8 +851,8 @@ struct Keys {
   uint32_t kept;
   double mass;
   uint32_t slab[64];
-  uint32_t listed, list_slot[kThreads];   // the counted tokens, where they are few: a thread each
-  int list_index[kThreads];
+  uint32_t listed, list_slot[kCounted];   // the counted tokens, where they are few
+  int list_index[kCounted];
 };
 
 __device__ __forceinline__ uint32_t count_of(const Keys& s, uint32_t slot) {
@@ -849,8 +963,10 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
   }
   // Of a short list (top_k): a sixteenth of it, the j-th smallest of the lanes' slots, bit by bit: of the lanes that agree
   // with it so far, those with a 0 come first. The worst of the waves' is a bound for the whole list.
+  // (Not of longer ones: of 126464 tokens top_k of 200 takes 22.6 us so and 300 24.2, counting all of them 23.5. The
+  // filtered row is quicker written from a list: 32 rows of 152064 with lists of up to 472 take 36 us so, 44 counting all.)
   uint32_t bound = 0;
-  const bool few = top_k > 0 && top_k <= kThreads;
+  const bool few = top_k > 0 && top_k <= (a.filtered ? 512 : 256);
   if (few) {
     const uint32_t own = tails == 0 && steps == 0 ? kLow : mine;   // a lane without a token of its own
     int j = (top_k + kWaves - 1) / kWaves;
@@ -905,6 +1021,12 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
   };
   typename E::t* out = a.filtered ? static_cast<typename E::t*>(a.filtered) + n * a.filtered_stride : nullptr;
   bool listed = false;
+  // (comparisons of the number of vectors are cheap to repeat, but kept from one loop to the next they fill the registers)
+  auto again = [&] {
+    int x = steps;
+    asm("" : "+s"(x));
+    return x;
+  };
   if (last <= end) {   // everything
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -923,41 +1045,74 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
       if (2 * e + 1 < tails) count(tail[e] >> 16);
     }
   } else {
-    const bool list = few || min_alone;
     uint32_t in = 0, inf = 0;
-    auto vector = [&](const uint32_t (&x)[4], int i0, int tokens) __attribute__((always_inline)) {
+    auto low_half = [](uint32_t x) { return x & 0xffff; };
+    auto least_of = [](const uint32_t (&x)[4]) {
       u16x2 m = {0xffff, 0xffff};
 #pragma unroll
       for (int e = 0; e < 4; ++e) m = __builtin_elementwise_min(m, __builtin_bit_cast(u16x2, x[e]));
-      if (min((uint32_t)m.x, (uint32_t)m.y) <= end) {
+      return min((uint32_t)m.x, (uint32_t)m.y);
+    };
+    auto infs_of = [&](const uint32_t (&x)[4], int tokens) __attribute__((always_inline)) {
+      if (last != kLow) return;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t y = e & 1 ? x[e >> 1] >> 16 : x[e >> 1] & 0xffff;
-          if (y <= end && e < tokens) {
-            count(y);
-            if (list) {
-              const uint32_t at = atomicAdd(&s.listed, 1u);
-              if (at < kThreads) {
-                s.list_slot[at] = y;
-                s.list_index[at] = i0 + e;
-              }
-            } else {
+      for (int e = 0; e < 8; ++e) inf += (e & 1 ? x[e >> 1] >> 16 : low_half(x[e >> 1])) == kLow && e < tokens;
+    };
+    if (few || min_alone) {
+      auto take = [&](uint32_t y, int i) __attribute__((always_inline)) {
+        const uint32_t at = atomicAdd(&s.listed, 1u);
+        if (at < kCounted) {
+          s.list_slot[at] = y;
+          s.list_index[at] = i;
+        }
+      };
+      auto vector = [&](const uint32_t (&x)[4], int i0, int tokens) __attribute__((always_inline)) {
+        if (least_of(x) <= end) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t y0 = low_half(x[e]), y1 = x[e] >> 16;
+            if (min(y0, y1) <= end) {
+              if (y0 <= end && 2 * e < tokens) take(y0, i0 + 2 * e);
+              if (y1 <= end && 2 * e + 1 < tokens) take(y1, i0 + 2 * e + 1);
+            }
+          }
+        }
+        infs_of(x, tokens);
+      };
+      const int held = again();
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        if (j < held) vector(v[j], 8 * (t + j * kThreads), 8);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      vector(tail, tail_at, tails);
+      __syncthreads();
+      seen = __builtin_amdgcn_readfirstlane(s.listed);
+      listed = seen <= kCounted;
+    }
+    if (!listed) {
+      auto vector = [&](const uint32_t (&x)[4], int tokens) __attribute__((always_inline)) {
+        if (least_of(x) <= end) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t y = e & 1 ? x[e >> 1] >> 16 : low_half(x[e >> 1]);
+            if (y <= end && e < tokens) {
+              count(y);
               ++in;
             }
           }
         }
-      }
-      if (last == kLow) {
+        infs_of(x, tokens);
+      };
+      inf = 0;
+      const int held = again();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) inf += (e & 1 ? x[e >> 1] >> 16 : x[e >> 1] & 0xffff) == kLow && e < tokens;
+      for (int j = 0; j < NV; ++j) {
+        if (j < held) vector(v[j], 8);
+        __builtin_amdgcn_sched_barrier(0);
       }
-    };
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      if (j < steps) vector(v[j], 8 * (t + j * kThreads), 8);
-      __builtin_amdgcn_sched_barrier(0);
+      vector(tail, tails);
     }
-    vector(tail, tail_at, tails);
 #pragma unroll
     for (int k = 32; k >= 1; k >>= 1) {
       inf += __shfl_xor(inf, k);
@@ -969,13 +1124,12 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
       s.wave_hi[wid] = in;
     }
     __syncthreads();
-    seen = list ? s.listed : 0;
+    if (!listed) seen = 0;
     for (int k = 0; k < kWaves; ++k) {
       infs += s.wave_n[k];
       seen += s.wave_hi[k];
     }
     seen = __builtin_amdgcn_readfirstlane(seen);
-    listed = list && seen <= kThreads;
     // then nearly all that is filtered is -inf: written now, beside what follows, and the kept ones over it
     if (listed && out) {
       const uint32_t gone = (uint32_t)E::to(-INFINITY) * 0x10001u;
@@ -988,6 +1142,20 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
   }
   __syncthreads();
   const uint32_t finite = V - infs;
+  const bool low = least && limit > 63.0;   // what min_p keeps may not have been counted
+  if (listed && !low && short_enough(seen, finite, top_k)) {
+    const uint32_t x = s.list_slot[t];   // (of the listed only)
+    const int index = s.list_index[t];
+    uint32_t rank;
+    const uint32_t kept = draw_short(*reinterpret_cast<Short*>(s.count), a, n, w, Filters{top_k, top_p, a.r[n], least, limit},
+                                     seen, top_k > 0 ? finite : seen, x == kMinusZero ? kZero : x, index, slot_value<E>(x), rank);
+    if (out && t < (int)seen && rank < kept) out[index] = (typename E::t)(x & 0x8000 ? x : x ^ 0x7fff);
+    return;
+  }
+  if (listed) {
+    for (uint32_t i = t; i < seen; i += kThreads) count(s.list_slot[i]);
+    __syncthreads();
+  }
   if (t == 0) {   // the two zeros are equal
     const uint32_t minus = count_of(s, kMinusZero);
     if (minus) {
@@ -1060,7 +1228,6 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
   // A count that ran over its 16 bits shows in their sum. Those, and ranks among what is not counted, are rare and left
   // to the other way.
   const bool far = top_k > 0 && (uint32_t)top_k > counted && (uint32_t)top_k < finite;
-  const bool low = least && limit > 63.0;
   if (seen != counted || s.give_up || far || low) {
     __syncthreads();
     sample_row_apart<E>(a, n, *reinterpret_cast<Shared*>(lds));
@@ -1130,16 +1297,18 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
     __syncthreads();
     auto same = [&](uint32_t x) __attribute__((always_inline)) { return x == slot || (zero && x == kMinusZero); };
     if (listed && eq <= 64) {   // among the listed: s.slab[0 ..] takes the indexes of the equal ones
-      const bool mine = t < (int)seen && same(s.list_slot[t]);
-      const uint32_t index = mine ? s.list_index[t] : 0;
-      if (mine && eq == 1) s.token = index;
+      for (uint32_t i = t; i < seen; i += kThreads)
+        if (same(s.list_slot[i])) {
+          if (eq == 1) s.token = s.list_index[i];
+          else s.slab[atomicAdd(&s.wave_n[0], 1u)] = s.list_index[i];
+        }
       if (eq > 1) {
-        if (mine) s.slab[atomicAdd(&s.wave_n[0], 1u)] = index;
         __syncthreads();
-        uint32_t before = 0;
-        if (mine)
-          for (uint32_t k = 0; k < eq; ++k) before += s.slab[k] < index;
-        if (mine && before == at) s.token = index;
+        if (t < (int)eq) {   // each sees how many lie before it
+          uint32_t before = 0;
+          for (uint32_t k = 0; k < eq; ++k) before += s.slab[k] < s.slab[t];
+          if (before == at) s.token = s.slab[t];
+        }
       }
       __syncthreads();
       return s.token;
@@ -1168,9 +1337,10 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
         else if (m) atomicAdd(&s.slab[j < steps ? j : NV], __popc(m));
       }
     };
+    const int held = again();
 #pragma unroll
     for (int j = 0; j < NV; ++j)
-      if (j < steps) vector(v[j], j, 8);
+      if (j < held) vector(v[j], j, 8);
     vector(tail, steps, tails);
     __syncthreads();
     if (eq > 1) {
@@ -1205,8 +1375,8 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
   if (is_cut && s.cut.at + 1 < s.cut.eq) until = __builtin_amdgcn_readfirstlane(index_of(s.cut));
   const uint32_t after = slot == kZero ? kMinusZero : slot;
   if (listed && s.kept <= seen) {   // (else some are kept that were not counted, of no mass)
-    if (t < (int)seen) {
-      const uint32_t x = s.list_slot[t], i = s.list_index[t];
+    for (uint32_t k = t; k < seen; k += kThreads) {
+      const uint32_t x = s.list_slot[k], i = s.list_index[k];
       if (x <= after && !(x >= slot && (int)i > until)) out[i] = (typename E::t)(x & 0x8000 ? x : x ^ 0x7fff);
     }
     return;
@@ -1217,14 +1387,15 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
     u16x2 m = {0xffff, 0xffff};
 #pragma unroll
     for (int e = 0; e < 4; ++e) m = __builtin_elementwise_min(m, __builtin_bit_cast(u16x2, x[e]));
-    if (min((uint32_t)m.x, (uint32_t)m.y) > after) return o;   // most, in most rows
+    const uint32_t bound = i0 > until ? slot - 1 : after;
+    if (min((uint32_t)m.x, (uint32_t)m.y) > bound) return o;   // most, in most rows
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      // halves above `after` go: 0xffff there
+      // halves above the bound go: 0xffff there
       const u16x2 y = __builtin_bit_cast(u16x2, x[e]);
-      const u16x2 over = y ^ __builtin_elementwise_min(y, u16x2{(unsigned short)after, (unsigned short)after});
+      const u16x2 over = y ^ __builtin_elementwise_min(y, u16x2{(unsigned short)bound, (unsigned short)bound});
       uint32_t drop = __builtin_bit_cast(uint32_t, u16x2{0, 0} - __builtin_elementwise_min(over, u16x2{1, 1}));
-      if (until < V) {   // and of the cut's own those behind the last kept one
+      if ((uint32_t)(until - i0) < 8u) {   // the last kept one of the cut's own is in here
         const uint32_t x0 = x[e] & 0xffff, x1 = x[e] >> 16;
         drop |= x0 >= slot && i0 + 2 * e > until ? 0xffffu : 0;
         drop |= x1 >= slot && i0 + 2 * e + 1 > until ? 0xffff0000u : 0;
@@ -1233,9 +1404,10 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
     }
     return o;
   };
+  const int held = again();
 #pragma unroll
   for (int j = 0; j < NV; ++j)
-    if (j < steps) reinterpret_cast<Any16*>(out + 8 * (t + j * kThreads))->v = left(v[j], 8 * (t + j * kThreads));
+    if (j < held) reinterpret_cast<Any16*>(out + 8 * (t + j * kThreads))->v = left(v[j], 8 * (t + j * kThreads));
   const u32x4 o = left(tail, tail_at);
   if (tails == 8) {
     reinterpret_cast<Any16*>(out + tail_at)->v = o;

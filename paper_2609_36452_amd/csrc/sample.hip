@@ -1319,6 +1319,8 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
       for (int e = 0; e < 8; ++e) m |= (uint32_t)(same(e & 1 ? x[e >> 1] >> 16 : x[e >> 1] & 0xffff) && e < tokens) << e;
       return m;
     };
+    // a few equal ones are gathered; more are counted in slabs, a vector each, and sought in one of them
+    const bool gather = !listed && eq <= 256;
     auto vector = [&](const uint32_t (&x)[4], int j, int tokens) __attribute__((always_inline)) {
       // a half that is equal leaves 0 in place of 1
       auto differ = [&](uint32_t key) __attribute__((always_inline)) {
@@ -1332,9 +1334,15 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
       uint32_t d = differ(slot);
       if (zero) d &= differ(kMinusZero);
       if (d != 0x10001u) {
-        const uint32_t m = matches(x, tokens);
-        if (m && eq == 1) s.token = 8 * (t + j * kThreads) + __builtin_ctz(m);
-        else if (m) atomicAdd(&s.slab[j < steps ? j : NV], __popc(m));
+        uint32_t m = matches(x, tokens);
+        const int i0 = 8 * (t + j * kThreads);
+        if (eq == 1) {
+          if (m) s.token = i0 + __builtin_ctz(m);
+        } else if (gather) {
+          for (; m; m &= m - 1) s.list_index[atomicAdd(&s.wave_n[0], 1u)] = i0 + __builtin_ctz(m);
+        } else if (m) {
+          atomicAdd(&s.slab[j < steps ? j : NV], __popc(m));
+        }
       }
     };
     const int held = again();
@@ -1343,7 +1351,16 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
       if (j < held) vector(v[j], j, 8);
     vector(tail, steps, tails);
     __syncthreads();
-    if (eq > 1) {
+    if (eq > 1 && gather) {   // each sees how many lie before it
+      if (t < (int)eq) {
+        const int index = s.list_index[t];
+        uint32_t before = 0;
+#pragma unroll 4
+        for (uint32_t k = 0; k < eq; ++k) before += s.list_index[k] < index;
+        if (before == at) s.token = index;
+      }
+      __syncthreads();
+    } else if (eq > 1) {
       uint32_t before = 0;
       int slab = 0;   // NV: the tail
       for (; slab < NV && before + s.slab[slab] <= at; ++slab) before += s.slab[slab];

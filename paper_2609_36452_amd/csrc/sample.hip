@@ -14,11 +14,16 @@
 // and the same in whatever order the atomics come.
 //   Rows of 16 bits that fit a workgroup's registers go another way, below.
 //
+//   Where few tokens may be kept (top_k of 1024 and less, min_p alone), what
+// lies below a bound for them is not counted, and up to 256 that are left are
+// ordered at once.
+//
 // Neither is bound by memory: a row is one workgroup's work, on one CU. Of fp32
-// 126464 logits take 35 us with top_k, 43 without a filter, 46 with top_p; 128
-// such rows 47 to 60, 7 rows of 32003 with min_p 19. What takes the time is an
-// LDS addition of 64 bits (four times one of 32) and an exponential for each
-// token that is counted, and the steps between the workgroup's barriers.
+// 126464 logits take 18 us with top_k 40, 43 without a filter, 47 with top_p;
+// 128 such rows 27, 69 and 62, 7 rows of 32003 with min_p 13. What takes the
+// time is an LDS addition of 64 bits (four times one of 32) and an exponential
+// for each token that is counted, and the steps between the workgroup's
+// barriers.
 #include <cstdint>
 
 #include "logit_rows.h"
@@ -96,6 +101,8 @@ __device__ __forceinline__ double lane_of(double v, int at) {
 }
 
 // All that may be kept, where it is few: no bins, but the tokens in their order, each thread counting those before its own.
+// One row of 126464 with top_k 40 and top_p takes 16.4 us so and 20.4 by the table of 16-bit values, 17.6 and 34.7 by bins;
+// with more tokens than these the counting, which grows with their square, takes as long as the bins.
 constexpr int kShort = 256;
 struct Short {
   unsigned long long key[kShort];   // places in the order, without their ties
@@ -779,10 +786,9 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleCall a) {
 // ------------------------------------------------- 16-bit logits, held in registers --
 //
 // A row of up to 163840 logits of 16 bits fits a workgroup's registers, and a
-// table with a 16-bit count for each of the 65536 values fits its LDS. (A row
-// of 126464 takes 22 us here, 256 rows with top_p 32, 32 of 152064 with the
-// filtered logits written 46, 256 of 32000 16; the other way 31, 57, 92 and
-// 39.) So the
+// table with a 16-bit count for each of the 65536 values fits its LDS. (256
+// rows of 126464 with top_p take 32 us here, 32 of 152064 with the filtered
+// logits written 36 to 42, 256 of 32000 16; the other way 57, 92 and 39.) So the
 // row is read once and counted by value, one LDS addition a token; masses are
 // then counts times the exponential of a value, and no token needs one of its
 // own. A thread sums the 64 values of its block of the table (equally spaced:

@@ -316,13 +316,15 @@ __global__ __launch_bounds__(256, 2) void k_fp8_tile(Fp8Dims q, Fp8Call a) {
     for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        raw[u][h] = __builtin_amdgcn_raw_buffer_load_b128(wrs, (wo + past) + h * 1024, (min(u, w_last) * q.nc + c) * 2048, NT ? 2 : 0);
+        raw[u][h] = __builtin_amdgcn_raw_buffer_load_b128(wrs, (wo + past) + h * 1024, (min(u, w_last) * q.nc + c) * 2048,
+                                                          NT ? 2 : 0);
   };
   auto load_x = [&](int c, int past, uint8_t* stage) {
 #pragma unroll
     for (int j = 0; j < NB; ++j)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          xrs, (__attribute__((address_space(3))) void*)(stage + j * 4096 + wid * 1024), 16, xo + past, (min(j, x_last) * q.nc + c) * 4096, 0, 0);
+          xrs, (__attribute__((address_space(3))) void*)(stage + j * 4096 + wid * 1024), 16, xo + past,
+          (min(j, x_last) * q.nc + c) * 4096, 0, 0);
   };
   // or a thread's 8 columns of a row of each block
   float own[kOwn ? NB : 1][8];

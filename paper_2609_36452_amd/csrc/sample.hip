@@ -195,7 +195,8 @@ __device__ __forceinline__ bool short_enough(uint32_t seen, uint32_t all, int to
   return seen <= kShort && (top_k <= 0 || ((uint32_t)top_k < all ? (uint32_t)top_k <= seen : seen == all));
 }
 
-// The token found: the `at`-th (by index) of `eq` tokens of the logit `key`, before which lie n tokens of mass m; each has mass w.
+// The token found: the `at`-th (by index) of `eq` tokens of the logit `key`, before which lie n tokens of mass m; each has
+// mass w.
 struct Place {
   uint32_t key, n, eq, at;
   int index;   // or -1: not known yet

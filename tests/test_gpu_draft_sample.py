@@ -168,6 +168,22 @@ def test_sample_short_lists_of_equal_logits(V, dtype):
         _check(z, _r(6, 31 + i), **kw)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_sample_short_lists_of_more_equal_logits_than_are_listed(dtype):
+    V = 30001
+    g = torch.Generator().manual_seed(32)
+    z = -3.0 - torch.rand((3, V), generator=g)
+    for row, n in enumerate((2049, 5000, 29000)):
+        z[row, torch.randperm(V, generator=g)[:n]] = 0.5
+    z[0, 77] = 1.0
+    z[2, 5:900] = -math.inf
+    z = z.to(dtype)
+    for i, kw in enumerate((dict(top_k=1), dict(top_k=100), dict(top_k=300, top_p=0.5), dict(top_k=1000), dict(min_p=0.5),
+                            dict(min_p=0.03))):
+        _check(z, _r(3, 40 + i), **kw)
+        _check(z, _r(3, 50 + i), filtered=False, **kw)
+
+
 def test_sample_random_numbers_at_their_ends():
     z = _logits(8, 2048, BF, 12)
     for r in (0.0, 2.0 ** -24, LAST):

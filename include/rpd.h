@@ -607,7 +607,7 @@ size_t rpd_fp8_workspace_size(int32_t V, int32_t d, int32_t M, int32_t statistic
  * exact operands (magnitudes below 2^-126 may count as 0, and what rounds to
  * 2^128 is infinite), sums are float32. Equal rows of the head give equal
  * logits; of equal logits the lowest index is the argmax.
- *   M          0 <= M <= 2^20 (0: nothing is done)
+ *   M          0 <= M <= 2^20 (0: nothing is done), M * V <= 2^38, M * d <= 2^36
  *   x          device [M][d] of type x_dtype (bf16, fp16 or fp32), rows x_stride >= d apart
  *   logits     device [M][V] of type logits_dtype (any of the three), rows
  *              logits_stride >= V apart, not over x; or NULL

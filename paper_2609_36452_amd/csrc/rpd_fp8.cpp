@@ -15,6 +15,12 @@ rpd_status check_head(int V, int d) {
   return RPD_OK;
 }
 
+// Rows that the launches hold: at most (V / 256 + 8) (M / 128 + 2) workgroups for the tiles of a whole sum and (M / 16 + 1)
+// (d / 512 + 1) for the rows, below 2^24 each. (Sums that are cut along the columns have fewer than 512 tiles.)
+bool rows_ok(int V, int d, int M) {
+  return M >= 1 && M <= 1 << 20 && (long long)M * V <= 1LL << 38 && (long long)M * d <= 1LL << 36;
+}
+
 Fp8Dims fp8_dims(int V, int d) {
   Fp8Dims q{};
   q.V = V;
@@ -138,7 +144,7 @@ rpd_status rpd_fp8_pack(int32_t V, int32_t d, const uint8_t* codes, const float*
 }
 
 size_t rpd_fp8_workspace_size(int32_t V, int32_t d, int32_t M, int32_t statistics) {
-  if (!head_ok(V, d) || M < 1 || M > 1 << 20) return 0;
+  if (!head_ok(V, d) || !rows_ok(V, d, M)) return 0;
   const Fp8Dims q = fp8_dims(V, d);
   Fp8Call a{};
   a.M = M;
@@ -162,6 +168,8 @@ rpd_status rpd_fp8_project(int32_t V, int32_t d, const void* packed, int32_t M, 
   if (!scale_ok(logit_scale))
     return fail(RPD_ERR_BAD_PARAM, "logit_scale must be finite and > 0, or 0 for 1 (got %g)", logit_scale);
   if (M == 0) return RPD_OK;
+  if (!rows_ok(V, d, M))
+    return fail(RPD_ERR_BAD_SHAPE, "need M*V<=2^38, M*d<=2^36 (got M=%d V=%d d=%d)", M, V, d);
   if (!packed || !x) return fail(RPD_ERR_NULL_POINTER, "packed and x are required");
   const int ns = (argmax != nullptr) + (confidence != nullptr) + (entropy != nullptr);
   if (logits ? ns != 0 : ns != 3)
@@ -190,9 +198,6 @@ rpd_status rpd_fp8_project(int32_t V, int32_t d, const void* packed, int32_t M, 
   a.confidence = confidence;
   a.entropy = entropy;
   fp8_plan(q, a);
-  if ((long long)a.nrt * (a.nvt + 7) * a.splits > kMaxBlocks || (long long)a.mb * q.nc > kMaxBlocks ||
-      (long long)M * up_div(V, 4) / 256 > kMaxBlocks)
-    return fail(RPD_ERR_BAD_SHAPE, "M * V or M * d is too large (M=%d V=%d d=%d)", M, V, d);
   const Fp8Space w = fp8_space(q, a, logits == nullptr);
   if (w.bytes > 0) {
     st = check_workspace(workspace, workspace_bytes, w.bytes);

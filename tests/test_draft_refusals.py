@@ -91,6 +91,30 @@ def test_project_refusals(kw, status):
     assert s == status and rpd.last_error()
 
 
+@pytest.mark.parametrize("V,d,M,logits", [
+    (126464, 4096, 135000, False), (126464, 4096, 136000, False), (126464, 4096, 1 << 20, False), (126464, 4096, 136000, True),
+    (152064, 3584, 1 << 20, True), (1 << 18, 128, 1 << 20, False), (1 << 18, 128, 1 << 20, True), (5, 1 << 16, 1 << 20, False),
+    (5, 1 << 16, 1 << 20, True)])
+def test_project_takes_many_rows(V, d, M, logits):
+    """Rows up to the bounds of rpd.h, among them those whose logits would be more than 2^34, pass the checks of shape:
+    such calls end at the workspace, before anything is enqueued."""
+    L = rpd.lib()
+    need = L.rpd_fp8_workspace_size(V, d, M, int(not logits))
+    assert need > 0
+    out = (P << 22, V, 0, None, None, None) if logits else (None, 0, 0, P, P, P)
+    assert L.rpd_fp8_project(V, d, P, M, P, d, 0, *out, 1.0, P, need - 1, None) == 4
+
+
+@pytest.mark.parametrize("V,d,M", [((1 << 18) + 1, 128, 1 << 20), (1 << 20, 128, (1 << 18) + 1), (5, (1 << 16) + 1, 1 << 20),
+                                   (5, 1 << 20, (1 << 16) + 1)])
+def test_project_refuses_more_rows_than_launches_hold(V, d, M):
+    L = rpd.lib()
+    assert L.rpd_fp8_workspace_size(V, d, M, 0) == 0 and L.rpd_fp8_workspace_size(V, d, M, 1) == 0
+    assert L.rpd_fp8_project(V, d, P, M, P, d, 0, P << 22, V, 0, None, None, None, 1.0, P, 1 << 50, None) == 2
+    assert L.rpd_fp8_project(V, d, P, M, P, d, 0, None, 0, 0, P, P, P, 1.0, P, 1 << 50, None) == 2
+    assert "M*V" in rpd.last_error()
+
+
 def test_python_refusals():
     """Host tensors, before the library is asked."""
     codes, scales = R.make_head(10, 20, 1, "cpu")

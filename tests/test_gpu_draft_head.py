@@ -447,3 +447,22 @@ def test_two_streams_at_once_over_one_head():
     for i in range(2):
         for run in got[i]:
             assert all(torch.equal(a, b) for a, b in zip(run, want[i]))
+
+
+def test_head_more_than_2_to_the_34_logits():
+    """Logits and statistics of many rows are those of the same rows in small calls."""
+    d, V, M = 128, 126464, 136000
+    codes, scales = R.make_head(V, d, 41, DEV)
+    head = rpd.Fp8Head(codes, scales)
+    x = _x(M, d, BF, 42)
+    o, y = head.stats(x), head.logits(x)
+    assert y.numel() > 1 << 34
+    w = R.values(codes.float(), scales, 128)
+    for at in (0, 68013, M - 130):
+        part = slice(at, at + 130)
+        small = head.stats(x[part])
+        assert all(torch.equal(o[k][part], small[k]) for k in o)
+        assert torch.equal(y[part], head.logits(x[part]))
+        _check(y[part][-5:], w, _values_of(x[part][-5:]))
+    del y
+    torch.cuda.empty_cache()   # 34 GB

@@ -187,7 +187,7 @@ hipError_t launch_fp8_project(const Fp8Dims& q, const Fp8Call& a, hipStream_t s)
 
 // ------------------------------------------------------------ sample.hip --
 
-constexpr float kSampleMaxScale = 1.2676506e30f;   // 2^100: 32 times it, and a difference of logits times that, stay floats
+constexpr float kSampleMaxScale = 1.2676506e30f;   // 2^100: 64 times it stays a float
 
 struct SampleCall {
   int N, V, dtype;

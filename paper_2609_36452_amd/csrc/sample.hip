@@ -52,13 +52,16 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 // to the fourth power, the fifth spread over the others as Chebyshev
 // polynomials are (x^5 = 5/4 h^2 x^3 - 5/16 h^4 x to within h^5 / 16 for |x| <=
 // h = 1/64: 5e-13 of the mass).
+// The bin is taken of half the distance, since the whole one may be beyond float32: 3e38 and -1e38 at a scale of 1e-38 are
+// 4 nats apart. Halving is exact but for subnormals, whose lost bit is 2^-44 of a bin at the largest scale.
 struct Weigh {
-  float top, k;       // maximum, bins per unit of logit
+  float top, half, k;   // maximum, half of it, bins per unit of logit
   double m, scale;
-  __device__ __forceinline__ Weigh(float t, float s) : top(t), k(s * (float)kPerNat), m((double)t), scale((double)s) {}
+  __device__ __forceinline__ Weigh(float t, float s)
+      : top(t), half(0.5f * t), k(s * (float)kPerNat), m((double)t), scale((double)s) {}
   // nats below the maximum
   __device__ __forceinline__ double below(float z) const { return (m - (double)z) * scale; }
-  __device__ __forceinline__ float bin_of(float z) const { return rintf(fminf((top - z) * k, (float)kFar)); }
+  __device__ __forceinline__ float bin_of(float z) const { return rintf(fminf(fmaf(-0.5f, z, half) * (2.f * k), (float)kFar)); }
   __device__ __forceinline__ int bin(float z) const { return (int)bin_of(z); }
   // fixed-point mass of a logit in bin b
   __device__ __forceinline__ unsigned long long mass(float z, float b) const {
@@ -369,11 +372,12 @@ __device__ __forceinline__ Place find(const typename E::t* row, int V, const Wei
     const int b = p.bin;
     // The bin's logits are an interval; its ends, 64 steps at once. The bin falls as the key rises: the largest key of a
     // bin >= b, then the smallest of a bin <= b.
-    // It lies within 0.6 of its middle's place, a step of the floats around.
+    // It lies within 0.6 of its middle's place, a step of the floats around; where that place is beyond float32 or nearly,
+    // anywhere.
     const uint32_t least = key_of(-3.402823466e38f);
     const float far = w.top - ((float)b + 0.6f) / w.k, near = w.top - ((float)b - 0.6f) / w.k;
     const uint32_t from = b == kFar || !(far > -3.0e38f) ? least : key_of(far) - 2;
-    uint32_t lo = from, hi = b == 0 || !(near < w.top) ? top : min(top, key_of(near) + 2);
+    uint32_t lo = from, hi = b == 0 || !(near < w.top) || !(near > -3.0e38f) ? top : min(top, key_of(near) + 2);
     while (lo < hi) {   // bin(lo) >= b, the answer in lo .. hi
       const uint32_t step = (hi - lo) / 64 + 1;
       const uint32_t k = lo + (uint32_t)(lane + 1) * step;

@@ -135,6 +135,31 @@ def test_sample_extreme_temperatures(scale, dtype):
         _check(z, r, scale=scale, **kw)
 
 
+@pytest.mark.parametrize("scale", [1e-44, 1e-40, 3e-39, 1e-38, 1e-37, 1e-36])
+@pytest.mark.parametrize("dtype,V", [(F32, 3001), (BF, 3001), (BF, 170001)])
+def test_sample_rows_wider_than_float32(dtype, V, scale):
+    """Finite logits whose distance is more than the largest float32, a few nats apart at their scale: spread, in a few
+    heaps, and two tokens alone."""
+    note(f"  sample wide V={V} {dtype} scale={scale}")
+    g = torch.Generator().manual_seed(33)
+    largest = torch.finfo(dtype).max
+    z = (largest * (2.0 * torch.rand((5, V), generator=g, dtype=torch.float64) - 1.0))
+    z[1] = largest * torch.tensor([0.99, 0.5, -0.2, -0.7, -0.98], dtype=torch.float64)[torch.randint(0, 5, (V,), generator=g)]
+    z[2] = -math.inf
+    z[2, 70], z[2, 7] = 3e38, -1e38
+    z[3, ::2] = -largest
+    z[3, 5] = largest
+    z[4] = -largest
+    z[4, -1] = largest
+    z = z.to(dtype)
+    r = torch.tensor([0.4, 0.93, 0.99, 0.9, 0.7])
+    for kw in (dict(), dict(top_k=V - 1), dict(top_k=1500), dict(top_k=2900, top_p=0.9), dict(top_k=40), dict(top_p=0.7),
+               dict(min_p=0.1), dict(min_p=1e-30), dict(top_k=2000, min_p=1e-3, top_p=0.999)):
+        o = _check(z, r, scale=scale, **kw)
+        if scale == 1e-38 and not kw:   # masses 1 and e^-4
+            assert o["kept"].tolist()[2] == 2 and int(o["token"][2]) == 7
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_sample_short_lists(dtype):
     """Lists around the number of lanes and of threads, of rows whose best tokens one thread or one wave holds."""

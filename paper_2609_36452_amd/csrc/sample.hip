@@ -449,18 +449,21 @@ __device__ __forceinline__ Place find(const typename E::t* row, int V, const Wei
       const bool in = lane < (int)count;
       const uint32_t key = in ? s.few_key[lane] : 0;
       const int index = in ? s.few_index[lane] : 0;
-      const double e = in ? (double)w.mass(value_of(key), (float)b) * unit : 0.0;
+      const unsigned long long units = in ? w.mass(value_of(key), (float)b) : 0;
+      const double e = (double)units * unit;
       uint32_t above = 0, equal = 0, at = 0;
-      double mass = m;   // of what is above
+      unsigned long long over = 0;   // the mass above, whole units: the list has the order in which its places were taken
       for (int j = 0; j < (int)count; ++j) {
         const uint32_t kj = __builtin_amdgcn_readlane(key, j);
         const int ij = __builtin_amdgcn_readlane(index, j);
-        const double ej = lane_of(e, j);
+        const unsigned long long uj = (unsigned long long)__builtin_amdgcn_readlane((uint32_t)(units >> 32), j) << 32 |
+                                      (uint32_t)__builtin_amdgcn_readlane((uint32_t)units, j);
         above += kj > key;
-        mass += kj > key ? ej : 0.0;
+        over += kj > key ? uj : 0;
         equal += kj == key;
         at += kj == key && ij < index;
       }
+      const double mass = m + (double)over * unit;
       const uint32_t order = above + at;
       const double upto = mass + (double)(at + 1) * e;
       const bool past = in && (q.by_rank ? n + order >= q.rank : q.reach ? upto >= q.mass : upto > q.mass);

@@ -160,6 +160,31 @@ def test_sample_rows_wider_than_float32(dtype, V, scale):
             assert o["kept"].tolist()[2] == 2 and int(o["token"][2]) == 7
 
 
+# Bin of 1/32 nat, first place and step of 60 logits in it, and 2^24 r: r times the whole mass is within a few 2^-53 of the
+# mass up to one of them, so that sums of it in another order fall on its other side. (The one of step 1 has no such border.)
+AT_A_BORDER = [
+    (32, 15652, 10181, 14917835), (11, 4846, 1670, 13519015), (33, 6377, 10460, 7725621), (55, 11517, 13589, 10921251),
+    (25, 11358, 9261, 13022668), (56, 5649, 3802, 16270733), (29, 6957, 14084, 14108715), (24, 7546, 78, 6791878),
+    (48, 10533, 1915, 13674402), (15, 8824, 2163, 9999348), (16, 373, 14319, 14615284), (41, 11521, 13161, 14680957),
+    (18, 14536, 5898, 12996707), (49, 5976, 9214, 14714304), (28, 1382, 13015, 10623538), (46, 0, 1, 8388608),
+    (42, 3754, 3687, 8381427), (24, 6154, 4734, 13287093), (31, 1268, 6807, 7432548), (12, 4667, 832, 8346118)]
+
+
+def test_sample_sums_do_not_depend_on_places():
+    """The same logits elsewhere in the row: the same one is drawn, and as many are kept, also where a last bit decides."""
+    V, rows = 4000, 64
+    g = torch.Generator().manual_seed(34)
+    places = torch.stack([torch.randperm(V, generator=g)[:61] for _ in range(rows)])
+    for b, first, step, n in AT_A_BORDER:
+        at = (first + step * torch.arange(60)) % 16381
+        logits = torch.cat([torch.zeros(1), -b / 32.0 + (at - 8190) * 2.0 ** -20])
+        z = torch.full((rows, V), -math.inf).scatter_(1, places, logits.expand(rows, 61)).to(DEV)
+        r = torch.full((rows,), n * 2.0 ** -24, device=DEV)
+        for o in (rpd.sample(z, r), rpd.sample(z, r, top_p=n * 2.0 ** -24)):
+            drawn = z.gather(1, o["token"].long().unsqueeze(1))
+            assert drawn.unique().numel() == 1 and o["prob"].unique().numel() == 1 and o["kept"].unique().numel() == 1
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_sample_short_lists(dtype):
     """Lists around the number of lanes and of threads, of rows whose best tokens one thread or one wave holds."""

@@ -953,8 +953,11 @@ class Fp8Head:
         """x [..., d] (bfloat16, float16 or float32) through the head: [..., V] of type ``out_dtype`` (x's if None), into
         ``out`` if given. Differentiable once in x, of a head made with ``train`` (the quantization counts as the
         identity, the weights are constants, and the upstream gradient is quantized as x is); with ``out`` or
-        ``stream``, x must not require a gradient. A backward pass that is captured into a graph must not meet leaves
-        that an earlier backward pass outside it still refers to (as for any torch function)."""
+        ``stream``, x must not require a gradient. There is no forward mode: a dual tensor is refused. A backward pass
+        that is captured into a graph must not meet leaves that an earlier backward pass outside it still refers to (as
+        for any torch function)."""
+        if torch.autograd.forward_ad.unpack_dual(x).tangent is not None:
+            raise NotImplementedError("x is a dual tensor: the head has no forward-mode derivative")
         if not (x.requires_grad and torch.is_grad_enabled()):
             return self._logits(x, out_dtype, out, stream)
         if not self.train:

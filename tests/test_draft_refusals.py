@@ -124,6 +124,20 @@ def test_python_refusals():
         rpd.fp8_quantize(torch.zeros((2, 2)))
 
 
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("train", [False, True])
+def test_dual_tensors_are_refused(train, grad):
+    """Forward mode has no rule to go by: its tangent is not dropped in silence."""
+    head = object.__new__(rpd.Fp8Head)
+    head.V, head.d, head.train = 10, 20, train
+    x = torch.ones((2, 20), requires_grad=grad)
+    with torch.autograd.forward_ad.dual_level():
+        with pytest.raises(NotImplementedError, match="forward-mode"):
+            head.logits(torch.autograd.forward_ad.make_dual(x, torch.ones((2, 20))))
+        with torch.no_grad(), pytest.raises(NotImplementedError, match="forward-mode"):
+            head.logits(torch.autograd.forward_ad.make_dual(x, torch.ones((2, 20))), out=torch.empty((2, 10)))
+
+
 # ------------------------------------------------------- the float64 forms --
 
 def test_reference_codes_are_torch_casts():

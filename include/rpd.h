@@ -670,8 +670,8 @@ typedef struct rpd_sample {
   int64_t filtered_stride;
 } rpd_sample;
 
-/* Workspace bytes of rpd_sample_tokens (pointers only tested for NULL); 0 if
- * the shape is out of range or none is needed. */
+/* Workspace bytes of rpd_sample_tokens: 0, it needs none of any shape
+ * (`workspace` may be NULL and is not used). */
 size_t rpd_sample_workspace_size(const rpd_sample* p);
 rpd_status rpd_sample_tokens(const rpd_sample* p, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -1030,11 +1030,5 @@ def sample(logits: torch.Tensor, r: torch.Tensor, logit_scale: float | torch.Ten
     problem = RpdSample(rows.shape[0], rows.shape[1], code, rows.data_ptr(), _row_stride(rows), r.data_ptr(),
                         float(scale), int(k), float(p), float(least), scales, ks, ps, leasts, o["token"].data_ptr(),
                         o["prob"].data_ptr(), o["kept"].data_ptr(), _ptr(o.get("logits")), max(rows.shape[1], 1))
-    nbytes = int(lib().rpd_sample_workspace_size(ctypes.byref(problem)))
-    ws = None
-    if nbytes:
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        if stream is not None:
-            ws.record_stream(stream)
-    _enqueue(dev, stream, lib().rpd_sample_tokens, ctypes.byref(problem), _ptr(ws), nbytes)
+    _enqueue(dev, stream, lib().rpd_sample_tokens, ctypes.byref(problem), None, 0)   # (needs no workspace)
     return o

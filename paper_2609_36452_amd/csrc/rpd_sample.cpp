@@ -11,9 +11,10 @@ bool shape_ok(const rpd_sample* p) { return p->N >= 0 && p->N < 1 << 22 && p->V 
 
 extern "C" {
 
-size_t rpd_sample_workspace_size(const rpd_sample* p) { return 0; }
+// a row is one workgroup's work, in its registers and LDS
+size_t rpd_sample_workspace_size(const rpd_sample*) { return 0; }
 
-rpd_status rpd_sample_tokens(const rpd_sample* p, void* workspace, size_t workspace_bytes, void* stream) {
+rpd_status rpd_sample_tokens(const rpd_sample* p, void* /*workspace*/, size_t /*workspace_bytes*/, void* stream) {
   clear_error();
   if (!p) return fail(RPD_ERR_NULL_POINTER, "problem is NULL");
   if (!shape_ok(p)) return fail(RPD_ERR_BAD_SHAPE, "need 0<=N<2^22, 1<=V<=2^20 (got N=%d V=%d)", p->N, p->V);

@@ -182,6 +182,11 @@ def test_sample_whole_top_k(top_k):
         rpd.sample(torch.zeros((2, 8)), torch.zeros((2,)), top_k=top_k)
 
 
+def test_sample_needs_no_workspace():
+    for kw in (dict(), dict(N=1 << 20, V=1 << 20, ls=1 << 20), dict(V=0)):
+        assert rpd.lib().rpd_sample_workspace_size(ctypes.byref(_sample(**kw))) == 0
+
+
 def test_sample_nothing():
     assert rpd.lib().rpd_sample_tokens(ctypes.byref(_sample(N=0, logits=None)), None, 0, None) == 0
     assert rpd.lib().rpd_sample_tokens(None, None, 0, None) == 1

@@ -354,6 +354,18 @@ __device__ __forceinline__ int first_of(const Bound& q, uint32_t n, double m, ui
   return hits ? __builtin_ctzll(hits) : any ? 63 - __builtin_clzll(any) : 0;
 }
 
+// of eq equal tokens of mass w each, which follow n tokens of mass m, the one at which the bound is passed
+__device__ __forceinline__ uint32_t which_of(const Bound& q, uint32_t n, double m, double w, uint32_t eq) {
+  if (q.by_rank) return min(q.rank - n, eq - 1);
+  if (eq == 1) return 0;
+  auto past = [&](double i) { return q.reach ? m + (i + 1.0) * w >= q.mass : m + (i + 1.0) * w > q.mass; };
+  double i = w > 0.0 ? floor((q.mass - m) / w) : 0.0;
+  i = fmin(fmax(i, 0.0), (double)(eq - 1));
+  while (i > 0.0 && past(i - 1.0)) i -= 1.0;
+  while (i < (double)(eq - 1) && !past(i)) i += 1.0;
+  return (uint32_t)i;
+}
+
 // by the first wave: of 32 times 64 bins, whose sums follow n0 tokens of mass m0
 __device__ __forceinline__ Spot locate(const Bins& b, const Bound& q, uint32_t n0, double m0) {
   const int lane = threadIdx.x & 63, g = (lane & 31) * 64;
@@ -517,17 +529,7 @@ __device__ __forceinline__ Place find(const typename E::t* row, int V, const Wei
   p.index = -1;
   p.m = m;
   p.w = (double)w.mass(value_of(hi), (float)b) * unit;
-  if (q.by_rank) {
-    p.at = min(q.rank - n, count - 1);
-  } else {
-    // the lowest i with m + (i + 1) w past the bound
-    auto past = [&](double i) { return q.reach ? m + (i + 1.0) * p.w >= q.mass : m + (i + 1.0) * p.w > q.mass; };
-    double i = p.w > 0.0 ? floor((q.mass - m) / p.w) : 0.0;
-    i = fmin(fmax(i, 0.0), (double)(count - 1));
-    while (i > 0.0 && past(i - 1.0)) i -= 1.0;
-    while (i < (double)(count - 1) && !past(i)) i += 1.0;
-    p.at = (uint32_t)i;
-  }
+  p.at = which_of(q, n, m, p.w, count);
   return p;
 }
 
@@ -839,11 +841,6 @@ __device__ __forceinline__ uint32_t slots_of(uint32_t w) {
 
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
-struct KeyBound {
-  bool by_rank, reach;
-  uint32_t rank;
-  double mass;
-};
 struct KeyPlace {   // as Place, with a slot in place of the key
   uint32_t slot, n, eq, at;
   double m, w;
@@ -876,44 +873,27 @@ __device__ __forceinline__ uint32_t count_of(const Keys& s, uint32_t slot) {
 
 // By the first wave: the token at which a bound is passed.
 template <class E>
-__device__ __forceinline__ KeyPlace find_key(const Keys& s, const Weigh& w, const KeyBound& q) {
+__device__ __forceinline__ KeyPlace find_key(const Keys& s, const Weigh& w, const Bound& q) {
   const int lane = threadIdx.x & 63;
-  auto passed = [&](uint32_t n, double m) { return q.by_rank ? n > q.rank : q.reach ? m >= q.mass : m > q.mass; };
-  // the first of the lanes in whose running sums the bound is passed (by rounding alone, the last that holds anything)
-  auto first_of = [&](uint32_t n, double m, uint32_t before, bool in) {
-    const bool some = in && n > before;
-    const unsigned long long hits = __ballot(some && passed(n, m)), any = __ballot(some);
-    return hits ? __builtin_ctzll(hits) : any ? 63 - __builtin_clzll(any) : 0;
-  };
   // 64 blocks of the 16 times 64, the block, the value
   const int g = lane & 15;
-  const int group = first_of(s.n_upto[g * 64 + 63], s.m_upto[g * 64 + 63], g ? s.n_upto[g * 64 - 1] : 0, lane < 16);
+  const int group = first_of(q, s.n_upto[g * 64 + 63], s.m_upto[g * 64 + 63], g ? s.n_upto[g * 64 - 1] : 0, lane < 16);
   const int b0 = group * 64 + lane;
-  const int b = group * 64 + first_of(s.n_upto[b0], s.m_upto[b0], b0 ? s.n_upto[b0 - 1] : 0, true);
+  const int b = group * 64 + first_of(q, s.n_upto[b0], s.m_upto[b0], b0 ? s.n_upto[b0 - 1] : 0, true);
   const uint32_t n0 = b ? s.n_upto[b - 1] : 0;
   const double m0 = b ? s.m_upto[b - 1] : 0.0;
   const uint32_t slot = b * 64 + lane, c = count_of(s, slot);
   const double e = c ? exp(-w.below(slot_value<E>(slot))) : 0.0;
   const uint32_t n = n0 + wave_scan(c);
   const double m = m0 + wave_scan((double)c * e);
-  const int at = first_of(n, m, n - c, true);
+  const int at = first_of(q, n, m, n - c, true);
   KeyPlace p;
   p.slot = b * 64 + at;
   p.eq = __builtin_amdgcn_readlane(c, at);
   p.n = __builtin_amdgcn_readlane(n, at) - p.eq;
   p.m = at ? lane_of(m, at - 1) : m0;
   p.w = lane_of(e, at);
-  p.at = 0;
-  if (q.by_rank) {
-    p.at = min(q.rank - p.n, p.eq - 1);
-  } else if (p.eq > 1) {
-    auto over = [&](double i) { return q.reach ? p.m + (i + 1.0) * p.w >= q.mass : p.m + (i + 1.0) * p.w > q.mass; };
-    double i = p.w > 0.0 ? floor((q.mass - p.m) / p.w) : 0.0;
-    i = fmin(fmax(i, 0.0), (double)(p.eq - 1));
-    while (i > 0.0 && over(i - 1.0)) i -= 1.0;
-    while (i < (double)(p.eq - 1) && !over(i)) i += 1.0;
-    p.at = (uint32_t)i;
-  }
+  p.at = which_of(q, p.n, p.m, p.w, p.eq);
   return p;
 }
 
@@ -1253,13 +1233,13 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
     KeyPlace cut{};
     bool is_cut = false;
     if (top_k > 0 && (uint32_t)top_k < kept) {
-      cut = find_key<E>(s, w, KeyBound{true, false, (uint32_t)top_k - 1, 0.0});
+      cut = find_key<E>(s, w, Bound{true, false, (uint32_t)top_k - 1, 0.0});
       is_cut = true;
       kept = top_k;
       mass = cut.upto();
     }
     if (top_p < 1.f) {
-      const KeyPlace p = find_key<E>(s, w, KeyBound{false, true, 0, fmax((double)top_p, 0.0) * mass});
+      const KeyPlace p = find_key<E>(s, w, Bound{false, true, 0, fmax((double)top_p, 0.0) * mass});
       if (p.rank() + 1 < kept) {
         cut = p;
         is_cut = true;
@@ -1280,13 +1260,13 @@ __global__ __launch_bounds__(kThreads) void k_sample_keys(SampleCall a) {
       for (int k = 32; k >= 1; k >>= 1) in += __shfl_xor(in, k);
       in += b ? s.n_upto[b - 1] : 0;
       if (in < kept) {
-        cut = find_key<E>(s, w, KeyBound{true, false, in - 1, 0.0});
+        cut = find_key<E>(s, w, Bound{true, false, in - 1, 0.0});
         is_cut = true;
         kept = in;
         mass = cut.upto();
       }
     }
-    KeyPlace p = find_key<E>(s, w, KeyBound{false, false, 0, fmin(fmax((double)a.r[n], 0.0), 1.0) * mass});
+    KeyPlace p = find_key<E>(s, w, Bound{false, false, 0, fmin(fmax((double)a.r[n], 0.0), 1.0) * mass});
     if (is_cut && p.rank() > cut.rank()) p = cut;   // by rounding alone
     if (lane == 0) {
       s.pick = p;

@@ -103,7 +103,8 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int k, int d, const u32x
   }
 }
 
-// 16 lanes a block of a row, 8 entries each, held between the maximum and the codes: 13 x 3584 fp16 takes 2.8 us
+// 16 lanes a block of a row, 8 entries each, held between the maximum and the codes: 13 x 3584 fp16 takes 2.8 us. Many rows
+// are bound by memory: 65536 x 4096 takes 163 us of bf16 and of fp16 (5.0 TB/s), 227 of fp32 (5.9), 8192 rows 21 and 25.
 template <class E>
 __global__ __launch_bounds__(256) void k_fp8_quantize_rows(Fp8Quantize a) {
   const long long g = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
